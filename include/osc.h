@@ -50,6 +50,8 @@ enum { OSC_FMT_MXFP4_OSC = 0, OSC_FMT_FP8_E4M3_TOKEN = 1, OSC_FMT_MXFP8 = 2,
 
 enum { OSC_FMT16_E8M0 = 0, OSC_FMT16_NVFP4 = 1 };             /* 4-bit formats with one scale per 16 channels */
 
+enum { OSC_ROPE_HALVES = 0, OSC_ROPE_PAIRS = 1 };             /* which two channels of a head turn together */
+
 const char *osc_last_error(void);
 int osc_version(void);
 
@@ -365,6 +367,103 @@ int osc_dual_gemm_g16(const uint8_t *Xq, const uint8_t *Xs16, float x_tensor_sca
                       int64_t ldb, const void *Wpack, float w_tensor_scale, int64_t M, int64_t N,
                       int64_t K, int32_t K_o, int fmt16, void *Y, int y_dtype, int64_t ldy,
                       void *stream);
+
+/* ---- attention around a paged cache ------------------------------------------------------------ */
+
+/*
+ * The step between the q|k|v projection and the o projection of a serving loop: the new tokens' cache
+ * slots, norms and rotation of query and key heads with the write into the cache, attention.
+ *
+ * Cache: K and V, each bf16 [n_pages][Hkv][page_size][D], contiguous, 16-byte aligned; a page holds
+ * page_size (16, 32, 64, 128 or 256) tokens of every key/value head, n_pages * page_size < 2^31.  Token j of a
+ * request lies in page block_table[b][j / page_size], row j % page_size; slot = page * page_size + row.
+ * A batch may have a prefix that all its requests share, in pages of its own (prefix_pages); a request's own
+ * tokens follow it and start a page of their own, so prefix_len need not be a multiple of page_size.
+ */
+
+/*
+ * Pages, slots and offsets of one step from the requests' lengths, on the device (no length is read back).
+ * Request b holds kv_lens[b] own tokens and gets q_lens[b] new ones (negative lengths count as 0):
+ *   need[b]  = ceil((kv + q) / page_size) - ceil(kv / page_size)
+ *   pages    are dealt in the order of the requests from the end of the free list: the n-th page dealt is
+ *            free_pages[n_free - 1 - n]; it goes into block_table[b] behind those the request has
+ *   refused  a request whose kv + q tokens do not fit a row of the table (it asks for no page), or whose pages,
+ *            counted over all requests up to and with it, exceed n_free while it needs any: it keeps its length, its
+ *            table row is not written, its new tokens get slot -1
+ *   token i of request b is row q_offsets[b] + i: position pos_base + kv + i, slot as above.
+ *   free_pages   int32 [n_pool];  n_free int32 [1]: how many of them, from the start, are free (limited to n_pool)
+ *   block_table  int32 [B, ldt], in and out: entries of the pages a request has are read, new ones written
+ *   kv_lens_out  int32 [B]: the lengths after the step (not the array kv_lens: keep two and swap them)
+ *   q_offsets    int32 [B + 1]: running sum of q_lens, refused requests included
+ *   positions, slots  int32 [T]; T at least the sum of q_lens (tokens past T get neither slot nor page); rows past
+ *            the sum get -1 in both (a launch padded to a fixed size)
+ *   info         int32 [4]: pages left, pages taken, requests refused, tokens.  info[0] is the next step's n_free
+ *            (n_free must not point into the info that this call writes)
+ * B <= 8192.  Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
+ */
+int osc_page_slots(const int32_t *kv_lens, const int32_t *q_lens, int32_t B, int32_t page_size, const int32_t *free_pages,
+                   int64_t n_pool, const int32_t *n_free, int32_t *block_table, int64_t ldt, int32_t pos_base,
+                   int64_t T, int32_t *kv_lens_out, int32_t *q_offsets, int32_t *positions, int32_t *slots,
+                   int32_t *info, void *stream);
+
+/*
+ * Rotation angles: cos_sin float [n_pos][rot], row p = cos(p * f_i) for i < rot/2, then sin(p * f_i), with
+ * f_i = base^(-2i/rot), angles in double precision, rounded once.  rot % 8 == 0.
+ */
+int osc_rope_table(double base, int32_t rot, int64_t n_pos, float *cos_sin, void *stream);
+
+/*
+ * Norms of query and key heads, rotation by position, write into the cache; one pass over the projection's
+ * output.  For every row t and every query and key head x of D channels:
+ *   z = x / sqrt(mean(x^2) + eps) * gamma          (z = x where gamma is NULL)
+ *   y = z with its first `rot` channels turned: pair i (0 <= i < rot/2) by the angle of position pos_a(i)[t]:
+ *       (u, w) -> (u cos - w sin, w cos + u sin), cos and sin from row pos_a(i)[t] of cos_sin, column i and rot/2 + i
+ *       OSC_ROPE_HALVES: u, w are channels i and i + rot/2;  OSC_ROPE_PAIRS: channels 2i and 2i + 1
+ * in single precision, rounded once to bf16.  Values are copied.
+ *   QKV        bf16 [T, ldx]: Hq query heads, Hkv key heads, Hkv value heads of D (64 or 128) channels, 16-byte aligned rows
+ *   gamma_q, gamma_k  bf16 [D] or NULL (no norm), 16-byte aligned
+ *   positions  int32 [n_axes, ldpos]: one row an axis, 1 to 3 axes (e.g. time, height, width); sections (host, int32
+ *              [n_axes], may be NULL for one axis): the first sections[0] pairs turn by axis 0, the next sections[1] by axis
+ *              1, ...; their sum is rot/2.  A row with a position outside [0, n_pos) on any axis is padding: its queries become
+ *              zeros and nothing of it is cached.
+ *   rot        rotated channels, a multiple of 8, 0 to D (0: positions only tell padding)
+ *   slots      int32 [T]; a slot outside the cache (-1): keys and values of that row are not cached
+ *   Qn         bf16 [T, ldq], 16-byte aligned rows; may be QKV itself if ldq == ldx
+ *   Kc, Vc     the cache; both NULL: only the queries are computed (slots, n_pages, page_size are ignored)
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
+ */
+int osc_qk_norm_rope(const void *QKV, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldx, const void *gamma_q,
+                     const void *gamma_k, float eps, const float *cos_sin, int64_t n_pos, int32_t rot, int style,
+                     const int32_t *positions, int64_t ldpos, const int32_t *sections, int32_t n_axes,
+                     const int32_t *slots, void *Qn, int64_t ldq, void *Kc, void *Vc, int64_t n_pages,
+                     int32_t page_size, void *stream);
+
+/*
+ * Attention of a step's rows.  Row t = q_offsets[b] + i (i < n = q_offsets[b+1] - q_offsets[b]) of request b sees the
+ * whole prefix and the request's own tokens 0 .. L - n + i, L = kv_lens[b] (its new tokens are in the cache by now):
+ *   O[t, h] = sum_j softmax_j(scale * Q[t, h] . K[j, h / (Hq/Hkv)]) V[j, h / (Hq/Hkv)]
+ * Scores and sums are single precision; the weights are rounded to bf16 for the second product (their sum is
+ * not), O is rounded once.  A row that sees nothing (no prefix, L - n + i < 0) gives zeros, and lse -infinity.
+ * The prefix is read once for all rows of short requests, not once a request.
+ *   Q          bf16 [T, ldq], Hq heads of D (64 or 128) channels;  O bf16 [T, ldo], 16-byte aligned rows
+ *   lse        float [T, Hq] or NULL: log of the softmax's denominator, log sum_j exp(scale * q . k_j)
+ *   prefix_pages int32 [ceil(prefix_len / page_size)];  block_table int32 [B, ldt];  kv_lens int32 [B] (limited to what a
+ *              row of the table can hold);  q_offsets int32 [B + 1], non-decreasing, within [0, T]; rows outside
+ *              [q_offsets[0], q_offsets[B]) are not written
+ *              A page outside [0, n_pages) is read as page 0: nothing outside the cache is touched.
+ *              What pages hold past a request's last token does not matter; cached tokens must be finite.
+ *   scale      > 0
+ *   workspace  osc_prefix_attention_workspace_bytes(...) bytes, 256-byte aligned; contents do not matter and are
+ *              not kept; calls that may overlap need one each
+ * B <= 8192, T * Hq < 2^31.  Results are identical from run to run.
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_WORKSPACE, OSC_ERR_HIP.
+ */
+size_t osc_prefix_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len);
+int osc_prefix_attention(const void *Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void *Kc,
+                         const void *Vc, int64_t n_pages, int32_t page_size, const int32_t *prefix_pages,
+                         int64_t prefix_len, const int32_t *block_table, int64_t ldt, const int32_t *kv_lens,
+                         const int32_t *q_offsets, int32_t B, float scale, void *O, int64_t ldo, float *lse,
+                         void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- offline profiling (calibration) ------------------------------------------ */
 

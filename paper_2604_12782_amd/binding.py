@@ -13,6 +13,7 @@ import torch
 OSC_DT_F32, OSC_DT_BF16 = 0, 1
 OSC_FMT_MXFP4_OSC, OSC_FMT_FP8_E4M3_TOKEN, OSC_FMT_MXFP8, OSC_FMT_MXFP4_OSC_G64 = 0, 1, 2, 3
 OSC_FMT16_E8M0, OSC_FMT16_NVFP4 = 0, 1
+OSC_ROPE_HALVES, OSC_ROPE_PAIRS = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libosc.so")
@@ -62,6 +63,13 @@ _SIGS = {
                                     i64, vp]),
     "osc_grouped_dual_gemm": (C.c_int, [vp, vp, vp, i64, vp, vp, i32, i64, vp, i64, i64, i32, vp,
                                         C.c_int, i64, vp]),
+    "osc_page_slots": (C.c_int, [vp, vp, i32, i32, vp, i64, vp, vp, i64, i32, i64, vp, vp, vp, vp, vp, vp]),
+    "osc_rope_table": (C.c_int, [C.c_double, i32, i64, vp, vp]),
+    "osc_qk_norm_rope": (C.c_int, [vp, i64, i32, i32, i32, i64, vp, vp, C.c_float, vp, i64, i32, C.c_int, vp, i64, vp, i32, vp, vp, i64, vp,
+                                   vp, i64, i32, vp]),
+    "osc_prefix_attention_workspace_bytes": (sz, [i64, i32, i32, i32, i32, i64]),
+    "osc_prefix_attention": (C.c_int, [vp, i64, i32, i32, i32, i64, vp, vp, i64, i32, vp, i64, vp, i64, vp, vp, i32, C.c_float, vp, i64, vp,
+                                       vp, sz, vp]),
 }
 
 
@@ -413,3 +421,39 @@ def osc_swiglu_quantize_act(G, U, want_y=False, out=None):
 def osc_swiglu_quantize_act_fp8(G, U, want_y=False, out=None):
     """SwiGLU + per-token FP8 quantiser in one pass -> (X8 uint8 [M, K], xs float32 [M], Yn uint16 [M, K] or None)."""
     return (_native or _load_native()).swiglu_quantize_act_fp8(G, U, want_y, out)
+
+
+def osc_page_slots(kv_lens, q_lens, free_pages, n_free, block_table, page_size, T, pos_base=0, out=None):
+    """Cache pages and slots of one step from lengths on the device -> (kv_lens after the step [B], q_offsets [B + 1], positions [T],
+    slots [T], info [4]), all int32; new pages are written into `block_table` [B, pages].  info[:1] is the next step's n_free."""
+    return (_native or _load_native()).page_slots(kv_lens, q_lens, free_pages, n_free, block_table, page_size, T, pos_base, out)
+
+
+def osc_rope_table(base, rot, n_pos, device="cuda", out=None):
+    """float32 [n_pos, rot]: cosines, then sines, of position * base^(-2i/rot), computed in double precision."""
+    if out is None:
+        out = torch.empty((n_pos, rot), dtype=torch.float32, device=device)
+    assert out.dtype == torch.float32 and out.is_contiguous() and tuple(out.shape) == (n_pos, rot), "need a float32 [n_pos, rot] table"
+    _check(lib().osc_rope_table(base, rot, n_pos, _ptr(out), _stream()))
+    return out
+
+
+def osc_qk_norm_rope(QKV, Hq, Hkv, D, cos_sin, positions, slots=None, Kc=None, Vc=None, gamma_q=None, gamma_k=None, eps=1e-6, rot=None,
+                     style=OSC_ROPE_HALVES, sections=None, out=None):
+    """Per-head norms, rotation and cache write of a projection's output [T, (Hq + 2 Hkv) D] -> queries bf16 [T, Hq D].
+    cos_sin float32 [n_pos, rot]; positions int32 [T] or [axes, T] with `sections` pairs an axis; Kc, Vc bf16
+    [pages, Hkv, page_size, D], updated in place at `slots` (int32 [T])."""
+    return (_native or _load_native()).qk_norm_rope(QKV, Hq, Hkv, D, cos_sin, positions, slots, Kc, Vc, gamma_q, gamma_k, eps, rot, style,
+                                                    sections, out)
+
+
+def osc_prefix_attention_workspace_bytes(T, B, Hq, Hkv, D, prefix_len):
+    return lib().osc_prefix_attention_workspace_bytes(T, B, Hq, Hkv, D, prefix_len)
+
+
+def osc_prefix_attention(Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets, scale=None, want_lse=False,
+                         workspace=None, out=None):
+    """Attention of rows Q [T, Hq D] over a shared prefix and each request's own cached tokens -> (O bf16 [T, Hq D], lse float32
+    [T, Hq] or None).  scale: D^-0.5 if None; workspace: uint8 device tensor of osc_prefix_attention_workspace_bytes(...), made here if None."""
+    return (_native or _load_native()).prefix_attention(Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets,
+                                                        scale, want_lse, workspace, out)

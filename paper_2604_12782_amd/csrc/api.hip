@@ -669,4 +669,131 @@ int osc_profile_calibrate_static(const void* X, int64_t S, int64_t H, int64_t ld
                                            n_hit, density, cbar, T_out, as_stream(stream));
 }
 
+// ---- attention around a paged cache ----
+
+static int check_page_size(const char* who, int32_t page_size, int* lg) {
+    REQUIRE(page_size >= 16 && page_size <= 256 && (page_size & (page_size - 1)) == 0, OSC_ERR_UNSUPPORTED,
+            "%s: page size %d (16, 32, 64, 128 or 256)", who, page_size);
+    *lg = __builtin_ctz((unsigned)page_size);
+    return OSC_OK;
+}
+
+static int check_heads(const char* who, int64_t T, int32_t Hq, int32_t Hkv, int32_t D) {
+    REQUIRE(T >= 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0, OSC_ERR_SHAPE, "%s: T=%lld Hq=%d Hkv=%d (Hq is a multiple of Hkv)", who, (long long)T,
+            Hq, Hkv);
+    REQUIRE(D == 64 || D == 128, OSC_ERR_UNSUPPORTED, "%s: heads of %d channels (64 or 128)", who, D);
+    REQUIRE(Hq <= 65536 / D && Hkv <= 65536 / D, OSC_ERR_UNSUPPORTED, "%s: %d heads of %d channels (at most 65536 channels)", who, Hq, D);
+    REQUIRE(T <= 0x7fffffff / Hq, OSC_ERR_UNSUPPORTED, "%s: T=%lld rows of %d heads are more than 2^31-1", who, (long long)T, Hq);
+    return OSC_OK;
+}
+
+static int check_cache(const char* who, int64_t n_pages, int lg, int32_t Hkv, const void* K, const void* V) {
+    REQUIRE(n_pages >= 0 && n_pages << lg <= 0x7fffffff, OSC_ERR_SHAPE, "%s: %lld pages (at most 2^31-1 slots)", who, (long long)n_pages);
+    REQUIRE(aligned(K, 16) && aligned(V, 16), OSC_ERR_UNSUPPORTED, "%s: the cache must be 16-byte aligned", who);
+    return OSC_OK;
+}
+
+int osc_page_slots(const int32_t* kv_lens, const int32_t* q_lens, int32_t B, int32_t page_size, const int32_t* free_pages, int64_t n_pool,
+                   const int32_t* n_free, int32_t* block_table, int64_t ldt, int32_t pos_base, int64_t T, int32_t* kv_lens_out,
+                   int32_t* q_offsets, int32_t* positions, int32_t* slots, int32_t* info, void* stream) {
+    int lg = 0, rc = check_page_size("osc_page_slots", page_size, &lg);
+    if (rc) return rc;
+    REQUIRE(B >= 0 && T >= 0 && ldt >= 0 && n_pool >= 0 && pos_base >= 0, OSC_ERR_SHAPE, "osc_page_slots: B=%d T=%lld ldt=%lld n_pool=%lld pos_base=%d", B,
+            (long long)T, (long long)ldt, (long long)n_pool, pos_base);
+    REQUIRE(B <= PAGED_MAX_REQUESTS, OSC_ERR_UNSUPPORTED, "osc_page_slots: %d requests (at most %d)", B, PAGED_MAX_REQUESTS);
+    REQUIRE(T <= 0x7fffffff && n_pool <= 0x7fffffff && ldt <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "osc_page_slots: an extent above 2^31-1");
+    if (B == 0) return OSC_OK;
+    REQUIRE(kv_lens && q_lens && n_free && kv_lens_out && q_offsets && info, OSC_ERR_NULL, "osc_page_slots: null pointer");
+    REQUIRE((free_pages || n_pool == 0) && (block_table || ldt == 0) && ((positions && slots) || T == 0), OSC_ERR_NULL,
+            "osc_page_slots: null pointer to an array that is not empty");
+    REQUIRE(kv_lens_out + B <= kv_lens || kv_lens + B <= kv_lens_out, OSC_ERR_UNSUPPORTED,
+            "osc_page_slots: the new lengths need an array of their own (every workgroup reads the old ones)");
+    REQUIRE(n_free < info || n_free >= info + 4, OSC_ERR_UNSUPPORTED, "osc_page_slots: n_free lies inside info, which this call writes");
+    return launch_page_slots(kv_lens, q_lens, B, lg, free_pages, n_pool, n_free, block_table, ldt, pos_base, T, kv_lens_out, q_offsets,
+                             positions, slots, info, as_stream(stream));
+}
+
+int osc_rope_table(double base, int32_t rot, int64_t n_pos, float* cos_sin, void* stream) {
+    REQUIRE(n_pos >= 0 && rot > 0 && rot % 8 == 0, OSC_ERR_SHAPE, "osc_rope_table: n_pos=%lld rot=%d (a multiple of 8)", (long long)n_pos, rot);
+    REQUIRE(base > 0.0 && base <= 1e30, OSC_ERR_SHAPE, "osc_rope_table: base %g", base);
+    REQUIRE(rot <= 65536 && n_pos <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "osc_rope_table: rot=%d n_pos=%lld", rot, (long long)n_pos);
+    if (n_pos == 0) return OSC_OK;
+    REQUIRE(cos_sin, OSC_ERR_NULL, "osc_rope_table: null pointer");
+    return launch_rope_table(base, rot, n_pos, cos_sin, as_stream(stream));
+}
+
+int osc_qk_norm_rope(const void* QKV, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldx, const void* gamma_q, const void* gamma_k,
+                     float eps, const float* cos_sin, int64_t n_pos, int32_t rot, int style, const int32_t* positions, int64_t ldpos,
+                     const int32_t* sections, int32_t n_axes, const int32_t* slots, void* Qn, int64_t ldq, void* Kc, void* Vc, int64_t n_pages,
+                     int32_t page_size, void* stream) {
+    static const char* who = "osc_qk_norm_rope";
+    int lg = 4, rc = check_heads(who, T, Hq, Hkv, D);
+    if (rc) return rc;
+    REQUIRE(!Kc == !Vc, OSC_ERR_NULL, "%s: one of the two caches is null", who);
+    if (Kc) {
+        rc = check_page_size(who, page_size, &lg);
+        if (rc) return rc;
+        rc = check_cache(who, n_pages, lg, Hkv, Kc, Vc);
+        if (rc) return rc;
+    }
+    REQUIRE(rot >= 0 && rot <= D && rot % 8 == 0, OSC_ERR_SHAPE, "%s: %d rotated channels of %d (a multiple of 8)", who, rot, D);
+    REQUIRE(style == OSC_ROPE_HALVES || style == OSC_ROPE_PAIRS, OSC_ERR_UNSUPPORTED, "%s: style %d", who, style);
+    REQUIRE(n_axes >= 1 && n_axes <= 3, OSC_ERR_UNSUPPORTED, "%s: %d axes of positions (1 to 3)", who, n_axes);
+    if (n_axes > 1) {
+        REQUIRE(sections, OSC_ERR_NULL, "%s: null sections", who);
+        int64_t sum = 0;
+        for (int32_t a = 0; a < n_axes; ++a) {
+            REQUIRE(sections[a] >= 0, OSC_ERR_SHAPE, "%s: section %d of %d pairs", who, a, sections[a]);
+            sum += sections[a];
+        }
+        REQUIRE(sum == rot / 2, OSC_ERR_SHAPE, "%s: sections of %lld pairs in all, %d are rotated", who, (long long)sum, rot / 2);
+        REQUIRE(ldpos >= T, OSC_ERR_SHAPE, "%s: ldpos=%lld", who, (long long)ldpos);
+    }
+    REQUIRE(ldx >= (int64_t)(Hq + 2 * Hkv) * D && ldq >= (int64_t)Hq * D, OSC_ERR_SHAPE, "%s: ldx=%lld ldq=%lld", who, (long long)ldx, (long long)ldq);
+    REQUIRE(eps >= 0.0f, OSC_ERR_SHAPE, "%s: eps=%g", who, (double)eps);
+    REQUIRE(n_pos >= 0, OSC_ERR_SHAPE, "%s: n_pos=%lld", who, (long long)n_pos);
+    if (T == 0) return OSC_OK;
+    REQUIRE(QKV && Qn && positions && (cos_sin || n_pos == 0 || rot == 0) && (!Kc || slots), OSC_ERR_NULL, "%s: null pointer", who);
+    REQUIRE(aligned(QKV, 16) && aligned(Qn, 16) && ldx % 8 == 0 && ldq % 8 == 0 && aligned(cos_sin, 16) && aligned(gamma_q, 16) &&
+                aligned(gamma_k, 16), OSC_ERR_UNSUPPORTED, "%s: rows, weights and angles must be 16-byte aligned", who);
+    return launch_qk_norm_rope(QKV, T, Hq, Hkv, D, ldx, gamma_q, gamma_k, eps, cos_sin, n_pos, rot, style == OSC_ROPE_PAIRS, positions, ldpos,
+                               n_axes, sections, slots, Qn, ldq, Kc, Vc, n_pages, lg, as_stream(stream));
+}
+
+size_t osc_prefix_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
+    if (T < 0 || B < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || prefix_len < 0) return 0;
+    return prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len);
+}
+
+int osc_prefix_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void* Kc, const void* Vc,
+                         int64_t n_pages, int32_t page_size, const int32_t* prefix_pages, int64_t prefix_len, const int32_t* block_table,
+                         int64_t ldt, const int32_t* kv_lens, const int32_t* q_offsets, int32_t B, float scale, void* O, int64_t ldo, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    static const char* who = "osc_prefix_attention";
+    int lg = 0, rc = check_heads(who, T, Hq, Hkv, D);
+    if (rc) return rc;
+    rc = check_page_size(who, page_size, &lg);
+    if (rc) return rc;
+    rc = check_cache(who, n_pages, lg, Hkv, Kc, Vc);
+    if (rc) return rc;
+    REQUIRE(B >= 0 && ldt >= 0 && prefix_len >= 0, OSC_ERR_SHAPE, "%s: B=%d ldt=%lld prefix_len=%lld", who, B, (long long)ldt, (long long)prefix_len);
+    REQUIRE(B <= PAGED_MAX_REQUESTS, OSC_ERR_UNSUPPORTED, "%s: %d requests (at most %d)", who, B, PAGED_MAX_REQUESTS);
+    REQUIRE(prefix_len <= 0x3fffffff && ldt <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "%s: prefix_len=%lld ldt=%lld", who, (long long)prefix_len, (long long)ldt);
+    REQUIRE(ldq >= (int64_t)Hq * D && ldo >= (int64_t)Hq * D, OSC_ERR_SHAPE, "%s: ldq=%lld ldo=%lld", who, (long long)ldq, (long long)ldo);
+    REQUIRE(scale > 0.0f && scale <= 1e6f, OSC_ERR_SHAPE, "%s: scale %g (a positive number)", who, (double)scale);
+    if (T == 0 || B == 0) return OSC_OK;
+    REQUIRE(Q && O && kv_lens && q_offsets && workspace && (block_table || ldt == 0) && (prefix_pages || prefix_len == 0), OSC_ERR_NULL,
+            "%s: null pointer", who);
+    REQUIRE((Kc && Vc && n_pages > 0) || (prefix_len == 0 && ldt == 0), OSC_ERR_NULL, "%s: no cache", who);
+    REQUIRE(aligned(Q, 16) && ldq % 8 == 0 && aligned(O, 16) && ldo % 8 == 0, OSC_ERR_UNSUPPORTED, "%s: rows must be 16-byte aligned", who);
+    REQUIRE(aligned(workspace, 256), OSC_ERR_UNSUPPORTED, "%s: workspace must be 256-byte aligned", who);
+    const size_t need = prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len);
+    REQUIRE(workspace_bytes >= need, OSC_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
+    AttnCall a;
+    a.Q = Q, a.T = T, a.Hq = Hq, a.Hkv = Hkv, a.D = D, a.ldq = ldq, a.K = Kc, a.V = Vc, a.n_pages = n_pages, a.lg = lg;
+    a.prefix_pages = prefix_pages, a.prefix_len = prefix_len, a.table = block_table, a.ldt = ldt, a.kv_lens = kv_lens, a.q_offsets = q_offsets;
+    a.B = B, a.scale = scale, a.O = O, a.ldo = ldo, a.lse = lse, a.workspace = static_cast<uint8_t*>(workspace);
+    return launch_prefix_attention(a, as_stream(stream));
+}
+
 }  // extern "C"

@@ -11,6 +11,8 @@
 #include <torch/csrc/utils/device_lazy_init.h>
 #include <torch/types.h>
 
+#include <cmath>
+
 #include "../../include/osc.h"
 
 namespace {
@@ -368,6 +370,165 @@ PyObject* quantize_act_dynamic(PyObject* const* a) {
     return tuple({&q, &s, &b, &idx});
 }
 
+[[noreturn]] void reject(const char* what) {
+    PyErr_SetString(PyExc_AssertionError, what);
+    throw PyFailed();
+}
+// a contiguous int32 tensor of at least n elements on `like`'s device (null for None)
+int32_t* ints(PyObject* o, int64_t n, const at::Tensor& like, const char* what) {
+    if (none(o)) return nullptr;
+    const at::Tensor& t = tensor(o);
+    if (t.scalar_type() != at::kInt || !t.is_contiguous() || t.numel() < n || t.device() != like.device()) reject(what);
+    return t.data_ptr<int32_t>();
+}
+int64_t rows_pitch(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+// rows16 of at least `width` columns, on `like`'s device
+const at::Tensor& rows16_of(PyObject* o, int64_t n, int64_t width, const at::Tensor& like, const char* what) {
+    const at::Tensor& t = rows16(o);
+    if (t.size(0) < n || t.size(1) < width || t.device() != like.device()) reject(what);
+    return t;
+}
+struct Cache {
+    void* data = nullptr;
+    int64_t pages = 0;
+    int32_t page_size = 16;
+    Cache(PyObject* o, int64_t Hkv, int64_t D, const at::Tensor& like) {
+        if (none(o)) return;
+        const at::Tensor& t = tensor(o);
+        if (!(t.dim() == 4 && t.is_contiguous() && t.element_size() == 2 && t.size(1) == Hkv && t.size(3) == D && t.device() == like.device()))
+            reject("need a contiguous bf16 cache [pages, Hkv, page_size, D]");
+        data = t.data_ptr(), pages = t.size(0), page_size = (int32_t)t.size(2);
+    }
+};
+
+// kv_lens, q_lens, free_pages, n_free, block_table, page_size, T, pos_base, out
+PyObject* page_slots(PyObject* const* a) {
+    const at::Tensor& kv = tensor(a[0]);
+    const int64_t B = kv.numel(), T = num(a[6]);
+    const int32_t ps = (int32_t)num(a[5]), base = (int32_t)num(a[7]);
+    const int32_t *pk = ints(a[0], B, kv, "kv_lens: int32 [B]"), *pq = ints(a[1], B, kv, "q_lens: int32 [B]");
+    const int32_t* pf = ints(a[2], 0, kv, "free_pages: int32 [pool]");
+    const int64_t pool = count(a[2]);
+    const int32_t* pn = ints(a[3], 1, kv, "n_free: int32 [1]");
+    const at::Tensor& table = tensor(a[4]);
+    if (!(table.dim() == 2 && table.scalar_type() == at::kInt && table.size(0) == B && table.stride(1) == 1 && table.device() == kv.device()))
+        reject("block_table: int32 [B, pages]");
+    // a row's width, not its pitch, is what a request may use; the pitch places the rows
+    const int64_t width = table.size(1), pitch_t = B > 1 ? table.stride(0) : width;
+    if (pitch_t != width) reject("block_table: rows one behind the other");
+    Ref lens, offs, pos, slots, info;
+    const Outs outs(a[8], 5);
+    if (outs) {
+        Ref* r[5] = {&lens, &offs, &pos, &slots, &info};
+        for (int i = 0; i < 5; ++i) r[i]->share(outs.item[i]);
+    } else {
+        lens.own(fresh(kv, {B}, at::kInt));
+        offs.own(fresh(kv, {B + 1}, at::kInt));
+        pos.own(fresh(kv, {T < 0 ? 0 : T}, at::kInt));
+        slots.own(fresh(kv, {T < 0 ? 0 : T}, at::kInt));
+        info.own(fresh(kv, {4}, at::kInt));
+    }
+    int32_t *o0 = ints(lens.o, B, kv, "lengths: int32 [B]"), *o1 = ints(offs.o, B + 1, kv, "q_offsets: int32 [B + 1]"),
+            *o2 = ints(pos.o, T, kv, "positions: int32 [T]"), *o3 = ints(slots.o, T, kv, "slots: int32 [T]"), *o4 = ints(info.o, 4, kv, "info: int32 [4]");
+    int32_t* pt = table.data_ptr<int32_t>();
+    if (B > 0x7fffffff) reject("too many requests");
+    enqueue([&](void* st) { return osc_page_slots(pk, pq, (int32_t)B, ps, pf, pool, pn, pt, width, base, T, o0, o1, o2, o3, o4, st); });
+    return tuple({&lens, &offs, &pos, &slots, &info});
+}
+
+// QKV, Hq, Hkv, D, cos_sin, positions, slots, Kc, Vc, gamma_q, gamma_k, eps, rot, style, sections, out
+PyObject* qk_norm_rope(PyObject* const* a) {
+    const at::Tensor& X = rows16(a[0]);
+    const int64_t T = X.size(0), Hq = num(a[1]), Hkv = num(a[2]), D = num(a[3]);
+    if (Hq < 0 || Hkv < 0 || D < 0 || Hq > 65536 || Hkv > 65536 || D > 65536 || X.size(1) < (Hq + 2 * Hkv) * D) reject("QKV: bf16 [T, (Hq + 2 Hkv) D]");
+    const at::Tensor& cs = tensor(a[4]);
+    if (!(cs.dim() == 2 && cs.scalar_type() == at::kFloat && cs.is_contiguous() && cs.device() == X.device())) reject("cos_sin: float32 [n_pos, rot]");
+    const int64_t rot = none(a[12]) ? cs.size(1) : num(a[12]);
+    if (cs.size(1) != rot) reject("cos_sin: float32 [n_pos, rot]");
+    const at::Tensor& pos = tensor(a[5]);
+    const int64_t axes = pos.dim() == 2 ? pos.size(0) : 1;
+    if (!(pos.dim() >= 1 && pos.dim() <= 2 && pos.scalar_type() == at::kInt && pos.is_contiguous() && pos.size(-1) == T && pos.device() == X.device()))
+        reject("positions: int32 [T] or [axes, T]");
+    int32_t sec[3] = {0, 0, 0};
+    Ref seq;
+    if (axes > 1 && axes <= 3) {
+        seq.own(PySequence_Fast(a[14], "`sections` is a sequence of numbers"));
+        if (!seq.o) throw PyFailed();
+        if (PySequence_Fast_GET_SIZE(seq.o) != axes) reject("sections: one number an axis");
+        for (int64_t i = 0; i < axes; ++i) sec[i] = (int32_t)num(PySequence_Fast_GET_ITEM(seq.o, i));
+    }
+    const Cache K(a[7], Hkv, D, X), V(a[8], Hkv, D, X);
+    if (!none(a[7]) && !none(a[8]) && (K.pages != V.pages || K.page_size != V.page_size)) reject("the two caches differ in shape");
+    const int32_t* ps = ints(a[6], T, X, "slots: int32 [T]");
+    void* g[2];
+    for (int i = 0; i < 2; ++i) {
+        if (!none(a[9 + i])) {
+            const at::Tensor& t = tensor(a[9 + i]);
+            if (t.element_size() != 2 || t.numel() != D || !t.is_contiguous() || t.device() != X.device()) reject("gamma: bf16 [D]");
+        }
+        g[i] = ptr(a[9 + i]);
+    }
+    const float eps = real(a[11]);
+    const int style = (int)num(a[13]);
+    Ref y;
+    if (!none(a[15])) y.share(a[15]);
+    else y.own(fresh(X, {T, Hq * D}, at::kBFloat16));
+    const at::Tensor& Y = rows16_of(y.o, T, Hq * D, X, "out: bf16 [T, Hq D]");
+    void *x = X.data_ptr(), *py = Y.data_ptr();
+    const int64_t ldx = rows_pitch(X), ldy = rows_pitch(Y);
+    enqueue([&](void* st) {
+        return osc_qk_norm_rope(x, T, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, ldx, g[0], g[1], eps, cs.data_ptr<float>(), cs.size(0), (int32_t)rot, style,
+                                pos.data_ptr<int32_t>(), T, axes > 1 ? sec : nullptr, (int32_t)axes, ps, py, ldy, K.data, V.data, K.pages,
+                                K.page_size, st);
+    });
+    return y.give();
+}
+
+// Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets, scale, want_lse, workspace, out
+PyObject* prefix_attention(PyObject* const* a) {
+    const at::Tensor& Q = rows16(a[0]);
+    const int64_t T = Q.size(0), Hq = num(a[1]), Hkv = num(a[2]), D = num(a[3]), P = num(a[7]);
+    if (Hq <= 0 || Hkv <= 0 || D <= 0 || Hq > 65536 || Hkv > 65536 || D > 65536 || Q.size(1) < Hq * D) reject("Q: bf16 [T, Hq D]");
+    const Cache K(a[4], Hkv, D, Q), V(a[5], Hkv, D, Q);
+    if (K.pages != V.pages || K.page_size != V.page_size) reject("the two caches differ in shape");
+    const int32_t* pp = ints(a[6], P > 0 ? (P + K.page_size - 1) / K.page_size : 0, Q, "prefix_pages: int32, one a page of the prefix");
+    const at::Tensor& table = tensor(a[8]);
+    if (!(table.dim() == 2 && table.scalar_type() == at::kInt && table.is_contiguous() && table.device() == Q.device())) reject("block_table: int32 [B, pages]");
+    const int64_t B = table.size(0);
+    if (B > 0x7fffffff) reject("too many requests");
+    const int32_t *kl = ints(a[9], B, Q, "kv_lens: int32 [B]"), *qo = ints(a[10], B + 1, Q, "q_offsets: int32 [B + 1]");
+    const float scale = none(a[11]) ? 1.0f / sqrtf((float)D) : real(a[11]);
+    Ref o, lse, ws;
+    const Outs outs(a[14], 2);
+    if (outs) {
+        o.share(outs.item[0]);
+        lse.share(outs.item[1]);
+    } else {
+        o.own(fresh(Q, {T, Hq * D}, at::kBFloat16));
+        if (truth(a[12])) lse.own(fresh(Q, {T, Hq}, at::kFloat));
+        else lse.share(Py_None);
+    }
+    const at::Tensor& O = rows16_of(o.o, T, Hq * D, Q, "out: bf16 [T, Hq D]");
+    if (!none(lse.o)) {
+        const at::Tensor& t = tensor(lse.o);
+        if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() < T * Hq || t.device() != Q.device()) reject("lse: float32 [T, Hq]");
+    }
+    if (none(a[13])) {
+        const int64_t n = (int64_t)osc_prefix_attention_workspace_bytes(T, (int32_t)B, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, P);
+        ws.own(fresh(Q, {n}, at::kByte));
+    } else ws.share(a[13]);
+    const at::Tensor& W = tensor(ws.o);
+    if (!W.is_contiguous() || W.device() != Q.device()) reject("workspace: a contiguous device tensor");
+    void *q = Q.data_ptr(), *po = O.data_ptr(), *pl = ptr(lse.o), *pw = W.data_ptr();
+    const int64_t ldq = rows_pitch(Q), ldo = rows_pitch(O), ldt = table.size(1);
+    const int32_t* pt = table.data_ptr<int32_t>();
+    enqueue([&](void* st) {
+        return osc_prefix_attention(q, T, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, ldq, K.data, V.data, K.pages, K.page_size, pp, P, pt, ldt, kl, qo,
+                                    (int32_t)B, scale, po, ldo, (float*)pl, pw, W.nbytes(), st);
+    });
+    return tuple({&o, &lse});
+}
+
 PyObject* current_stream(PyObject* const*) { return PyLong_FromVoidPtr(stream()); }
 
 PyObject* bind_error(PyObject* const* a) {
@@ -395,6 +556,9 @@ PyMethodDef methods[] = {
     OSC_NATIVE("quantize_act_g16", quantize_act_g16, 6),
     OSC_NATIVE("dual_gemm_g16", dual_gemm_g16, 12),
     OSC_NATIVE("quantize_act_dynamic", quantize_act_dynamic, 4),
+    OSC_NATIVE("page_slots", page_slots, 9),
+    OSC_NATIVE("qk_norm_rope", qk_norm_rope, 16),
+    OSC_NATIVE("prefix_attention", prefix_attention, 15),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling of the per-step calls", -1, methods,

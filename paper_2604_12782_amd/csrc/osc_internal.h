@@ -122,6 +122,39 @@ int launch_dual_gemm_g16(const uint8_t* Xq, const uint8_t* Xs, float xts, const 
                          const uint8_t* Ws, const uint16_t* WLt, int64_t ldwl, float wts, int64_t M, int64_t N, int64_t K,
                          int32_t K_o, int fmt, void* Y, int y_dtype, int64_t ldy, hipStream_t st);
 
+// attention around the cache: pages, norms with rotation (paged.hip), attention (attention.hip)
+int launch_page_slots(const int32_t* kv_lens, const int32_t* q_lens, int32_t B, int lg, const int32_t* free_pages, int64_t n_pool,
+                      const int32_t* n_free, int32_t* table, int64_t ldt, int32_t pos_base, int64_t T, int32_t* kv_out,
+                      int32_t* q_offsets, int32_t* positions, int32_t* slots, int32_t* info, hipStream_t st);
+int launch_rope_table(double base, int32_t rot, int64_t n_pos, float* out, hipStream_t st);
+int launch_qk_norm_rope(const void* X, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldx, const void* gq, const void* gk,
+                        float eps, const float* cos_sin, int64_t n_pos, int32_t rot, bool pairs, const int32_t* pos, int64_t ldpos,
+                        int32_t n_axes, const int32_t* sections, const int32_t* slots, void* Y, int64_t ldy, void* K, void* V,
+                        int64_t n_pages, int lg, hipStream_t st);
+struct AttnCall {
+    const void* Q;
+    int64_t T;
+    int32_t Hq, Hkv, D;
+    int64_t ldq;
+    const void *K, *V;  // pages [n_pages][Hkv][1 << lg][D]
+    int64_t n_pages;
+    int lg;
+    const int32_t* prefix_pages;
+    int64_t prefix_len;
+    const int32_t* table;
+    int64_t ldt;
+    const int32_t *kv_lens, *q_offsets;
+    int32_t B;
+    float scale;
+    void* O;
+    int64_t ldo;
+    float* lse;  // or null
+    uint8_t* workspace;
+};
+constexpr int32_t PAGED_MAX_REQUESTS = 8192;  // both kernels hold the requests' running sums in LDS
+size_t prefix_attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len);
+int launch_prefix_attention(const AttnCall& a, hipStream_t st);
+
 struct GemmProblem {
     // activations
     const uint8_t* Xq;   // dual: codes [*, K/2]; fp8, mxfp8: codes [*, K]

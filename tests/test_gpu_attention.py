@@ -1,0 +1,346 @@
+"""Cache pages, per-head norms with rotation, and attention behind a shared prefix, on the GPU against their plain
+forms in 64 bits (oracle/attention.py).
+
+Tolerances.  bf16 results are rounded once: 2^-8 of the value.  Norm and rotation are about 30 single-precision
+operations on terms no larger than the pair's length: 2^-19 of it.  Attention weights are rounded to bf16 before
+the second product: 2^-8 of the weighted average of |v|; scores are sums of D products (D 2^-24 of the sum of their
+magnitudes, times the scale), and an error of a score is a relative error of its weight."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def osc():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2604_12782_amd as m
+    m.lib()
+    return m
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+# ---- pages and slots ----------------------------------------------------------------------------------------------
+
+
+def check_slots(osc, kv, q, ps, n_pool, n_free, width, T, base=0, seed=0):
+    gen = np.random.default_rng(seed)
+    B = len(kv)
+    pages = gen.permutation(n_pool + B * width)
+    free, table = pages[:n_pool], pages[n_pool:].reshape(B, width)
+    want = ref.page_slots(kv, q, ps, free, n_free, table, T, base)
+    d_table = i32(table)
+    got = osc.osc_page_slots(i32(kv), i32(q), i32(free), i32([n_free]), d_table, ps, T, base)
+    for name, g, w in zip(("lengths", "offsets", "positions", "slots", "info", "table"), (*got, d_table), want):
+        assert np.array_equal(g.cpu().numpy(), w), name
+    return got
+
+
+@pytest.mark.parametrize("ps", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 255, 256, 257, 1025])
+def test_slots(osc, B, ps):
+    gen = np.random.default_rng(B * 7 + ps)
+    kv, q = gen.integers(0, 3 * ps, B), gen.integers(0, 2 * ps, B)
+    kv[gen.random(B) < 0.3] = ps  # full pages
+    q[gen.random(B) < 0.3] = 1
+    q[gen.random(B) < 0.2] = 0
+    check_slots(osc, kv, q, ps, 3 * B + 5, 3 * B + 5, 6, int(q.sum()), 11)
+    check_slots(osc, kv, q, ps, 3 * B + 5, 3 * B + 2, 6, int(q.sum()) + 77, 0)  # padded rows; not the whole list is free
+
+
+def test_slots_refused(osc):
+    kv, q = [0, 15, 16, 40, 5, 0, 3], [33, 1, 1, 200, 11, 0, 30]
+    for n_free in range(0, 9):  # the fourth asks for more than its row of the table; others run out of pages
+        got = check_slots(osc, kv, q, 16, 9, n_free, 5, sum(q), 3, seed=n_free)
+        assert got[4][2].item() >= 1
+    check_slots(osc, kv, q, 16, 9, 10 ** 6, 5, sum(q))  # more free than the list holds
+    check_slots(osc, kv, q, 16, 9, -4, 5, sum(q))
+    check_slots(osc, [-5, 7], [3, -2], 16, 4, 4, 2, 3)  # negative lengths count as none
+    # sums past 32 bits: that request is refused, and the row offsets stop at the largest number
+    lens, offs, pos, slots, info = osc.osc_page_slots(i32([2 ** 31 - 1, 5]), i32([2 ** 31 - 1, 9]), i32([3, 2]), i32([2]), i32([[0, 0], [1, 0]]), 16, 50)
+    assert lens.tolist() == [2 ** 31 - 1, 14] and offs.tolist() == [0, 2 ** 31 - 1, 2 ** 31 - 1] and info.tolist() == [2, 0, 1, 2 ** 31 - 1]
+    assert (slots == -1).all()
+
+
+def test_slots_most_requests(osc):
+    gen = np.random.default_rng(5)
+    kv, q = gen.integers(0, 40, 8192), gen.integers(0, 9, 8192)
+    check_slots(osc, kv, q, 16, 8192, 8192, 4, int(q.sum()))
+
+
+def test_slots_step_by_step(osc):
+    """a serving loop: lengths, free count and table go from step to step on the device"""
+    B, ps, width, n_pool = 5, 16, 8, 30
+    lens = [i32([0, 3, 16, 0, 31]), torch.empty(B, dtype=torch.int32, device=DEV)]
+    table = i32(100 + np.arange(B * width).reshape(B, width))
+    free, n_free = i32(np.arange(n_pool)[::-1].copy()), i32([n_pool])
+    w_lens, w_table, w_free = lens[0].cpu().numpy(), table.cpu().numpy(), n_pool
+    gen = np.random.default_rng(3)
+    for step in range(12):
+        q = gen.integers(0, 14, B)
+        T = int(q.sum())
+        want = ref.page_slots(w_lens, q, ps, free.cpu().numpy(), w_free, w_table, T, 100)
+        kv, offs, pos, slots, info = osc.osc_page_slots(lens[step % 2], i32(q), free, n_free, table, ps, T, 100)
+        for g, w in zip((kv, offs, pos, slots, info, table), want):
+            assert np.array_equal(g.cpu().numpy(), w), step
+        lens[1 - step % 2], n_free = kv, info[:1].clone()
+        w_lens, w_table, w_free = want[0], want[5], want[4][0]
+
+
+# ---- norms, rotation, cache ------------------------------------------------------------------------------------------
+
+
+def test_rope_table(osc):
+    for base, rot, n in ((10000.0, 128, 300), (1e6, 64, 77), (5e5, 8, 70000)):
+        got, want = f64(osc.osc_rope_table(base, rot, n)), ref.rope_angles(base, rot, n)
+        assert np.abs(got - want).max() <= 2.0 ** -24 + n * 2.0 ** -50  # one rounding, and the angle's own in double
+
+
+def check_rope(osc, T, Hq, Hkv, D, rot, style, axes, norm, ps=16, pad=0, seed=0, cache=True, inplace=False, sections=None, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    width = (Hq + 2 * Hkv) * D
+    x = (torch.randn(T, width + pad, generator=g) * scale).bfloat16().to(DEV)[:, :width]
+    gq, gk = ((1 + 0.3 * torch.randn(D, generator=g)).bfloat16().to(DEV) for _ in range(2)) if norm else (None, None)
+    n_pos = 501
+    cs = osc.osc_rope_table(10000.0, rot, n_pos) if rot else torch.zeros((n_pos, 0), device=DEV)
+    pos = torch.randint(0, n_pos, (axes, T), generator=g, dtype=torch.int32)
+    half = rot // 2
+    if sections is None:
+        sections = [half] if axes == 1 else [half // 3, half - half // 3] if axes == 2 else [half // 4, half // 3, half - half // 4 - half // 3]
+    n_pages = T // ps + 3
+    slots = torch.randperm(n_pages * ps, generator=g)[:T].int()
+    out_of_range = torch.zeros(T, dtype=torch.bool)
+    skip = torch.zeros(T, dtype=torch.bool)
+    if T > 4:
+        pos[axes - 1, 1], pos[0, 3] = n_pos, -1
+        out_of_range[1] = out_of_range[3] = True
+        slots[2], slots[4] = -1, n_pages * ps
+        skip[2] = skip[4] = True
+    K, V = (torch.randn(n_pages, Hkv, ps, D, generator=g).bfloat16().to(DEV) for _ in range(2))
+    want_K, want_V = f64(K), f64(V)
+    x64, pos_n = f64(x).reshape(T, Hq + 2 * Hkv, D), pos.clamp(0, n_pos - 1).numpy()
+    cs64 = f64(cs)
+    args = (1e-6, cs64, pos_n, sections, rot, style == osc.OSC_ROPE_PAIRS)
+    wq, sq = ref.head_rope(x64[:, :Hq], None if gq is None else f64(gq), *args)
+    wk, sk = ref.head_rope(x64[:, Hq:Hq + Hkv], None if gk is None else f64(gk), *args)
+    wq[out_of_range.numpy()] = 0
+    size_K = np.zeros_like(want_K)
+    for t in range(T):
+        if not (out_of_range[t] or skip[t]):
+            s = int(slots[t])
+            want_K[s // ps, :, s % ps], want_V[s // ps, :, s % ps], size_K[s // ps, :, s % ps] = wk[t], x64[t, Hq + Hkv:], sk[t]
+    out = x[:, :Hq * D] if inplace else None
+    y = osc.osc_qk_norm_rope(x, Hq, Hkv, D, cs, pos.to(DEV) if axes > 1 else pos[0].to(DEV), slots.to(DEV) if cache else None, K if cache else None,
+                             V if cache else None, gq, gk, 1e-6, rot, style, sections, out)
+    err = np.abs(f64(y).reshape(T, Hq, D) - wq)
+    assert (err <= 2.0 ** -8 * np.abs(wq) + 2.0 ** -19 * sq).all()
+    if cache:
+        assert (np.abs(f64(K) - want_K) <= (size_K > 0) * 2.0 ** -8 * np.abs(want_K) + 2.0 ** -19 * size_K).all()
+        assert np.array_equal(f64(V), want_V)
+    return y
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,D", [(1, 32, 8, 128), (7, 5, 5, 64), (65, 4, 1, 128), (33, 8, 2, 64), (130, 3, 1, 64), (300, 32, 4, 128)])
+@pytest.mark.parametrize("style", [0, 1])
+def test_rope(osc, T, Hq, Hkv, D, style):
+    for axes, norm in ((1, True), (1, False), (3, True), (2, False)):
+        for rot in (D, D // 2, 24):
+            check_rope(osc, T, Hq, Hkv, D, rot, style, axes, norm, ps=16 << (T % 5), seed=T + axes + rot)
+
+
+def test_rope_forms(osc):
+    check_rope(osc, 9, 4, 2, 128, 128, 0, 1, True, pad=24)             # strided rows
+    check_rope(osc, 9, 4, 2, 128, 128, 0, 1, True, cache=False)        # queries alone
+    check_rope(osc, 9, 4, 2, 128, 128, 0, 1, True, inplace=True)       # over the projection's own queries
+    check_rope(osc, 9, 4, 2, 64, 0, 0, 1, True)                        # nothing turned
+    check_rope(osc, 9, 4, 2, 64, 64, 1, 3, True, sections=[0, 32, 0])  # empty axes
+    check_rope(osc, 9, 4, 2, 64, 64, 0, 2, True, sections=[5, 27])
+    check_rope(osc, 9, 4, 2, 128, 64, 0, 1, True, scale=2.0 ** 40)     # squares far above, and below, what 16 bits hold
+    check_rope(osc, 9, 4, 2, 128, 64, 1, 1, True, scale=2.0 ** -7)
+    check_rope(osc, 2000, 6, 2, 128, 128, 0, 1, True, ps=64)
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------
+
+
+def make(seed, B, P, kv, n, Hq, Hkv, D, ps, std=1.5, extra_cols=0):
+    """a cache that holds NaN wherever no token is"""
+    g = torch.Generator().manual_seed(seed)
+    pages = [-(-a // ps) for a in kv]
+    n_prefix = -(-P // ps)
+    n_pages = n_prefix + sum(pages) + 2
+    perm = torch.randperm(n_pages, generator=g)
+    K, V = (torch.full((n_pages, Hkv, ps, D), float("nan")) for _ in range(2))
+    table = torch.full((B, max(pages + [1]) + 1), 10 ** 9, dtype=torch.int32)
+    at = n_prefix
+
+    def fill(pg, L):
+        for j in range(L):
+            K[pg[j // ps], :, j % ps] = torch.randn(Hkv, D, generator=g)
+            V[pg[j // ps], :, j % ps] = torch.randn(Hkv, D, generator=g) + 0.3
+    fill(perm, P)
+    for b in range(B):
+        pg = perm[at:at + pages[b]]
+        at += pages[b]
+        table[b, :pages[b]] = pg.int()
+        fill(pg, kv[b])
+    T = sum(n)
+    Q = (torch.randn(T, Hq * D + extra_cols, generator=g) * std).bfloat16()
+    offs = np.concatenate([[0], np.cumsum(n)])
+    return dict(Q=Q.to(DEV)[:, :Hq * D], K=K.bfloat16().to(DEV), V=V.bfloat16().to(DEV), prefix=perm[:n_prefix].int().to(DEV), P=P, table=table.to(DEV),
+                kv=i32(kv), offs=i32(offs), Hq=Hq, Hkv=Hkv, D=D, scale=D ** -0.5)
+
+
+def call(osc, s, **kw):
+    return osc.osc_prefix_attention(s["Q"], s["Hq"], s["Hkv"], s["D"], s["K"], s["V"], s["prefix"], s["P"], s["table"], s["kv"], s["offs"], s["scale"],
+                                    want_lse=True, **kw)
+
+
+def check_attention(osc, s, got=None):
+    o, lse = call(osc, s) if got is None else got
+    T, D, scale = s["Q"].shape[0], s["D"], s["scale"]
+    wo, wl, av, big = ref.prefix_attention(f64(s["Q"]).reshape(T, s["Hq"], D), f64(s["K"]), f64(s["V"]), s["prefix"].cpu().numpy(), s["P"],
+                                           s["table"].cpu().numpy(), s["kv"].cpu().numpy(), s["offs"].cpu().numpy(), scale)
+    n = s["P"] + int(s["kv"].max())
+    score = scale * (D + 4) * 2.0 ** -24 * big  # of a score
+    err = np.abs(f64(o).reshape(T, s["Hq"], D) - wo)
+    assert (err <= 2.0 ** -8 * np.abs(wo) + (2.0 ** -8 + 2 * score[..., None] + 2.0 ** -18) * av).all(), (err / (av + 1e-30)).max()
+    empty = np.isinf(wl)
+    assert np.array_equal(np.isinf(f64(lse)), empty)
+    tol = score + 2.0 ** -21 * (np.abs(np.where(empty, 0, wl)) + scale * big) + (n + 8) * 2.0 ** -24
+    assert (np.abs(np.where(empty, 0, f64(lse)) - np.where(empty, 0, wl)) <= tol).all()
+    return o, lse
+
+
+HEADS = [(4, 1, 128), (32, 8, 128), (6, 2, 64), (3, 3, 64), (12, 1, 128), (40, 8, 64), (48, 1, 64)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", HEADS)
+@pytest.mark.parametrize("P", [0, 1, 16, 31, 33, 250])
+def test_attention_decode(osc, Hq, Hkv, D, P):
+    kv = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 130]
+    ps = 16 << ((Hq + P) % 5)
+    check_attention(osc, make(P + Hq, len(kv), P, kv, [1] * len(kv), Hq, Hkv, D, ps))
+
+
+@pytest.mark.parametrize("ps", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("P", [0, 40, 129])
+def test_attention_ragged(osc, ps, P):
+    """prompts, chunks of prompts, single tokens and idle requests in one step"""
+    n = [5, 1, 0, 33, 1, 70, 8, 0, 17, 130]
+    kv = [5, 90, 12, 40, 1, 170, 8, 0, 300, 133]
+    check_attention(osc, make(ps + P, len(n), P, kv, n, 8, 2, 128, ps))
+    check_attention(osc, make(ps + P + 1, len(n), P, kv, n, 3, 1, 64, ps, extra_cols=40))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_rows_that_see_nothing(osc, D):
+    s = make(1, 4, 0, [0, 3, 1, 5], [1, 5, 40, 5], 4, 2, D, 16)
+    o, lse = check_attention(osc, s)
+    assert torch.isneginf(lse).any() and (o[0] == 0).all()
+    check_attention(osc, make(2, 3, 7, [0, 0, 2], [1, 3, 4], 4, 2, D, 16))  # they see the prefix alone
+
+
+def test_attention_one_long_request(osc):
+    check_attention(osc, make(3, 1, 0, [2900], [1], 4, 1, 128, 64))
+    check_attention(osc, make(4, 1, 2100, [1], [1], 4, 1, 64, 32))
+    check_attention(osc, make(5, 2, 1000, [900, 3], [3, 2], 4, 2, 128, 16))
+
+
+def test_attention_sharp_and_flat(osc):
+    """scores up to several hundred, whose maximum rises from tile to tile; and all alike"""
+    s = make(6, 3, 70, [100, 37, 200], [1, 2, 1], 8, 2, 128, 32, std=40.0)
+    check_attention(osc, s)
+    s["scale"] = 1e-4
+    check_attention(osc, s)
+    s["K"] = torch.where(torch.isnan(s["K"]), s["K"], torch.sort(torch.nan_to_num(s["K"]).abs(), dim=2)[0].to(s["K"].dtype))
+    s["Q"] = s["Q"].abs()
+    s["scale"] = 0.1
+    check_attention(osc, s)
+
+
+def test_attention_bad_pages_stay_inside(osc):
+    """page numbers outside the cache: other rows are right, nothing outside is read"""
+    s = make(7, 4, 20, [50, 60, 17, 4], [1, 2, 1, 1], 4, 2, 64, 16)
+    good, _ = call(osc, s)
+    s["table"][1] = -7
+    s["K"], s["V"] = torch.nan_to_num(s["K"]), torch.nan_to_num(s["V"])
+    o, _ = call(osc, s)
+    rows = [0, 3, 4]
+    assert torch.equal(o[rows], good[rows])
+    s["kv"][2] = 2 ** 30  # longer than its row of the table can say: limited to it
+    o, _ = call(osc, s)
+    assert torch.equal(o[[0, 4]], good[[0, 4]])
+    s["offs"] = i32([0, 5, 1, 5, 2])  # offsets that fall: nothing outside Q is read or written
+    call(osc, s)
+    torch.cuda.synchronize()
+
+
+def test_attention_twice_and_in_pieces(osc):
+    """the same bits from call to call, and rows do not depend on a workspace's contents"""
+    s = make(8, 20, 300, list(range(3, 203, 10)), [1] * 18 + [40, 9], 8, 2, 128, 16)
+    n = osc.osc_prefix_attention_workspace_bytes(s["Q"].shape[0], 20, 8, 2, 128, 300)
+    first = check_attention(osc, s)
+    for fill in (0, 255):
+        ws = torch.full((n,), fill, dtype=torch.uint8, device=DEV)
+        again = call(osc, s, workspace=ws)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_step_in_a_graph_and_on_a_stream(osc):
+    """slots, norms with rotation and attention of one step, captured once and replayed on new lengths, each replay against the same
+    calls made eagerly; on a stream that is not the default one"""
+    B, Hq, Hkv, D, ps, width, P = 6, 8, 2, 128, 16, 8, 50
+    g = torch.Generator().manual_seed(1)
+    n_pages = 80
+    K, V = (torch.randn(n_pages, Hkv, ps, D, generator=g).bfloat16().to(DEV) for _ in range(2))
+    prefix = i32([70, 71, 72, 73])
+    free, cs = i32(np.arange(60)), osc.osc_rope_table(1e4, D, 400)
+    gq = torch.ones(D, dtype=torch.bfloat16, device=DEV)
+    T = 16
+    x = torch.randn(T, (Hq + 2 * Hkv) * D, generator=g).bfloat16().to(DEV)
+    kv, q, n_free = i32([0] * B), i32([0] * B), i32([60])
+    ws = torch.empty(osc.osc_prefix_attention_workspace_bytes(T, B, Hq, Hkv, D, P), dtype=torch.uint8, device=DEV)
+
+    def step(table, K, V):
+        lens, offs, pos, slots, info = osc.osc_page_slots(kv, q, free, n_free, table, ps, T, P)
+        y = osc.osc_qk_norm_rope(x, Hq, Hkv, D, cs, pos, slots, K, V, gq, gq)
+        o, lse = osc.osc_prefix_attention(y, Hq, Hkv, D, K, V, prefix, P, table, lens, offs, want_lse=True, workspace=ws)
+        return lens, offs, pos, slots, info, y, o, lse
+    stream = torch.cuda.Stream()
+    table = i32(np.zeros((B, width)))
+    with torch.cuda.stream(stream):
+        step(table, K, V)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            outs = step(table, K, V)
+        gen = np.random.default_rng(0)
+        for k in range(5):
+            kv.copy_(i32(gen.integers(0, 60, B)))
+            q.copy_(i32(gen.integers(0, 3, B)))
+            x.copy_(torch.randn(x.shape, generator=g).bfloat16())
+            table.copy_(i32(np.arange(B * width).reshape(B, width) % 20))
+            t2, K2, V2 = table.clone(), K.clone(), V.clone()
+            graph.replay()
+            stream.synchronize()
+            got = [o.clone() for o in outs]
+            eager = step(t2, K2, V2)
+            stream.synchronize()
+            m = int(eager[1][-1])
+            for i, (a, b) in enumerate(zip(got, eager)):
+                a, b = (a[:m], b[:m]) if i >= 6 else (a, b)
+                assert torch.equal(a, b), (k, i)
+            assert torch.equal(table, t2) and torch.equal(K, K2) and torch.equal(V, V2)
