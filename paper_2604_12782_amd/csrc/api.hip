@@ -761,7 +761,7 @@ int osc_qk_norm_rope(const void* QKV, int64_t T, int32_t Hq, int32_t Hkv, int32_
 }
 
 size_t osc_prefix_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
-    if (T < 0 || B < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || prefix_len < 0) return 0;
+    if (T < 0 || B < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || prefix_len < 0 || Hq / Hkv > 128) return 0;
     return prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len);
 }
 
@@ -780,6 +780,7 @@ int osc_prefix_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int3
     REQUIRE(B <= PAGED_MAX_REQUESTS, OSC_ERR_UNSUPPORTED, "%s: %d requests (at most %d)", who, B, PAGED_MAX_REQUESTS);
     REQUIRE(prefix_len <= 0x3fffffff && ldt <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "%s: prefix_len=%lld ldt=%lld", who, (long long)prefix_len, (long long)ldt);
     REQUIRE(ldq >= (int64_t)Hq * D && ldo >= (int64_t)Hq * D, OSC_ERR_SHAPE, "%s: ldq=%lld ldo=%lld", who, (long long)ldq, (long long)ldo);
+    REQUIRE(Hq / Hkv <= 128, OSC_ERR_UNSUPPORTED, "%s: %d query heads a key/value head (at most 128)", who, Hq / Hkv);
     REQUIRE(scale > 0.0f && scale <= 1e6f, OSC_ERR_SHAPE, "%s: scale %g (a positive number)", who, (double)scale);
     if (T == 0 || B == 0) return OSC_OK;
     REQUIRE(Q && O && kv_lens && q_offsets && workspace && (block_table || ldt == 0) && (prefix_pages || prefix_len == 0), OSC_ERR_NULL,

@@ -1,4 +1,19 @@
 // Attention of a step's rows over a shared prefix and each request's own cached tokens.
+//
+// Rows.  Query heads that share a key/value head are rows of one problem: row r = i * G + g is token i of its request, head g of
+// the G = Hq / Hkv.  Requests are served in two ways:
+//   long   their own tiles of 128 rows walk the prefix and then their own tokens (`joint`)
+//   short  tiles of 32 rows walk the own tokens only; the short requests' rows, one behind the other, form tiles of 128 that
+//          walk the prefix, which is therefore read once for all of them (`packed`; 32 rows or fewer: one tile of 32)
+// With a prefix, long means 256 rows or more (a last tile that is not full costs at most a third); without one, more than 32.
+//
+// Work.  Tiles of 128 rows and tiles of 32 rows are two lists.  An item is a tile with the tokens that it walks; the items of
+// a list lie behind each other on a line whose length is tokens, and every workgroup takes an equal piece of both lines. So
+// all workgroups end together whatever the lengths are, no length is read back to the host, and an item is cut at most where a
+// piece ends.  What a workgroup computes of an item is a segment: unnormalised sums, their weight and their base.  A long request's tile
+// in one segment is written as it is; all others go to the workspace and a second kernel joins them, in the order of the
+// line: the same bits in every run.  The two lists are bound by different things (matrix cores and LDS; HBM), so
+// half of the workgroups take them in the other order.
 #include <algorithm>
 
 #include "osc_internal.h"
@@ -10,12 +25,19 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
+
+constexpr int WG = 256, WROWS = 128, GROUPS = 256;
+// Workgroups: two on a CU (LDS for their tiles), three where heads are small.
+template <int D>
+constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
+// The smallest pieces of the two lines: four tiles of 32 tokens (one a wavefront), and tokens of a wide tile
+constexpr int MIN_NARROW = 4, MIN_WIDE = 512;
+constexpr int SUPER = 4096, MAX_SUPER = 16;
 
 struct AttnArgs {
     const uint16_t* Q;
     int64_t T, ldq;
-    int Hq, Hkv, G;
+    int Hq, Hkv, G, tpt;  // tpt: tokens of a 128-row tile
     const uint8_t *K, *V;
     uint32_t n_pages;
     int lg;
@@ -25,214 +47,469 @@ struct AttnArgs {
     int64_t ldt;
     int max_kv;  // tokens that a row of the table can name
     const int32_t *kv_lens, *q_offsets;
-    int B;
-    float c;  // scale * log2(e): scores leave the matrix core unscaled, and powers are of two
+    int B, per;  // per: requests of a group
+    float c;     // scale * log2(e): scores leave the matrix core unscaled, and powers are of two
     uint16_t* O;
     int64_t ldo;
     float* lse;
+    // workspace: the plan, one record a request, segments in blocks of 32 rows: of long requests (two places a workgroup), of packed
+    // tiles, of short requests
+    struct Plan* plan;
+    int64_t* records;
+    uint8_t* blocks;
+    int64_t joint_blocks, packed_blocks, narrow_blocks;
 };
+template <int D>
+constexpr int block_bytes() { return 32 * (D + 2) * 4; }  // [32][D] sums, [32] base and weight
 
-// ---- a tile of 32 cached tokens in LDS ------------------------------------------------------------------------------
+__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uni(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)uni((int)(v >> 32)) << 32 | (uint32_t)uni((int)v));
+}
+
+// ---- where things are on the two lines -----------------------------------------------------------------------------------
+struct Request {
+    int q0, n, L;
+};
+struct Extent {  // of one request, or of all before one
+    int64_t narrow, items, rows, wide;
+};
+__device__ __forceinline__ Request request(const AttnArgs& p, int b) {
+    Request r;
+    const int T = (int)p.T;
+    r.q0 = min(max(p.q_offsets[b], 0), T);
+    r.n = max(min(p.q_offsets[b + 1], T) - r.q0, 0);
+    r.L = min(max(p.kv_lens[b], 0), p.max_kv);
+    return r;
+}
+__device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? 256 : 33); }
+__device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (n * p.G + 31) >> 5; }
+__device__ __forceinline__ int narrow_length(int L) { return max(1, (L + 31) >> 5); }
+// tokens that the first k tiles of a long request walk: each sees `seen` and tpt more than the one before it
+__device__ __forceinline__ int64_t wide_sum(const AttnArgs& p, int64_t seen, int64_t k) { return k * seen + p.tpt * (k * (k + 1) / 2); }
+__device__ __forceinline__ int64_t wide_seen(const AttnArgs& p, const Request& r) { return p.P + max(r.L - r.n, 0); }
+__device__ __forceinline__ int wide_tiles(const AttnArgs& p, int n) { return (n + p.tpt - 1) / p.tpt; }
+__device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r) {
+    Extent e{0, 0, 0, 0};
+    if (r.n == 0) return e;
+    if (is_long(p, r.n)) {
+        e.wide = p.Hkv * wide_sum(p, wide_seen(p, r), wide_tiles(p, r.n));
+    } else {
+        e.items = (int64_t)narrow_tiles(p, r.n) * p.Hkv;
+        e.narrow = e.items * narrow_length(r.L);
+        if (p.P) e.rows = r.n * p.G;
+    }
+    return e;
+}
+
+// What follows from the totals: the packed tiles at the start of their line, and the pieces' lengths.
+struct Plan {
+    int64_t narrow, wide;        // lengths of the lines
+    int64_t narrow0, items0;     // of which the prefix's narrow items are the first
+    int64_t wide0;               // of which the packed tiles are the first
+    int64_t narrow_per, wide_per;
+    int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; blocks of 64 tokens: of a piece of the prefix, of the prefix
+};
+// The prefix's blocks are cut into pieces that stay in an XCD's L2 while all packed tiles walk them.
+__device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
+    const int64_t n = (P + SUPER - 1) / SUPER;
+    return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
+}
+template <int D>
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int64_t narrow, int64_t rows, int64_t wide) {
+    Plan a;
+    a.rows = (int)min(rows, p.T * p.G);
+    a.nbp = (p.P + 63) >> 6;
+    a.narrow0 = a.items0 = a.wide0 = 0;
+    a.tiles = a.supers = a.super = 0;
+    if (a.rows > 32) {
+        a.tiles = (a.rows + WROWS - 1) / WROWS;
+        a.supers = super_count(p.P, a.tiles);
+        a.super = (a.nbp + a.supers - 1) / a.supers;
+        a.supers = (a.nbp + a.super - 1) / a.super;
+        a.wide0 = (int64_t)p.Hkv * a.tiles * a.nbp * 64;
+    } else if (a.rows > 0) {
+        a.items0 = p.Hkv;
+        a.narrow0 = (int64_t)p.Hkv * ((p.P + 31) >> 5);
+    }
+    a.narrow = a.narrow0 + narrow;
+    a.wide = a.wide0 + wide;
+    constexpr int N = attn_wgs<D>();
+    a.narrow_per = max((a.narrow + N - 1) / N, (int64_t)MIN_NARROW);
+    a.wide_per = max((a.wide + N - 1) / N, (int64_t)MIN_WIDE);
+    return a;
+}
+
+// what all lanes read from LDS, as the scalars that it is
+__device__ __forceinline__ Plan uni(const Plan& a) {
+    return Plan{uni(a.narrow), uni(a.wide), uni(a.narrow0), uni(a.items0), uni(a.wide0), uni(a.narrow_per), uni(a.wide_per),
+                uni(a.rows), uni(a.tiles), uni(a.supers), uni(a.super), uni(a.nbp)};
+}
+
+// Running sums over groups of `per` requests, in LDS: what a place on a line or a packed row is searched in.
+struct Sums {
+    int64_t narrow[GROUPS], items[GROUPS], rows[GROUPS], wide[GROUPS];
+};
+// the last group whose sum does not exceed x (x below the total)
+__device__ __forceinline__ int find_group(const int64_t (&sums)[GROUPS], int64_t x, int lane) {
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < GROUPS / 64; ++k) n += __popcll(__ballot(sums[k * 64 + lane] <= x));
+    return n - 1;
+}
+// The request that holds place x of a line: its number and what is before it.  All lanes of a wavefront take part.
+template <bool WIDE>
+__device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, int64_t x, int lane, Extent& before) {
+    const int g = uni(find_group(WIDE ? s.wide : s.narrow, x, lane));
+    before = Extent{uni(s.narrow[g]), uni(s.items[g]), uni(s.rows[g]), uni(s.wide[g])};
+    int b = g * p.per;
+    if (p.per > 1) {  // at most 32 requests of a group: one a lane
+        Extent e{0, 0, 0, 0};
+        if (lane < p.per && b + lane < p.B) e = extent(p, request(p, b + lane));
+        Extent sum = e;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t n = __shfl_up(sum.narrow, d), i = __shfl_up(sum.items, d), r = __shfl_up(sum.rows, d), w = __shfl_up(sum.wide, d);
+            if (lane >= d) sum.narrow += n, sum.items += i, sum.rows += r, sum.wide += w;
+        }
+        const int64_t end = WIDE ? before.wide + sum.wide : before.narrow + sum.narrow;
+        const int k = uni(__ffsll((unsigned long long)__ballot(end > x)) - 1);  // lanes past the group repeat its end, which is above x
+        before.narrow += uni(__shfl(sum.narrow - e.narrow, k));
+        before.items += uni(__shfl(sum.items - e.items, k));
+        before.rows += uni(__shfl(sum.rows - e.rows, k));
+        before.wide += uni(__shfl(sum.wide - e.wide, k));
+        b += k;
+    }
+    return uni(b);
+}
+// The token and head of packed row r (below the total), each lane its own.
+__device__ __forceinline__ void packed_row(const AttnArgs& p, const Sums& s, int r, int& t, int& g) {
+    int lo = 0, hi = GROUPS;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s.rows[mid] <= r) lo = mid;
+        else hi = mid;
+    }
+    int64_t at = s.rows[lo];
+    int b = lo * p.per;
+    Request q = request(p, b);
+    for (int last = min(p.B, b + p.per) - 1; b < last; q = request(p, ++b)) {
+        const int64_t n = extent(p, q).rows;
+        if (at + n > r) break;
+        at += n;
+    }
+    const int i = min((int)(r - at) / p.G, max(q.n - 1, 0));
+    t = min(q.q0 + i, (int)p.T - 1);
+    g = min((int)(r - at) - i * p.G, p.G - 1);
+}
+
+// ---- tiles of cached tokens in LDS ---------------------------------------------------------------------------------------------
 // Rows of D bf16 in pieces of 16 bytes; piece c of row r sits at c ^ spread(r), so that both readers find all banks: keys by
 // 32 rows of one piece, values by 8 rows of four neighbouring pieces.
 template <int D>
 __device__ __forceinline__ int spread(int r) {
     return D == 128 ? (r & 3) << 2 | ((r >> 2) & 3) : ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
 }
-
-struct Span {  // 32 tokens of one key/value head: its pages hold 16-token runs in one piece
-    const uint8_t *half0, *half1;  // bytes from the cache's start are the same for keys and values: held for keys
-    int last;                      // the last token there is, 0..31
-};
-
+// Start of the 16-token run that token j lies in (a page holds whole runs), for keys; values lie V - K further.
 template <int D>
-__device__ __forceinline__ Span locate(const AttnArgs& p, const int32_t* pages, int h, int j0, int end) {
-    auto at = [&](int j) {
-        uint32_t page = (uint32_t)pages[j >> p.lg];
-        if (page >= p.n_pages) page = 0;  // nothing outside the cache is read, whatever a table holds
-        return p.K + ((((int64_t)page * p.Hkv + h) << p.lg) + ((j & ((1 << p.lg) - 1)) & ~15)) * (D * 2);
-    };
-    Span s;
-    s.last = min(31, end - 1 - j0);
-    s.half0 = at(j0);
-    s.half1 = at(min(j0 + 16, end - 1));
-    return s;
+__device__ __forceinline__ const uint8_t* run_of(const AttnArgs& p, uint32_t page, int h, int j) {
+    if (page >= p.n_pages) page = 0;  // nothing outside the cache is read, whatever a table holds
+    return p.K + ((((int64_t)page * p.Hkv + h) << p.lg) + ((j & ((1 << p.lg) - 1)) & ~15)) * (D * 2);
 }
-
-// Asks for the tile: rows past the last token repeat it, so that whatever a page holds there is never multiplied.
+// Asks for 16 rows, tile rows 16 * half .., of which `last` + 1 exist from the run's start: rows past the last token repeat it, so that whatever a
+// page holds there is never multiplied.
 template <int D>
-__device__ __forceinline__ void fetch(const Span& s, int64_t shift, uint8_t* dst, int lane) {
-    constexpr int CH = D / 8, RPI = 64 / CH, NI = 32 / RPI;
+__device__ __forceinline__ void fetch16(const uint8_t* run, int half, int last, uint8_t* dst, int lane) {
+    constexpr int CH = D / 8, RPI = 64 / CH, NI = 16 / RPI;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-        const int r = i * RPI + lane / CH, piece = (lane % CH) ^ spread<D>(r), src = min(r, s.last);
-        const uint8_t* base = (src < 16 ? s.half0 : s.half1) + shift;
-        load_to_lds16(base + (src & 15) * (D * 2) + piece * 16, dst + i * 1024);
+        const int r = i * RPI + lane / CH, piece = (lane % CH) ^ spread<D>(r);  // spread() repeats after 16 rows
+        load_to_lds16(run + min(r, last) * (D * 2) + piece * 16, dst + half * (16 * D * 2) + i * 1024);
     }
 }
 
 // Softmax state of 32 rows, transposed: lane l holds row l % 32; its upper and lower half hold different tokens of a tile and
-// different channels of the sums.  `sum` is the lane's own share.
+// different channels of the sums.  `sum` is the lane's own share.  Weights are 2^(score * c - base); the base follows the
+// maximum only when that is 2^8 above it, so sums are rarely scaled.
 template <int D>
 struct State {
     v16f o[D / 32];
-    float top, sum;
+    float base, sum;
 };
-
-__device__ __forceinline__ float other_half_max(float v) {
+template <int D>
+__device__ __forceinline__ void clear(State<D>& st) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) st.o[d] = v16f{};
+    st.base = -INFINITY, st.sum = 0.0f;
+}
+__device__ __forceinline__ float half_max(float v) {
     const int x = __builtin_bit_cast(int, v);
     const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
     return fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1]));
 }
-__device__ __forceinline__ float other_half_sum(float v) {
+__device__ __forceinline__ float half_sum(float v) {
     const int x = __builtin_bit_cast(int, v);
     const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
     return __builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]);
 }
 
-// One tile: S^T = K Q^T leaves a lane 16 tokens of its row, the weights go to bf16 and are the second operand of O^T += V^T P^T as
-// they lie, because the order of the tokens inside a product is free as long as both operands have the same.
-// `seen`: tokens below it count for the lane's row.
-template <int D, bool MASK>
-__device__ __forceinline__ void attend(State<D>& st, const v8bf (&q)[D / 16], const uint8_t* kt, const uint8_t* vt, int lane, float c, int seen) {
-    const int r = lane & 31, hi = lane >> 5;
-    v16f s = {};
+// N tiles of 32 tokens: S^T = K Q^T leaves a lane 16 tokens of its row a tile, the weights go to bf16 and are the second operand of
+// O^T += V^T P^T as they lie, because the order of the tokens inside a product is free as long as both operands have the same.
+// LDS addresses are numbers, the lane's part made once: a tile starts at a multiple of 256 bytes, so a piece's place is an exclusive or.
+// Fragments are read in batches that wait for themselves while the products of the batch before run.  (The compiler
+// would put a wait for every request on its way from HBM before the reads, which are of another buffer.)
+template <int D>
+__device__ __forceinline__ uint32_t key_lane(int lane) {
+    const int r = lane & 31;
+    return r * (D * 2) + (((lane >> 5) ^ spread<D>(r)) << 4);
+}
+template <int D>
+__device__ __forceinline__ uint32_t value_lane(int lane) {
+    const int i = lane & 15, row = 4 * (lane >> 5) + (i >> 2);
+    return row * (D * 2) + (((((lane >> 4) & 1) * 2 + ((i & 3) >> 1)) ^ spread<D>(row)) << 4) + (i & 1) * 8;
+}
+template <int X, int Y>
+__device__ __forceinline__ void read_keys(v8bf (&f)[4], uint32_t a, uint32_t b) {  // X, Y: offsets of two rows' pieces
+    asm volatile(
+        "ds_read_b128 %0, %4 offset:%6\n\tds_read_b128 %1, %4 offset:%7\n\tds_read_b128 %2, %5 offset:%6\n\tds_read_b128 %3, %5 offset:%7\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+        : "v"(a), "v"(b), "i"(X), "i"(Y)
+        : "memory");
+}
+__device__ __forceinline__ void read_keys(v8bf (&f)[4], uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+        : "v"(a), "v"(b), "v"(c), "v"(d)
+        : "memory");
+}
+template <int X, int Y>
+__device__ __forceinline__ void read_values(v4s (&f)[4], uint32_t a, uint32_t b, uint32_t c, uint32_t d) {  // two channels' pieces, two runs of tokens each
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%9\n\tds_read_b64_tr_b16 %2, %6 offset:%8\n\t"
+        "ds_read_b64_tr_b16 %3, %7 offset:%9\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+        : "v"(a), "v"(b), "v"(c), "v"(d), "i"(X), "i"(Y)
+        : "memory");
+}
+template <int X, int Y>
+__device__ __forceinline__ void read_values(v4s (&f)[8], const uint32_t (&a)[8]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%17\n\tds_read_b64_tr_b16 %2, %10 offset:%16\n\t"
+        "ds_read_b64_tr_b16 %3, %11 offset:%17\n\tds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%17\n\t"
+        "ds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%17\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7])
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]), "i"(X), "i"(Y)
+        : "memory");
+}
+__device__ __forceinline__ v16f mfma(v8bf a, v8bf b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+template <int D, int N>
+__device__ __forceinline__ void scores(v16f (&s)[N], const v8bf (&q)[D / 16], uint32_t kt) {
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-        const v8bf kf = *reinterpret_cast<const v8bf*>(kt + r * (D * 2) + (((2 * k + hi) ^ spread<D>(r)) << 4));
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[k], s, 0, 0, 0);
-    }
-    if (MASK) {
+    for (int u = 0; u < N; ++u) s[u] = v16f{};
+    v8bf f[4];
+    if constexpr (N == 2) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-            if ((e & 3) + 8 * (e >> 2) + 4 * hi >= seen) s[e] = -INFINITY;
-    }
-    float top = s[0];
+        for (int k = 0; k < D / 16; k += 2) {
+            read_keys<0, 32 * D * 2>(f, kt ^ (k << 5), kt ^ ((k + 1) << 5));
+            s[0] = mfma(f[0], q[k], s[0]);
+            s[1] = mfma(f[1], q[k], s[1]);
+            s[0] = mfma(f[2], q[k + 1], s[0]);
+            s[1] = mfma(f[3], q[k + 1], s[1]);
+        }
+    } else {
 #pragma unroll
-    for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
-    top = fmaxf(other_half_max(top), st.top);
-    const float base = top == -INFINITY ? 0.0f : top * c;  // a row that has seen nothing yet keeps sums of zero
-    const float fade = __builtin_amdgcn_exp2f(st.top * c - base);
-    st.top = top;
-    float sum = 0.0f;
+        for (int k = 0; k < D / 16; k += 4) {
+            read_keys(f, kt ^ (k << 5), kt ^ ((k + 1) << 5), kt ^ ((k + 2) << 5), kt ^ ((k + 3) << 5));
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -base));
-        sum += s[e];
-    }
-    st.sum = st.sum * fade + sum;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) st.o[d][e] *= fade;
-    const int i = lane & 15;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        v8bf w;  // rounded to 8 bits for the matrix core: half an ulp each, and of either sign; their sum is taken before
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = (__bf16)s[8 * k + e];
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-            union {
-                v4s part[2];
-                v8bf all;
-            } vf;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int row = 16 * k + 8 * x + 4 * hi + (i >> 2), piece = 4 * d + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
-                vf.part[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) v4s*)(lds_ptr)(vt + row * (D * 2) + ((piece ^ spread<D>(row)) << 4) + (i & 1) * 8));
-            }
-            st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.all, w, st.o[d], 0, 0, 0);
+            for (int j = 0; j < 4; ++j) s[0] = mfma(f[j], q[k + j], s[0]);
         }
     }
 }
-
-template <int D>
-__global__ __launch_bounds__(256) void prefix_attention_kernel(const AttnArgs p) {
-    constexpr int TILE = 32 * D * 2;
-    extern __shared__ uint8_t lds[];
-    int32_t* first = reinterpret_cast<int32_t*>(lds + 8 * TILE + 1024);  // row tiles before request b
-    __shared__ int64_t wsum[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int T = (int)p.T;
-    auto rows_of = [&](int b, int& q0, int& n) {
-        q0 = min(max(p.q_offsets[b], 0), T);
-        n = max(min(p.q_offsets[b + 1], T) - q0, 0);
-    };
-    {
-        const int per = (p.B + 255) / 256, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
-        int64_t mine = 0;  // offsets that do not rise can name more rows than there are: 64 bits, and the stored sums stay in range
-        for (int b = b0; b < b1; ++b) {
-            int q0, n;
-            rows_of(b, q0, n);
-            mine += (n * p.G + 31) >> 5;
-        }
-        int64_t s = mine;
+// `seen`: tokens below it count for the lane's row
+template <int D, int N, bool MASK>
+__device__ __forceinline__ void weigh(State<D>& st, v16f (&s)[N], int lane, float c, int seen) {
+    if (MASK) {
+        const int hi = lane >> 5;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t u = __shfl_up(s, d);
-            if (lane >= d) s += u;
-        }
-        if (lane == 63) wsum[wave] = s;
-        __syncthreads();
-        s -= mine;
-        for (int w = 0; w < wave; ++w) s += wsum[w];
-        for (int b = b0; b < b1; ++b) {
-            int q0, n;
-            rows_of(b, q0, n);
-            first[b] = (int)min(s, (int64_t)0x7fffffff);
-            s += (n * p.G + 31) >> 5;
-        }
-        if (tid == 255) first[p.B] = (int)min(s, (int64_t)0x7fffffff);
-        __syncthreads();
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (32 * u + (e & 3) + 8 * (e >> 2) + 4 * hi >= seen) s[u][e] = -INFINITY;
     }
-    const int64_t units = (int64_t)first[p.B] * p.Hkv;
-    uint8_t* mine = lds + wave * 2 * TILE;
-    const int64_t to_v = p.V - p.K;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int tile = (int)(u / p.Hkv), h = (int)(u - (int64_t)tile * p.Hkv);
-        int b = 0, hi = p.B;
-        while (hi - b > 1) {
-            const int mid = (b + hi) >> 1;
-            if (first[mid] <= tile) b = mid;
-            else hi = mid;
+    float top = s[0][0];
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+    top = half_max(top) * c;
+    if (__ballot(top > st.base + 8.0f)) {
+        const float base = fmaxf(st.base, top);
+        const float fade = base == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.base - base);
+        st.base = base;
+        st.sum *= fade;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) st.o[d][e] *= fade;
+    }
+    const float base = st.base == -INFINITY ? 0.0f : st.base;  // a row that has seen nothing yet keeps sums of zero
+    float sum = 0.0f;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][e], c, -base));
+            sum += s[u][e];
         }
-        b = __builtin_amdgcn_readfirstlane(b);
-        int q0, n;
-        rows_of(b, q0, n);
-        const int L = min(max(p.kv_lens[b], 0), p.max_kv);
-        const int r0 = (tile - first[b]) * 32, r = r0 + (lane & 31), rows = n * p.G;
-        const int rc = min(r, rows - 1), ti = rc / p.G, g = rc - ti * p.G;
+    st.sum += sum;
+}
+// tokens 16 T .. of the tile, times the weights of half a score tile
+template <int D, int T>
+__device__ __forceinline__ void gather16(State<D>& st, const v16f& s, const uint32_t (&at)[D / 16]) {
+    v8bf w;  // rounded to 8 bits for the matrix core: half an ulp each, and of either sign; their sum is taken before
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = (__bf16)s[8 * (T & 1) + e];
+    constexpr int X = 16 * T * D * 2, Y = X + 8 * D * 2;
+    union {
+        v4s part[D / 16];
+        v8bf all[D / 32];
+    } f;
+    if constexpr (D == 128) read_values<X, Y>(f.part, at);
+    else read_values<X, Y>(f.part, at[0], at[1], at[2], at[3]);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) st.o[d] = mfma(f.all[d], w, st.o[d]);
+}
+template <int D, int N>
+__device__ __forceinline__ void gather(State<D>& st, const v16f (&s)[N], uint32_t vt) {
+    uint32_t at[D / 16];  // a run of eight tokens on, the spread differs in one bit
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) at[2 * d] = vt ^ (d << 6), at[2 * d + 1] = vt ^ (d << 6) ^ 32;
+    gather16<D, 0>(st, s[0], at);
+    gather16<D, 1>(st, s[0], at);
+    if constexpr (N == 2) {
+        gather16<D, 2>(st, s[1], at);
+        gather16<D, 3>(st, s[1], at);
+    }
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2bf));  // nearest even
+}
+__device__ __forceinline__ float lse_of(float base, float sum) {
+    return sum > 0.0f ? (base + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+}
+__device__ __forceinline__ uint32_t lds_at(const uint8_t* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p; }
+__device__ __forceinline__ void lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// ---- a piece of the line of 32-row tiles ----------------------------------------------------------------------------------------
+// The four wavefronts hold the same rows and take every fourth tile of 32 tokens, each in LDS of its own: keys of the next tile are
+// asked for once this tile's scores are there, values once they are summed, so half a tile or more is on its way at any time and
+// no wavefront waits for another before the segment's end.
+template <int D>
+__device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_lds, const Sums& sums, uint8_t* lds, float* stats, int64_t w) {
+    const Plan plan = uni(in_lds);
+    constexpr int TILE = 32 * D * 2, NI = D / 16;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // what follows from it is made here, not kept in registers from the kernel's start
+    const int lane = tid & 63, wave = uni(tid >> 6);
+    const int64_t to_v = p.V - p.K;
+    uint8_t *kt = lds + wave * 2 * TILE, *vt = kt + TILE;
+    const uint32_t kl = lds_at(kt) + key_lane<D>(lane), vl = lds_at(vt) + value_lane<D>(lane);
+    int64_t x = w * plan.narrow_per;
+    const int64_t end = min(x + plan.narrow_per, plan.narrow);
+    while (x < end) {
+        // the item at x: its start and length on the line, its rows, its tokens
+        int64_t start, item;
+        int length, h, r0, rows, tokens, seen = 0, clear_to, b = -1;
+        Request rq{0, 0, 0};
+        const int32_t* pages;
+        if (x < plan.narrow0) {
+            length = (p.P + 31) >> 5;
+            h = (int)(x / length);
+            start = (int64_t)h * length, item = h;
+            r0 = 0, rows = plan.rows, tokens = p.P, clear_to = p.P, pages = p.prefix_pages;
+        } else {
+            Extent before;
+            b = find_request<false>(p, sums, x - plan.narrow0, lane, before);
+            rq = request(p, b);
+            length = narrow_length(rq.L);
+            const int nt = narrow_tiles(p, rq.n), k = (int)((x - plan.narrow0 - before.narrow) / length);
+            start = plan.narrow0 + before.narrow + (int64_t)k * length, item = plan.items0 + before.items + k;
+            h = k / nt;
+            r0 = (k - h * nt) * 32, rows = rq.n * p.G;
+            tokens = max(0, rq.L - rq.n + min(r0 + 31, rows - 1) / p.G + 1), clear_to = rq.L - rq.n + r0 / p.G + 1;
+            pages = p.table + (int64_t)b * p.ldt;
+        }
+        const int64_t stop = min(end, start + length);
+        const int t0 = (int)(x - start), t1 = min((int)(stop - start), (tokens + 31) >> 5);
+        x = stop;
+
+        const int rc = min(r0 + (lane & 31), rows - 1);
+        int ti = rc / p.G, g = rc - ti * p.G;
+        if (b < 0) {
+            packed_row(p, sums, rc, ti, g);
+            seen = p.P;
+        } else {
+            seen = rq.L - rq.n + ti + 1;
+            ti += rq.q0;
+        }
         v8bf q[D / 16];
-        const uint16_t* qp = p.Q + (int64_t)(q0 + ti) * p.ldq + (h * p.G + g) * D + (lane >> 5) * 8;
+        const uint16_t* qp = p.Q + (int64_t)ti * p.ldq + (h * p.G + g) * D + (lane >> 5) * 8;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) q[k] = *reinterpret_cast<const v8bf*>(qp + k * 16);
-        const int seen = L - n + ti + 1;  // own tokens that the lane's row may see
-        const int own = max(0, L - n + min(r0 + 31, rows - 1) / p.G + 1);
-        const int clear = L - n + r0 / p.G + 1;  // ... that all rows may see
-        const int np = (p.P + 31) >> 5, nt = np + ((own + 31) >> 5);
 
         State<D> st;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) st.o[d] = v16f{};
-        st.top = -INFINITY, st.sum = 0.0f;
-        for (int k = wave; k < nt; k += 4) {
-            const bool pre = k < np;
-            const int j0 = (pre ? k : k - np) * 32, end = pre ? p.P : own;
-            const Span sp = locate<D>(p, pre ? p.prefix_pages : p.table + (int64_t)b * p.ldt, h, j0, end);
-            fetch<D>(sp, 0, mine, lane);
-            fetch<D>(sp, to_v, mine + TILE, lane);
-            wait_vmcnt<0>();
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (j0 + 32 > (pre ? p.P : clear)) attend<D, true>(st, q, mine, mine + TILE, lane, p.c, (pre ? p.P : seen) - j0);
-            else attend<D, false>(st, q, mine, mine + TILE, lane, p.c, 0);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        clear(st);
+        auto runs = [&](int tile, const uint8_t*& a, const uint8_t*& c) {
+            const int j = tile * 32, j2 = min(j + 16, tokens - 1);
+            a = run_of<D>(p, (uint32_t)pages[j >> p.lg], h, j);
+            c = run_of<D>(p, (uint32_t)pages[j2 >> p.lg], h, j2);
+        };
+        auto fetch = [&](int tile, const uint8_t* a, const uint8_t* c, int64_t shift, uint8_t* dst) {
+            const int left = tokens - 1 - tile * 32;
+            fetch16<D>(a + shift, 0, min(left, 15), dst, lane);
+            fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : ((tokens - 1) & 15), dst, lane);
+        };
+        int tile = t0 + wave;
+        const uint8_t *ra = nullptr, *rb = nullptr, *na = nullptr, *nb = nullptr;
+        if (tile < t1) {
+            runs(tile, ra, rb);
+            fetch(tile, ra, rb, 0, kt);
+            lds_order();  // the waits below count: keys first
+            fetch(tile, ra, rb, to_v, vt);
         }
-        // the four wavefronts' parts: each leaves its sums in its own LDS, [row][channel], pieces of 16 bytes spread by row
-        st.sum = other_half_sum(st.sum);
+        for (; tile < t1; tile += 4) {
+            const bool more = tile + 4 < t1;
+            if (more) runs(tile + 4, na, nb);
+            wait_vmcnt<NI>();  // the keys are there; the values may not be
+            lds_order();
+            v16f s[1];
+            scores<D, 1>(s, q, kl);
+            lds_order();
+            __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the keys are read
+            if (more) fetch(tile + 4, na, nb, 0, kt);
+            const int j0 = tile * 32;
+            if (j0 + 32 > clear_to) weigh<D, 1, true>(st, s, lane, p.c, seen - j0);
+            else weigh<D, 1, false>(st, s, lane, p.c, 0);
+            if (more) wait_vmcnt<NI>();
+            else wait_vmcnt<0>();
+            lds_order();
+            gather<D, 1>(st, s, vl);
+            lds_order();
+            __builtin_amdgcn_s_waitcnt(0xC07F);
+            if (more) fetch(tile + 4, na, nb, to_v, vt);
+        }
+        // The four wavefronts' parts: each leaves its sums in its own LDS, [row][channel], pieces of 16 bytes spread by row
+        st.sum = half_sum(st.sum);
         float* parts = reinterpret_cast<float*>(lds);
-        float* stats = reinterpret_cast<float*>(lds + 8 * TILE);  // [wave][row] top, then sum
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -241,66 +518,442 @@ __global__ __launch_bounds__(256) void prefix_attention_kernel(const AttnArgs p)
                 *reinterpret_cast<float4*>(parts + wave * 32 * D + row * D + ((piece ^ (row & 7)) << 2)) =
                     make_float4(st.o[d][4 * e], st.o[d][4 * e + 1], st.o[d][4 * e + 2], st.o[d][4 * e + 3]);
             }
-        if (lane < 32) stats[wave * 32 + lane] = st.top, stats[128 + wave * 32 + lane] = st.sum;
+        if (lane < 32) stats[wave * 32 + lane] = st.base, stats[128 + wave * 32 + lane] = st.sum;
         __syncthreads();
         const int row = tid >> 3, part = tid & 7;
-        if (r0 + row < rows) {
-            float top = -INFINITY, w[4], sum = 0.0f;
+        const bool direct = p.P == 0 && t0 == 0 && stop == start + length;
+        const int64_t slot = item + w;
+        if (r0 + row < rows && (direct || slot < p.narrow_blocks)) {
+            float base = -INFINITY, f[4], sum = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) top = fmaxf(top, stats[k * 32 + row]);
-            const float base = top == -INFINITY ? 0.0f : top * p.c;
+            for (int k = 0; k < 4; ++k) base = fmaxf(base, stats[k * 32 + row]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                w[k] = __builtin_amdgcn_exp2f(stats[k * 32 + row] * p.c - base);
-                sum += w[k] * stats[128 + k * 32 + row];
+                f[k] = base == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stats[k * 32 + row] - base);
+                sum += f[k] * stats[128 + k * 32 + row];
             }
-            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-            const int to = (r0 + row) / p.G, tg = r0 + row - to * p.G;
-            const int64_t t = q0 + to;
-            uint16_t* out = p.O + t * p.ldo + (h * p.G + tg) * D;
+            const float inv = !direct ? 1.0f : sum > 0.0f ? 1.0f / sum : 0.0f;
+            const int to = (r0 + row) / p.G, head = h * p.G + (r0 + row - to * p.G);
+            const int64_t t = rq.q0 + to;
+            uint8_t* blk = p.blocks + (p.joint_blocks + p.packed_blocks + slot) * block_bytes<D>();
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) {
                 const int piece = k * 8 + part;
-                float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const float4 y = *reinterpret_cast<const float4*>(parts + v * 32 * D + row * D + ((piece ^ (row & 7)) << 2));
-                    x[0] = fmaf(w[v], y.x, x[0]), x[1] = fmaf(w[v], y.y, x[1]), x[2] = fmaf(w[v], y.z, x[2]), x[3] = fmaf(w[v], y.w, x[3]);
+                    const float4 z = *reinterpret_cast<const float4*>(parts + v * 32 * D + row * D + ((piece ^ (row & 7)) << 2));
+                    y[0] = fmaf(f[v], z.x, y[0]), y[1] = fmaf(f[v], z.y, y[1]), y[2] = fmaf(f[v], z.z, y[2]), y[3] = fmaf(f[v], z.w, y[3]);
                 }
-                ushort4 y;
-                y.x = f32_to_bf16_rne(x[0] * inv), y.y = f32_to_bf16_rne(x[1] * inv), y.z = f32_to_bf16_rne(x[2] * inv), y.w = f32_to_bf16_rne(x[3] * inv);
-                *reinterpret_cast<ushort4*>(out + piece * 4) = y;
+                if (direct) {
+                    *reinterpret_cast<uint2*>(p.O + t * p.ldo + head * D + piece * 4) = make_uint2(pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv));
+                } else {
+                    *reinterpret_cast<float4*>(blk + (row * D + piece * 4) * 4) = make_float4(y[0], y[1], y[2], y[3]);
+                }
             }
-            if (p.lse && part == 0)
-                p.lse[t * p.Hq + h * p.G + tg] = sum > 0.0f ? (base + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+            if (part == 0) {
+                if (!direct) *reinterpret_cast<float2*>(blk + (32 * D + row * 2) * 4) = make_float2(base, sum);
+                else if (p.lse) p.lse[t * p.Hq + head] = lse_of(base, sum);
+            }
         }
         __syncthreads();
     }
 }
 
-size_t prefix_attention_workspace(int64_t, int32_t, int32_t, int32_t, int32_t, int64_t) { return 256; }
+// ---- a piece of the line of 128-row tiles -----------------------------------------------------------------------------------------
+// Every wavefront has 32 rows; all read the same 64 tokens from LDS, of which each has asked for 16, a block ahead.
+template <int D>
+__device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds, const Sums& sums, uint8_t* lds, int64_t w) {
+    const Plan plan = uni(in_lds);
+    constexpr int TILE = 64 * D * 2;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // what follows from it is made here, not kept in registers from the kernel's start
+    const int lane = tid & 63, wave = uni(tid >> 6);
+    const int64_t to_v = p.V - p.K;
+    const uint32_t kl = key_lane<D>(lane), vl = value_lane<D>(lane);
+    int64_t x = w * plan.wide_per;
+    const int64_t end = min(x + plan.wide_per, plan.wide);
+    while (x < end) {
+        int64_t start, length, slot;
+        int h, rows, n_prefix, n_own, b = -1, first_block = 0, own = 0, r0 = 0, t_base = 0;
+        Request rq{0, 0, 0};
+        if (x < plan.wide0) {
+            // head, then piece of the prefix, then tile
+            const int64_t head = (int64_t)plan.tiles * plan.nbp * 64, piece = (int64_t)plan.tiles * plan.super * 64;
+            h = (int)(x / head);
+            const int64_t y = x - h * head;
+            const int s = (int)(y / piece), blocks = min(plan.super, plan.nbp - s * plan.super);
+            const int tile = (int)((y - s * piece) / (blocks * 64));
+            length = blocks * 64;
+            start = h * head + s * piece + tile * length;
+            r0 = tile * WROWS, rows = plan.rows - r0;
+            first_block = s * plan.super, n_prefix = blocks, n_own = 0;
+            slot = p.joint_blocks + ((int64_t)(h * plan.supers + s) * plan.tiles + tile + w) * 4;
+        } else {
+            Extent before;
+            b = find_request<true>(p, sums, x - plan.wide0, lane, before);
+            rq = request(p, b);
+            const int nt = wide_tiles(p, rq.n);
+            const int64_t seen = wide_seen(p, rq), head = wide_sum(p, seen, nt), y = x - plan.wide0 - before.wide;
+            h = (int)(y / head);
+            int lo = 0, hi = nt;  // the last tile that starts at or before y
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (wide_sum(p, seen, mid) <= y - h * head) lo = mid;
+                else hi = mid;
+            }
+            start = plan.wide0 + before.wide + h * head + wide_sum(p, seen, lo);
+            length = seen + (int64_t)(lo + 1) * p.tpt;
+            t_base = lo * p.tpt;
+            const int tokens = min(p.tpt, rq.n - t_base);
+            rows = tokens * p.G;
+            own = max(0, rq.L - rq.n + t_base + tokens);
+            n_prefix = plan.nbp, n_own = (own + 63) >> 6;
+            slot = 0;
+        }
+        const int64_t stop = min(end, start + length);
+        const int blocks = n_prefix + n_own;
+        const int k0 = (int)((x - start) * blocks / length), k1 = stop == start + length ? blocks : (int)((stop - start) * blocks / length);
+        const bool whole = x == start && stop == start + length;
+        if (b >= 0) slot = (2 * w + (x == start)) * 4;
+        x = stop;
+
+        const int r = wave * 32 + (lane & 31), rc = min(r, rows - 1);
+        int ti = rc / p.G, g = rc - ti * p.G, seen = 0;
+        if (b < 0) packed_row(p, sums, r0 + rc, ti, g);
+        else {
+            seen = rq.L - rq.n + t_base + ti + 1;
+            ti += rq.q0 + t_base;
+        }
+        const int clear_to = rq.L - rq.n + t_base + (wave * 32) / p.G + 1;  // own tokens that all of the wavefront's rows see
+        v8bf q[D / 16];
+        const uint16_t* qp = p.Q + (int64_t)ti * p.ldq + (h * p.G + g) * D + (lane >> 5) * 8;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) q[k] = *reinterpret_cast<const v8bf*>(qp + k * 16);
+
+        State<D> st;
+        clear(st);
+        // the wavefront's 16 tokens of block k: their page's number is read a block before it is needed
+        auto token = [&](int k, int& last) {
+            const bool pre = k < n_prefix;
+            const int n = pre ? p.P : own, j = ((pre ? k + first_block : k - n_prefix) * 64) + wave * 16;
+            const int jc = min(j, n - 1);
+            last = j < n ? min(15, n - 1 - j) : (n - 1) & 15;
+            return jc;
+        };
+        auto page_of = [&](int k) {
+            int last;
+            const int j = token(k, last) >> p.lg;
+            return (uint32_t)(k < n_prefix ? p.prefix_pages[j] : p.table[(int64_t)b * p.ldt + j]);
+        };
+        auto fetch = [&](int k, uint32_t page) {
+            int last;
+            const int j = token(k, last);
+            const uint8_t* run = run_of<D>(p, page, h, j);
+            uint8_t* dst = lds + (k & 1) * 2 * TILE;
+            fetch16<D>(run, wave, last, dst, lane);
+            fetch16<D>(run + to_v, wave, last, dst + TILE, lane);
+        };
+        uint32_t page = 0;
+        if (k0 < k1) {
+            fetch(k0, page_of(k0));
+            if (k0 + 1 < k1) page = page_of(k0 + 1);
+        }
+        for (int k = k0; k < k1; ++k) {
+            wait_vmcnt<0>();
+            __syncthreads();  // everyone's part of block k is there, and everyone is done with block k - 1
+            if (k + 1 < k1) {
+                fetch(k + 1, page);
+                if (k + 2 < k1) page = page_of(k + 2);
+            }
+            const uint32_t buffer = lds_at(lds) + (k & 1) * 2 * TILE;
+            if (wave * 32 < rows) {
+                const bool pre = k < n_prefix;
+                const int j0 = (pre ? k + first_block : k - n_prefix) * 64;
+                v16f s[2];
+                scores<D, 2>(s, q, buffer + kl);
+                if (j0 + 64 > (pre ? p.P : clear_to)) weigh<D, 2, true>(st, s, lane, p.c, (pre ? p.P : seen) - j0);
+                else weigh<D, 2, false>(st, s, lane, p.c, 0);
+                gather<D, 2>(st, s, buffer + TILE + vl);
+            }
+        }
+        st.sum = half_sum(st.sum);
+        const bool direct = whole && b >= 0;
+        const int hi = lane >> 5;
+        if (r < rows) {
+            if (direct) {
+                const float inv = st.sum > 0.0f ? 1.0f / st.sum : 0.0f;
+                uint16_t* out = p.O + (int64_t)ti * p.ldo + (h * p.G + g) * D;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<uint2*>(out + 32 * d + 8 * e + 4 * hi) =
+                            make_uint2(pack2(st.o[d][4 * e] * inv, st.o[d][4 * e + 1] * inv), pack2(st.o[d][4 * e + 2] * inv, st.o[d][4 * e + 3] * inv));
+                if (p.lse && hi == 0) p.lse[(int64_t)ti * p.Hq + h * p.G + g] = lse_of(st.base, st.sum);
+            } else if (slot + 4 <= p.joint_blocks + (b < 0 ? p.packed_blocks : 0)) {
+                uint8_t* blk = p.blocks + (slot + wave) * block_bytes<D>();
+                const int row = lane & 31;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<float4*>(blk + (row * D + 32 * d + 8 * e + 4 * hi) * 4) =
+                            make_float4(st.o[d][4 * e], st.o[d][4 * e + 1], st.o[d][4 * e + 2], st.o[d][4 * e + 3]);
+                if (hi == 0) *reinterpret_cast<float2*>(blk + (32 * D + row * 2) * 4) = make_float2(st.base, st.sum);
+            }
+        }
+        __syncthreads();  // the next item's first block lands where others may still be reading this one's last
+    }
+}
+
+struct AttnShared {
+    Sums sums;
+    Plan plan;
+    int64_t part[4][4];
+    float stats[256];
+};
+
+template <int D>
+__global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(const AttnArgs p) {
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    AttnShared& sh = *reinterpret_cast<AttnShared*>(lds + 8 * 32 * D * 2);  // behind the tiles, which start at 0
+    Sums& sums = sh.sums;
+    Plan& plan = sh.plan;
+    float* stats = sh.stats;
+    auto& part = sh.part;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Extent mine{0, 0, 0, 0};
+    const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
+    for (int b = b0; b < b1; ++b) {
+        const Extent e = extent(p, request(p, b));
+        mine.narrow += e.narrow, mine.items += e.items, mine.rows += e.rows, mine.wide += e.wide;
+    }
+    int64_t v[4] = {mine.narrow, mine.items, mine.rows, mine.wide}, total[4];
+    const int64_t own[4] = {mine.narrow, mine.items, mine.rows, mine.wide};
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t u = __shfl_up(v[k], d);
+            if (lane >= d) v[k] += u;
+        }
+    if (lane == 63)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) part[wave][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        v[k] -= own[k];
+        total[k] = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (u < wave) v[k] += part[u][k];
+            total[k] += part[u][k];
+        }
+    }
+    sums.narrow[tid] = v[0], sums.items[tid] = v[1], sums.rows[tid] = v[2], sums.wide[tid] = v[3];
+    if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
+        if (tid == 0) *p.plan = make_plan<D>(p, total[0], total[2], total[3]);
+        for (int b = b0; b < b1; ++b) {
+            const Extent e = extent(p, request(p, b));
+            int64_t* r = p.records + (int64_t)b * 4;
+            r[0] = v[0], r[1] = v[1], r[2] = v[2], r[3] = v[3];
+            v[0] += e.narrow, v[1] += e.items, v[2] += e.rows, v[3] += e.wide;
+        }
+    }
+    if (tid == 0) plan = make_plan<D>(p, total[0], total[2], total[3]);
+    __syncthreads();
+
+    // Workgroups are dealt to the XCDs in turn: each XCD takes a run of pieces, whose items are neighbours and share keys and values.
+    const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
+    auto piece = [&](int64_t all, int64_t per) -> int64_t {
+        const int64_t used = (all + per - 1) / per, run = (used + 7) / 8;
+        return i < run ? xcd * run + i : -1;
+    };
+    const bool swap = blockIdx.x >= attn_wgs<D>() / 2;
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {
+        if ((turn == 0) == swap) {
+            const int64_t w = piece(uni(plan.narrow), uni(plan.narrow_per));
+            if (w >= 0) narrow_piece<D>(p, plan, sums, lds, stats, w);
+        } else {
+            const int64_t w = piece(uni(plan.wide), uni(plan.wide_per));
+            if (w >= 0) wide_piece<D>(p, plan, sums, lds, w);
+        }
+    }
+}
+
+// ---- the segments of a row, joined ------------------------------------------------------------------------------------------------
+// D/4 lanes a row, four channels each.  A lane first reads base and weight of one segment, so up to D/4 of them arrive together.
+template <int D>
+__global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnArgs p) {
+    constexpr int LANES = D / 4, RPW = 64 / LANES;
+    const int lane = threadIdx.x & 63, sub = lane / LANES, l = lane % LANES;
+    const int per_token = (p.Hq + RPW - 1) / RPW;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int t = (int)(unit / per_token);
+    if (t >= p.T) return;
+    const int head = (int)(unit - (int64_t)t * per_token) * RPW + sub;
+    int lo = 0, hi = p.B + 1;  // the last request that starts at or before t
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const int n = __popcll(__ballot(at < hi && p.q_offsets[min(at, p.B)] <= t));
+        if (n == 0) return;
+        lo += (n - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    const int b = lo;
+    if (b >= p.B || head >= p.Hq) return;
+    const Request rq = request(p, b);
+    const int i = t - rq.q0;
+    if (i < 0 || i >= rq.n) return;
+    const Plan& plan = *p.plan;
+    const int64_t* rec = p.records + (int64_t)b * 4;
+    const int h = head / p.G, g = head - h * p.G, r = i * p.G + g;
+
+    // `count` segments at most; segment j's block and the row in it, or no block
+    int64_t s0, s1, first, packed0 = 0;
+    int own, more = 0, tile = 0, at_row, spread_pre = 0;
+    const bool joint = is_long(p, rq.n);
+    if (joint) {
+        const int64_t seen = wide_seen(p, rq);
+        tile = i / p.tpt;
+        s0 = plan.wide0 + rec[3] + h * wide_sum(p, seen, wide_tiles(p, rq.n)) + wide_sum(p, seen, tile);
+        s1 = s0 + seen + (int64_t)(tile + 1) * p.tpt;
+        first = s0 / plan.wide_per;
+        own = (int)((s1 - 1) / plan.wide_per - first) + 1;
+        if (own == 1) return;  // written by the first kernel
+        at_row = r - tile * p.tpt * p.G;
+    } else {
+        const int length = narrow_length(rq.L);
+        const int64_t k = (int64_t)h * narrow_tiles(p, rq.n) + r / 32;
+        s0 = plan.narrow0 + rec[0] + k * length;
+        s1 = s0 + length;
+        first = s0 / plan.narrow_per;
+        own = (int)((s1 - 1) / plan.narrow_per - first) + 1;
+        if (own == 1 && p.P == 0) return;
+        at_row = r & 31;
+        first += plan.items0 + rec[1] + k;  // its block in the narrow part
+        packed0 = rec[2] + r;
+        if (p.P) {
+            if (plan.tiles) {
+                spread_pre = (int)((plan.super * 64 - 1) / plan.wide_per) + 2;
+                more = plan.supers * spread_pre;
+            } else {
+                const int cp = (p.P + 31) >> 5;
+                more = (int)(((int64_t)(h + 1) * cp - 1) / plan.narrow_per - (int64_t)h * cp / plan.narrow_per) + 1;
+            }
+        }
+    }
+    auto block_of = [&](int j, int& row) -> int64_t {
+        if (j < own) {
+            row = at_row & 31;
+            if (joint) return (2 * (first + j) + (j == 0)) * 4 + (at_row >> 5);
+            return first + j < p.narrow_blocks ? p.joint_blocks + p.packed_blocks + first + j : -1;
+        }
+        j -= own;
+        if (j >= more) return -1;
+        if (!plan.tiles) {
+            const int64_t blk = h + (int64_t)h * ((p.P + 31) >> 5) / plan.narrow_per + j;
+            row = (int)packed0 & 31;
+            return blk < p.narrow_blocks ? p.joint_blocks + p.packed_blocks + blk : -1;
+        }
+        const int s = j / spread_pre, k = j - s * spread_pre, pt = (int)(packed0 / WROWS), blocks = min(plan.super, plan.nbp - s * plan.super);
+        const int64_t a = (int64_t)h * plan.tiles * plan.nbp * 64 + (int64_t)s * plan.tiles * plan.super * 64 + (int64_t)pt * blocks * 64;
+        const int64_t w = a / plan.wide_per + k;
+        if (w > (a + blocks * 64 - 1) / plan.wide_per) return -1;
+        row = (int)packed0 & 31;
+        const int64_t blk = ((int64_t)(h * plan.supers + s) * plan.tiles + pt + w) * 4;
+        return blk + 4 <= p.packed_blocks ? p.joint_blocks + blk + ((packed0 % WROWS) >> 5) : -1;
+    };
+    float base = -INFINITY, sum = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const int count = own + more;
+    for (int j0 = 0; j0 < count; j0 += LANES) {
+        int row = 0;
+        const int64_t blk = block_of(j0 + l, row);
+        float bs = -INFINITY, wt = 0.0f;
+        const uint8_t* at = p.blocks + (blk < 0 ? 0 : blk) * block_bytes<D>();
+        if (blk >= 0) {
+            const float2 z = *reinterpret_cast<const float2*>(at + (32 * D + row * 2) * 4);
+            bs = z.x, wt = z.y;
+        }
+        float top = bs;
+#pragma unroll
+        for (int d = 1; d < LANES; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        const float next = fmaxf(base, top), fade = next == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(base - next);
+        acc.x *= fade, acc.y *= fade, acc.z *= fade, acc.w *= fade;
+        sum *= fade;
+        base = next;
+        const float f = wt > 0.0f ? __builtin_amdgcn_exp2f(bs - base) : 0.0f;  // a segment without weight may not have left sums
+        const int64_t off = (at - p.blocks) + row * D * 4;
+        const int m = min(LANES, count - j0);
+        for (int j = 0; j < m; ++j) {
+            const float fj = __shfl(f, sub * LANES + j), wj = __shfl(wt, sub * LANES + j);
+            const int64_t oj = __shfl(off, sub * LANES + j);
+            if (fj > 0.0f) {
+                const float4 z = *reinterpret_cast<const float4*>(p.blocks + oj + l * 16);
+                acc.x = fmaf(fj, z.x, acc.x), acc.y = fmaf(fj, z.y, acc.y), acc.z = fmaf(fj, z.z, acc.z), acc.w = fmaf(fj, z.w, acc.w);
+                sum = fmaf(fj, wj, sum);
+            }
+        }
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    *reinterpret_cast<uint2*>(p.O + (int64_t)t * p.ldo + head * D + l * 4) = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+    if (p.lse && l == 0) p.lse[(int64_t)t * p.Hq + head] = lse_of(base, sum);
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------------------
+struct AttnSpace {
+    int64_t joint, packed, narrow;  // blocks
+    size_t records, blocks, total;  // offsets
+};
+static AttnSpace attn_space(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t P) {
+    const int64_t G = Hq / Hkv, rows = T * G, wgs = D == 128 ? attn_wgs<128>() : attn_wgs<64>(), some = std::min<int64_t>(B, T);
+    const int64_t is_short = P ? std::min<int64_t>(rows, 255 * (int64_t)B) : 0;  // rows that walk the prefix packed, at most
+    AttnSpace a;
+    a.joint = rows >= (P ? 256 : 33) ? 2 * wgs * 4 : 0;
+    const int64_t tiles = (is_short + WROWS - 1) / WROWS;
+    a.packed = is_short > 32 ? (Hkv * tiles * super_count(P, tiles) + wgs) * 4 : 0;
+    a.narrow = Hkv * (1 + (P ? is_short / 32 + some : some)) + wgs;
+    a.records = 256;
+    a.blocks = align_up(a.records + (size_t)B * 32, 256);
+    a.total = a.blocks + (size_t)(a.joint + a.packed + a.narrow) * (32 * (D + 2) * 4);
+    return a;
+}
+
+size_t prefix_attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
+    return attn_space(T, B, Hq, Hkv, D, prefix_len).total;
+}
+
+template <int D>
+static int launch(const AttnArgs& p, hipStream_t st) {
+    static LdsReserved r;
+    constexpr size_t lds = 8 * 32 * D * 2 + sizeof(AttnShared);
+    const int rc = reserve_lds((const void*)prefix_attention_kernel<D>, lds, r);
+    if (rc) return rc;
+    constexpr int rows = 64 / (D / 4);
+    const int64_t waves = p.T * ((p.Hq + rows - 1) / rows), wgs = (waves + 3) / 4;
+    prefix_attention_kernel<D><<<dim3(attn_wgs<D>()), WG, lds, st>>>(p);
+    prefix_attention_join_kernel<D><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
+    return check_launch("osc_prefix_attention");
+}
 
 int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
     AttnArgs p;
     p.Q = static_cast<const uint16_t*>(a.Q), p.T = a.T, p.ldq = a.ldq, p.Hq = a.Hq, p.Hkv = a.Hkv, p.G = a.Hq / a.Hkv;
+    p.tpt = WROWS / p.G;
     p.K = static_cast<const uint8_t*>(a.K), p.V = static_cast<const uint8_t*>(a.V), p.n_pages = (uint32_t)a.n_pages, p.lg = a.lg;
     p.prefix_pages = a.prefix_pages, p.P = (int)a.prefix_len, p.table = a.table, p.ldt = a.ldt;
-    p.max_kv = (int)std::min<int64_t>(a.ldt << a.lg, 0x7fffffff);
-    p.kv_lens = a.kv_lens, p.q_offsets = a.q_offsets, p.B = a.B, p.c = a.scale * 1.44269504088896341f;
+    p.max_kv = (int)std::min<int64_t>(a.ldt << a.lg, 0x3fffffff);
+    p.kv_lens = a.kv_lens, p.q_offsets = a.q_offsets, p.B = a.B, p.per = (a.B + GROUPS - 1) / GROUPS, p.c = a.scale * 1.44269504088896341f;
     p.O = static_cast<uint16_t*>(a.O), p.ldo = a.ldo, p.lse = a.lse;
-    const int cus = cu_count();
-    if (cus <= 0) return fail(OSC_ERR_HIP, "osc_prefix_attention: cannot read the device");
-    auto go = [&](auto kernel, LdsReserved& r, size_t lds) {
-        const int rc = reserve_lds((const void*)kernel, lds, r);
-        if (rc) return rc;
-        const int64_t most = ((int64_t)a.B + a.T * p.G / 32) * a.Hkv;
-        kernel<<<dim3((unsigned)std::min<int64_t>(most, 2 * cus)), 256, lds, st>>>(p);
-        return check_launch("osc_prefix_attention");
-    };
-    static LdsReserved r64, r128;
-    const size_t extra = 1024 + ((size_t)a.B + 1) * 4;
-    if (a.D == 64) return go(prefix_attention_kernel<64>, r64, 8 * 32 * 64 * 2 + extra);
-    return go(prefix_attention_kernel<128>, r128, 8 * 32 * 128 * 2 + extra);
+    const AttnSpace s = attn_space(a.T, a.B, a.Hq, a.Hkv, a.D, a.prefix_len);
+    p.plan = reinterpret_cast<Plan*>(a.workspace), p.records = reinterpret_cast<int64_t*>(a.workspace + s.records);
+    p.blocks = a.workspace + s.blocks;
+    p.joint_blocks = s.joint, p.packed_blocks = s.packed, p.narrow_blocks = s.narrow;
+    return a.D == 64 ? launch<64>(p, st) : launch<128>(p, st);
 }
 
 }  // namespace osc

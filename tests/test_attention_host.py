@@ -58,7 +58,7 @@ def test_rope_refusals(code, change):
 @pytest.mark.parametrize("code,change", [
     (SHAPE, dict(Hq=7)), (UNSUPPORTED, dict(D=80)), (UNSUPPORTED, dict(ps=20)), (SHAPE, dict(T=-1)), (SHAPE, dict(B=-1)), (SHAPE, dict(ldt=-1)), (SHAPE, dict(P=-1)),
     (UNSUPPORTED, dict(B=8193)), (UNSUPPORTED, dict(P=2 ** 30)), (SHAPE, dict(ldq=1016)), (SHAPE, dict(ldo=1016)), (SHAPE, dict(scale=0.0)), (SHAPE, dict(scale=-1.0)),
-    (SHAPE, dict(scale=float("nan"))), (SHAPE, dict(scale=float("inf"))), (NULL, dict(Q=None)), (NULL, dict(O=None)), (NULL, dict(kv=None)), (NULL, dict(offs=None)),
+    (UNSUPPORTED, dict(Hq=129, Hkv=1, D=64, ldq=129 * 64, ldo=129 * 64)), (SHAPE, dict(scale=float("nan"))), (SHAPE, dict(scale=float("inf"))), (NULL, dict(Q=None)), (NULL, dict(O=None)), (NULL, dict(kv=None)), (NULL, dict(offs=None)),
     (NULL, dict(ws=None)), (NULL, dict(table=None)), (NULL, dict(pp=None)), (NULL, dict(K=None)), (NULL, dict(V=None)), (NULL, dict(n_pages=0)),
     (UNSUPPORTED, dict(Q=P + 2)), (UNSUPPORTED, dict(ldq=1028)), (UNSUPPORTED, dict(O=P + 8)), (UNSUPPORTED, dict(ldo=1028)), (UNSUPPORTED, dict(ws=P + 16)),
     (UNSUPPORTED, dict(K=P + 4)), (WORKSPACE, dict()), (0, dict(T=0, Q=None)), (0, dict(B=0, kv=None))])

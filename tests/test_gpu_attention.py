@@ -259,6 +259,35 @@ def test_attention_one_long_request(osc):
     check_attention(osc, make(5, 2, 1000, [900, 3], [3, 2], 4, 2, 128, 16))
 
 
+@pytest.mark.parametrize("P", [0, 50])
+@pytest.mark.parametrize("B", [257, 600, 1100])
+def test_attention_many_requests(osc, B, P):
+    """more requests than a workgroup has lanes; idle and empty ones among them, and two long ones"""
+    gen = np.random.default_rng(B + P)
+    n, kv = gen.integers(0, 3, B), gen.integers(0, 40, B)
+    n[B // 3], kv[B // 3] = 150, 170
+    n[B - 2], kv[B - 2] = 129, 129
+    check_attention(osc, make(B + P, B, P, kv.tolist(), n.tolist(), 2, 1, 64, 16))
+
+
+def test_attention_long_prefix(osc):
+    """a prefix in several pieces, packed rows of several tiles that cut requests in two"""
+    n = [1, 3, 2, 1, 7] * 8
+    kv = [5, 3, 40, 100, 9] * 8
+    check_attention(osc, make(11, 40, 9001, kv, n, 8, 1, 64, 64))
+    check_attention(osc, make(12, 40, 4097, kv, n, 6, 1, 128, 128))
+
+
+def test_attention_prompts(osc):
+    check_attention(osc, make(13, 2, 100, [500, 410], [500, 300], 4, 2, 128, 16))
+    check_attention(osc, make(14, 3, 0, [333, 1, 700], [333, 1, 200], 5, 1, 64, 32))
+
+
+def test_attention_many_heads_a_key_head(osc):
+    check_attention(osc, make(15, 3, 70, [40, 3, 100], [3, 1, 2], 128, 1, 64, 16))
+    check_attention(osc, make(16, 3, 0, [40, 3, 100], [3, 1, 2], 100, 1, 128, 16))
+
+
 def test_attention_sharp_and_flat(osc):
     """scores up to several hundred, whose maximum rises from tile to tile; and all alike"""
     s = make(6, 3, 70, [100, 37, 200], [1, 2, 1], 8, 2, 128, 32, std=40.0)
