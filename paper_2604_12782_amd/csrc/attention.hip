@@ -30,8 +30,8 @@ constexpr int WG = 256, WROWS = 128, GROUPS = 256;
 // Workgroups: two on a CU (LDS for their tiles), three where heads are small.
 template <int D>
 constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
-// The smallest pieces of the two lines: four tiles of 32 tokens (one a wavefront), and tokens of a wide tile
-constexpr int MIN_NARROW = 4, MIN_WIDE = 512;
+// The smallest pieces of the two lines
+constexpr int MIN_NARROW = 1, MIN_WIDE = 512, WIDE_EDGE = 128;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
 
 struct AttnArgs {
@@ -84,10 +84,13 @@ __device__ __forceinline__ Request request(const AttnArgs& p, int b) {
 }
 __device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? 256 : 33); }
 __device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (n * p.G + 31) >> 5; }
-__device__ __forceinline__ int narrow_length(int L) { return max(1, (L + 31) >> 5); }
+// The line of 32-row tiles is measured in 128 tokens (a tile a wavefront), and starting and ending a segment costs about half of that
+__device__ __forceinline__ int narrow_length(int L) { return (L + 191) >> 7; }
+__device__ __forceinline__ int narrow_tile(int64_t y) { return max(0, (int)(4 * y) - 2); }  // where place y of an item is, in tiles of 32
 // tokens that the first k tiles of a long request walk: each sees `seen` and tpt more than the one before it
 __device__ __forceinline__ int64_t wide_sum(const AttnArgs& p, int64_t seen, int64_t k) { return k * seen + p.tpt * (k * (k + 1) / 2); }
-__device__ __forceinline__ int64_t wide_seen(const AttnArgs& p, const Request& r) { return p.P + max(r.L - r.n, 0); }
+// and what starting and ending a segment costs, as tokens
+__device__ __forceinline__ int64_t wide_seen(const AttnArgs& p, const Request& r) { return WIDE_EDGE + p.P + max(r.L - r.n, 0); }
 __device__ __forceinline__ int wide_tiles(const AttnArgs& p, int n) { return (n + p.tpt - 1) / p.tpt; }
 __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r) {
     Extent e{0, 0, 0, 0};
@@ -106,7 +109,7 @@ __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r) {
 struct Plan {
     int64_t narrow, wide;        // lengths of the lines
     int64_t narrow0, items0;     // of which the prefix's narrow items are the first
-    int64_t wide0;               // of which the packed tiles are the first
+    int64_t wide0, head;         // of which the packed tiles are the first, `head` for every key/value head
     int64_t narrow_per, wide_per;
     int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; blocks of 64 tokens: of a piece of the prefix, of the prefix
 };
@@ -120,17 +123,18 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int64_t narrow, int
     Plan a;
     a.rows = (int)min(rows, p.T * p.G);
     a.nbp = (p.P + 63) >> 6;
-    a.narrow0 = a.items0 = a.wide0 = 0;
+    a.narrow0 = a.items0 = a.wide0 = a.head = 0;
     a.tiles = a.supers = a.super = 0;
     if (a.rows > 32) {
         a.tiles = (a.rows + WROWS - 1) / WROWS;
         a.supers = super_count(p.P, a.tiles);
         a.super = (a.nbp + a.supers - 1) / a.supers;
         a.supers = (a.nbp + a.super - 1) / a.super;
-        a.wide0 = (int64_t)p.Hkv * a.tiles * a.nbp * 64;
+        a.head = (int64_t)a.tiles * (a.nbp * 64 + a.supers * WIDE_EDGE);
+        a.wide0 = p.Hkv * a.head;
     } else if (a.rows > 0) {
         a.items0 = p.Hkv;
-        a.narrow0 = (int64_t)p.Hkv * ((p.P + 31) >> 5);
+        a.narrow0 = (int64_t)p.Hkv * narrow_length(p.P);
     }
     a.narrow = a.narrow0 + narrow;
     a.wide = a.wide0 + wide;
@@ -142,7 +146,7 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int64_t narrow, int
 
 // what all lanes read from LDS, as the scalars that it is
 __device__ __forceinline__ Plan uni(const Plan& a) {
-    return Plan{uni(a.narrow), uni(a.wide), uni(a.narrow0), uni(a.items0), uni(a.wide0), uni(a.narrow_per), uni(a.wide_per),
+    return Plan{uni(a.narrow), uni(a.wide), uni(a.narrow0), uni(a.items0), uni(a.wide0), uni(a.head), uni(a.narrow_per), uni(a.wide_per),
                 uni(a.rows), uni(a.tiles), uni(a.supers), uni(a.super), uni(a.nbp)};
 }
 
@@ -203,6 +207,8 @@ __device__ __forceinline__ void packed_row(const AttnArgs& p, const Sums& s, int
     g = min((int)(r - at) - i * p.G, p.G - 1);
 }
 
+__device__ __forceinline__ uint32_t lds_at(const uint8_t* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p; }
+
 // ---- tiles of cached tokens in LDS ---------------------------------------------------------------------------------------------
 // Rows of D bf16 in pieces of 16 bytes; piece c of row r sits at c ^ spread(r), so that both readers find all banks: keys by
 // 32 rows of one piece, values by 8 rows of four neighbouring pieces.
@@ -212,19 +218,27 @@ __device__ __forceinline__ int spread(int r) {
 }
 // Start of the 16-token run that token j lies in (a page holds whole runs), for keys; values lie V - K further.
 template <int D>
-__device__ __forceinline__ const uint8_t* run_of(const AttnArgs& p, uint32_t page, int h, int j) {
+__device__ __forceinline__ const uint8_t* run_of(const AttnArgs& p, int page_number, int h, int j) {
+    uint32_t page = (uint32_t)uni(page_number);
     if (page >= p.n_pages) page = 0;  // nothing outside the cache is read, whatever a table holds
     return p.K + ((((int64_t)page * p.Hkv + h) << p.lg) + ((j & ((1 << p.lg) - 1)) & ~15)) * (D * 2);
 }
-// Asks for 16 rows, tile rows 16 * half .., of which `last` + 1 exist from the run's start: rows past the last token repeat it, so that whatever a
-// page holds there is never multiplied.
+// 16 bytes a lane from memory to LDS, at `to` + 16 lane.  (The request's own instruction, not the compiler's builtin: that
+// makes every later LDS read wait for all requests on their way, also those for other tiles.  It has no result in
+// registers; the waits are counted by hand below.)
+__device__ __forceinline__ void request16(const uint8_t* base, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");  // m0 is not the compiler's to keep: it sets it before any use
+}
+// Asks for 16 rows, tile rows 16 * half .., of which `last` + 1 exist from the run's start: rows past the last token repeat it, so that
+// whatever a page holds there is never multiplied.
 template <int D>
-__device__ __forceinline__ void fetch16(const uint8_t* run, int half, int last, uint8_t* dst, int lane) {
+__device__ __forceinline__ void fetch16(const uint8_t* run, int half, int last, uint32_t to, int lane) {
     constexpr int CH = D / 8, RPI = 64 / CH, NI = 16 / RPI;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int r = i * RPI + lane / CH, piece = (lane % CH) ^ spread<D>(r);  // spread() repeats after 16 rows
-        load_to_lds16(run + min(r, last) * (D * 2) + piece * 16, dst + half * (16 * D * 2) + i * 1024);
+        const uint32_t whole = r * (D * 2) + piece * 16, cut = min(r, last) * (D * 2) + piece * 16;
+        request16(run, last == 15 ? whole : cut, to + half * (16 * D * 2) + i * 1024);
     }
 }
 
@@ -256,8 +270,6 @@ __device__ __forceinline__ float half_sum(float v) {
 // N tiles of 32 tokens: S^T = K Q^T leaves a lane 16 tokens of its row a tile, the weights go to bf16 and are the second operand of
 // O^T += V^T P^T as they lie, because the order of the tokens inside a product is free as long as both operands have the same.
 // LDS addresses are numbers, the lane's part made once: a tile starts at a multiple of 256 bytes, so a piece's place is an exclusive or.
-// Fragments are read in batches that wait for themselves while the products of the batch before run.  (The compiler
-// would put a wait for every request on its way from HBM before the reads, which are of another buffer.)
 template <int D>
 __device__ __forceinline__ uint32_t key_lane(int lane) {
     const int r = lane & 31;
@@ -268,77 +280,47 @@ __device__ __forceinline__ uint32_t value_lane(int lane) {
     const int i = lane & 15, row = 4 * (lane >> 5) + (i >> 2);
     return row * (D * 2) + (((((lane >> 4) & 1) * 2 + ((i & 3) >> 1)) ^ spread<D>(row)) << 4) + (i & 1) * 8;
 }
-template <int X, int Y>
-__device__ __forceinline__ void read_keys(v8bf (&f)[4], uint32_t a, uint32_t b) {  // X, Y: offsets of two rows' pieces
-    asm volatile(
-        "ds_read_b128 %0, %4 offset:%6\n\tds_read_b128 %1, %4 offset:%7\n\tds_read_b128 %2, %5 offset:%6\n\tds_read_b128 %3, %5 offset:%7\n\t"
-        "s_waitcnt lgkmcnt(0)"
-        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
-        : "v"(a), "v"(b), "i"(X), "i"(Y)
-        : "memory");
-}
-__device__ __forceinline__ void read_keys(v8bf (&f)[4], uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    asm volatile(
-        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
-        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
-        : "v"(a), "v"(b), "v"(c), "v"(d)
-        : "memory");
-}
-template <int X, int Y>
-__device__ __forceinline__ void read_values(v4s (&f)[4], uint32_t a, uint32_t b, uint32_t c, uint32_t d) {  // two channels' pieces, two runs of tokens each
-    asm volatile(
-        "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%9\n\tds_read_b64_tr_b16 %2, %6 offset:%8\n\t"
-        "ds_read_b64_tr_b16 %3, %7 offset:%9\n\ts_waitcnt lgkmcnt(0)"
-        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
-        : "v"(a), "v"(b), "v"(c), "v"(d), "i"(X), "i"(Y)
-        : "memory");
-}
-template <int X, int Y>
-__device__ __forceinline__ void read_values(v4s (&f)[8], const uint32_t (&a)[8]) {
-    asm volatile(
-        "ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%17\n\tds_read_b64_tr_b16 %2, %10 offset:%16\n\t"
-        "ds_read_b64_tr_b16 %3, %11 offset:%17\n\tds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%17\n\t"
-        "ds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%17\n\ts_waitcnt lgkmcnt(0)"
-        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7])
-        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]), "i"(X), "i"(Y)
-        : "memory");
-}
 __device__ __forceinline__ v16f mfma(v8bf a, v8bf b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-
+__device__ __forceinline__ v8bf read16(uint32_t at) { return *(const __attribute__((address_space(3))) v8bf*)(uintptr_t)at; }
+__device__ __forceinline__ v4s read_turned(uint32_t at) {  // four rows of one channel, of 16 channels over 16 lanes
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)at);
+}
+// Reads run a batch ahead of the products: the barriers keep the compiler from drawing each read to its use.
 template <int D, int N>
 __device__ __forceinline__ void scores(v16f (&s)[N], const v8bf (&q)[D / 16], uint32_t kt) {
+    constexpr int BATCH = 4 / N, STEPS = D / 16 / BATCH;  // pieces of a batch: four reads
+    v8bf f[2][BATCH][N];
+    auto read = [&](int j) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+            for (int u = 0; u < N; ++u) f[j & 1][i][u] = read16((kt ^ ((j * BATCH + i) << 5)) + u * (32 * D * 2));
+    };
 #pragma unroll
     for (int u = 0; u < N; ++u) s[u] = v16f{};
-    v8bf f[4];
-    if constexpr (N == 2) {
+    read(0);
 #pragma unroll
-        for (int k = 0; k < D / 16; k += 2) {
-            read_keys<0, 32 * D * 2>(f, kt ^ (k << 5), kt ^ ((k + 1) << 5));
-            s[0] = mfma(f[0], q[k], s[0]);
-            s[1] = mfma(f[1], q[k], s[1]);
-            s[0] = mfma(f[2], q[k + 1], s[0]);
-            s[1] = mfma(f[3], q[k + 1], s[1]);
-        }
-    } else {
+    for (int j = 0; j < STEPS; ++j) {
+        if (j + 1 < STEPS) read(j + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int k = 0; k < D / 16; k += 4) {
-            read_keys(f, kt ^ (k << 5), kt ^ ((k + 1) << 5), kt ^ ((k + 2) << 5), kt ^ ((k + 3) << 5));
+        for (int i = 0; i < BATCH; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[0] = mfma(f[j], q[k + j], s[0]);
-        }
+            for (int u = 0; u < N; ++u) s[u] = mfma(f[j & 1][i][u], q[j * BATCH + i], s[u]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 // `seen`: tokens below it count for the lane's row
-template <int D, int N, bool MASK>
-__device__ __forceinline__ void weigh(State<D>& st, v16f (&s)[N], int lane, float c, int seen) {
-    if (MASK) {
-        const int hi = lane >> 5;
+template <int N>
+__device__ __forceinline__ void mask(v16f (&s)[N], int lane, int seen) {
+    const int left = seen - 4 * (lane >> 5);
 #pragma unroll
-        for (int u = 0; u < N; ++u)
+    for (int u = 0; u < N; ++u)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (32 * u + (e & 3) + 8 * (e >> 2) + 4 * hi >= seen) s[u][e] = -INFINITY;
-    }
+        for (int e = 0; e < 16; ++e) s[u][e] = 32 * u + (e & 3) + 8 * (e >> 2) < left ? s[u][e] : -INFINITY;
+}
+template <int D, int N>
+__device__ __forceinline__ void weigh(State<D>& st, v16f (&s)[N], float c) {
     float top = s[0][0];
 #pragma unroll
     for (int u = 0; u < N; ++u)
@@ -366,32 +348,34 @@ __device__ __forceinline__ void weigh(State<D>& st, v16f (&s)[N], int lane, floa
         }
     st.sum += sum;
 }
-// tokens 16 T .. of the tile, times the weights of half a score tile
-template <int D, int T>
-__device__ __forceinline__ void gather16(State<D>& st, const v16f& s, const uint32_t (&at)[D / 16]) {
-    v8bf w;  // rounded to 8 bits for the matrix core: half an ulp each, and of either sign; their sum is taken before
+template <int D>
+union Values {  // 16 tokens of all channels
+    v4s part[D / 16];
+    v8bf all[D / 32];
+};
+template <int D>
+__device__ __forceinline__ void read_values(Values<D>& f, uint32_t vt, int t) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = (__bf16)s[8 * (T & 1) + e];
-    constexpr int X = 16 * T * D * 2, Y = X + 8 * D * 2;
-    union {
-        v4s part[D / 16];
-        v8bf all[D / 32];
-    } f;
-    if constexpr (D == 128) read_values<X, Y>(f.part, at);
-    else read_values<X, Y>(f.part, at[0], at[1], at[2], at[3]);
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d) st.o[d] = mfma(f.all[d], w, st.o[d]);
+    for (int d = 0; d < D / 32; ++d) {
+        f.part[2 * d] = read_turned((vt ^ (d << 6)) + 16 * t * (D * 2));
+        f.part[2 * d + 1] = read_turned((vt ^ (d << 6) ^ 32) + (16 * t + 8) * (D * 2));  // eight tokens on, the spread differs in one bit
+    }
 }
+// `f`: the first 16 tokens' values
 template <int D, int N>
-__device__ __forceinline__ void gather(State<D>& st, const v16f (&s)[N], uint32_t vt) {
-    uint32_t at[D / 16];  // a run of eight tokens on, the spread differs in one bit
+__device__ __forceinline__ void gather(State<D>& st, const v16f (&s)[N], const Values<D>& first, uint32_t vt) {
+    Values<D> f[2];
+    f[0] = first;
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) at[2 * d] = vt ^ (d << 6), at[2 * d + 1] = vt ^ (d << 6) ^ 32;
-    gather16<D, 0>(st, s[0], at);
-    gather16<D, 1>(st, s[0], at);
-    if constexpr (N == 2) {
-        gather16<D, 2>(st, s[1], at);
-        gather16<D, 3>(st, s[1], at);
+    for (int t = 0; t < 2 * N; ++t) {
+        if (t + 1 < 2 * N) read_values<D>(f[(t + 1) & 1], vt, t + 1);
+        v8bf w;  // rounded to 8 bits for the matrix core: half an ulp each, and of either sign; their sum is taken before
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (__bf16)s[t >> 1][8 * (t & 1) + e];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) st.o[d] = mfma(f[t & 1].all[d], w, st.o[d]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -403,10 +387,17 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 __device__ __forceinline__ float lse_of(float base, float sum) {
     return sum > 0.0f ? (base + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
 }
-__device__ __forceinline__ uint32_t lds_at(const uint8_t* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p; }
 __device__ __forceinline__ void lds_order() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_sched_barrier(0);
+}
+
+// a barrier for LDS alone: it does not wait for stores to memory
+__device__ __forceinline__ void lds_barrier() {
+    lds_order();
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    lds_order();
 }
 
 // ---- a piece of the line of 32-row tiles ----------------------------------------------------------------------------------------
@@ -421,8 +412,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
     asm volatile("" : "+v"(tid));  // what follows from it is made here, not kept in registers from the kernel's start
     const int lane = tid & 63, wave = uni(tid >> 6);
     const int64_t to_v = p.V - p.K;
-    uint8_t *kt = lds + wave * 2 * TILE, *vt = kt + TILE;
-    const uint32_t kl = lds_at(kt) + key_lane<D>(lane), vl = lds_at(vt) + value_lane<D>(lane);
+    const uint32_t kt = lds_at(lds) + wave * 2 * TILE, vt = kt + TILE, kl = kt + key_lane<D>(lane), vl = vt + value_lane<D>(lane);
     int64_t x = w * plan.narrow_per;
     const int64_t end = min(x + plan.narrow_per, plan.narrow);
     while (x < end) {
@@ -432,7 +422,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
         Request rq{0, 0, 0};
         const int32_t* pages;
         if (x < plan.narrow0) {
-            length = (p.P + 31) >> 5;
+            length = narrow_length(p.P);
             h = (int)(x / length);
             start = (int64_t)h * length, item = h;
             r0 = 0, rows = plan.rows, tokens = p.P, clear_to = p.P, pages = p.prefix_pages;
@@ -449,7 +439,8 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
             pages = p.table + (int64_t)b * p.ldt;
         }
         const int64_t stop = min(end, start + length);
-        const int t0 = (int)(x - start), t1 = min((int)(stop - start), (tokens + 31) >> 5);
+        const int t0 = narrow_tile(x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(stop - start), (tokens + 31) >> 5);
+        const bool whole = x == start && stop == start + length;
         x = stop;
 
         const int rc = min(r0 + (lane & 31), rows - 1);
@@ -470,10 +461,10 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
         clear(st);
         auto runs = [&](int tile, const uint8_t*& a, const uint8_t*& c) {
             const int j = tile * 32, j2 = min(j + 16, tokens - 1);
-            a = run_of<D>(p, (uint32_t)pages[j >> p.lg], h, j);
-            c = run_of<D>(p, (uint32_t)pages[j2 >> p.lg], h, j2);
+            a = run_of<D>(p, pages[j >> p.lg], h, j);
+            c = run_of<D>(p, pages[j2 >> p.lg], h, j2);
         };
-        auto fetch = [&](int tile, const uint8_t* a, const uint8_t* c, int64_t shift, uint8_t* dst) {
+        auto fetch = [&](int tile, const uint8_t* a, const uint8_t* c, int64_t shift, uint32_t dst) {
             const int left = tokens - 1 - tile * 32;
             fetch16<D>(a + shift, 0, min(left, 15), dst, lane);
             fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : ((tokens - 1) & 15), dst, lane);
@@ -497,12 +488,14 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
             __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the keys are read
             if (more) fetch(tile + 4, na, nb, 0, kt);
             const int j0 = tile * 32;
-            if (j0 + 32 > clear_to) weigh<D, 1, true>(st, s, lane, p.c, seen - j0);
-            else weigh<D, 1, false>(st, s, lane, p.c, 0);
+            if (j0 + 32 > clear_to) mask<1>(s, lane, seen - j0);
+            weigh<D, 1>(st, s, p.c);
             if (more) wait_vmcnt<NI>();
             else wait_vmcnt<0>();
             lds_order();
-            gather<D, 1>(st, s, vl);
+            Values<D> f;
+            read_values<D>(f, vl, 0);
+            gather<D, 1>(st, s, f, vl);
             lds_order();
             __builtin_amdgcn_s_waitcnt(0xC07F);
             if (more) fetch(tile + 4, na, nb, to_v, vt);
@@ -521,7 +514,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
         if (lane < 32) stats[wave * 32 + lane] = st.base, stats[128 + wave * 32 + lane] = st.sum;
         __syncthreads();
         const int row = tid >> 3, part = tid & 7;
-        const bool direct = p.P == 0 && t0 == 0 && stop == start + length;
+        const bool direct = p.P == 0 && whole;
         const int64_t slot = item + w;
         if (r0 + row < rows && (direct || slot < p.narrow_blocks)) {
             float base = -INFINITY, f[4], sum = 0.0f;
@@ -556,7 +549,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
                 else if (p.lse) p.lse[t * p.Hq + head] = lse_of(base, sum);
             }
         }
-        __syncthreads();
+        lds_barrier();
     }
 }
 
@@ -579,13 +572,13 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
         Request rq{0, 0, 0};
         if (x < plan.wide0) {
             // head, then piece of the prefix, then tile
-            const int64_t head = (int64_t)plan.tiles * plan.nbp * 64, piece = (int64_t)plan.tiles * plan.super * 64;
-            h = (int)(x / head);
-            const int64_t y = x - h * head;
+            const int64_t piece = (int64_t)plan.tiles * (plan.super * 64 + WIDE_EDGE);
+            h = (int)(x / plan.head);
+            const int64_t y = x - h * plan.head;
             const int s = (int)(y / piece), blocks = min(plan.super, plan.nbp - s * plan.super);
-            const int tile = (int)((y - s * piece) / (blocks * 64));
-            length = blocks * 64;
-            start = h * head + s * piece + tile * length;
+            length = blocks * 64 + WIDE_EDGE;
+            const int tile = (int)((y - s * piece) / length);
+            start = h * plan.head + s * piece + tile * length;
             r0 = tile * WROWS, rows = plan.rows - r0;
             first_block = s * plan.super, n_prefix = blocks, n_own = 0;
             slot = p.joint_blocks + ((int64_t)(h * plan.supers + s) * plan.tiles + tile + w) * 4;
@@ -613,7 +606,8 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
         }
         const int64_t stop = min(end, start + length);
         const int blocks = n_prefix + n_own;
-        const int k0 = (int)((x - start) * blocks / length), k1 = stop == start + length ? blocks : (int)((stop - start) * blocks / length);
+        auto block_at = [&](int64_t y) { return y >= length ? blocks : (int)(max(y - WIDE_EDGE, (int64_t)0) * blocks / (length - WIDE_EDGE)); };
+        const int k0 = block_at(x - start), k1 = block_at(stop - start);
         const bool whole = x == start && stop == start + length;
         if (b >= 0) slot = (2 * w + (x == start)) * 4;
         x = stop;
@@ -644,38 +638,45 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
         auto page_of = [&](int k) {
             int last;
             const int j = token(k, last) >> p.lg;
-            return (uint32_t)(k < n_prefix ? p.prefix_pages[j] : p.table[(int64_t)b * p.ldt + j]);
+            return k < n_prefix ? p.prefix_pages[j] : p.table[(int64_t)b * p.ldt + j];
         };
-        auto fetch = [&](int k, uint32_t page) {
+        auto fetch = [&](int k, int page) {
             int last;
             const int j = token(k, last);
             const uint8_t* run = run_of<D>(p, page, h, j);
-            uint8_t* dst = lds + (k & 1) * 2 * TILE;
+            const uint32_t dst = lds_at(lds) + (k & 1) * 2 * TILE;
             fetch16<D>(run, wave, last, dst, lane);
             fetch16<D>(run + to_v, wave, last, dst + TILE, lane);
         };
-        uint32_t page = 0;
+        int page = 0;
         if (k0 < k1) {
             fetch(k0, page_of(k0));
             if (k0 + 1 < k1) page = page_of(k0 + 1);
         }
-        for (int k = k0; k < k1; ++k) {
+        auto next = [&](int k) {
             wait_vmcnt<0>();
             __syncthreads();  // everyone's part of block k is there, and everyone is done with block k - 1
             if (k + 1 < k1) {
                 fetch(k + 1, page);
                 if (k + 2 < k1) page = page_of(k + 2);
             }
-            const uint32_t buffer = lds_at(lds) + (k & 1) * 2 * TILE;
-            if (wave * 32 < rows) {
+        };
+        if (wave * 32 < rows) {
+            for (int k = k0; k < k1; ++k) {
+                next(k);
+                const uint32_t buffer = lds_at(lds) + (k & 1) * 2 * TILE;
                 const bool pre = k < n_prefix;
                 const int j0 = (pre ? k + first_block : k - n_prefix) * 64;
                 v16f s[2];
                 scores<D, 2>(s, q, buffer + kl);
-                if (j0 + 64 > (pre ? p.P : clear_to)) weigh<D, 2, true>(st, s, lane, p.c, (pre ? p.P : seen) - j0);
-                else weigh<D, 2, false>(st, s, lane, p.c, 0);
-                gather<D, 2>(st, s, buffer + TILE + vl);
+                Values<D> f;  // on their way while the weights are made
+                read_values<D>(f, buffer + TILE + vl, 0);
+                if (j0 + 64 > (pre ? p.P : clear_to)) mask<2>(s, lane, (pre ? p.P : seen) - j0);
+                weigh<D, 2>(st, s, p.c);
+                gather<D, 2>(st, s, f, buffer + TILE + vl);
             }
+        } else {
+            for (int k = k0; k < k1; ++k) next(k);
         }
         st.sum = half_sum(st.sum);
         const bool direct = whole && b >= 0;
@@ -703,7 +704,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
                 if (hi == 0) *reinterpret_cast<float2*>(blk + (32 * D + row * 2) * 4) = make_float2(st.base, st.sum);
             }
         }
-        __syncthreads();  // the next item's first block lands where others may still be reading this one's last
+        lds_barrier();  // the next item's first block lands where others may still be reading this one's last
     }
 }
 
@@ -838,10 +839,10 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         packed0 = rec[2] + r;
         if (p.P) {
             if (plan.tiles) {
-                spread_pre = (int)((plan.super * 64 - 1) / plan.wide_per) + 2;
+                spread_pre = (int)((plan.super * 64 + WIDE_EDGE - 1) / plan.wide_per) + 2;
                 more = plan.supers * spread_pre;
             } else {
-                const int cp = (p.P + 31) >> 5;
+                const int cp = narrow_length(p.P);
                 more = (int)(((int64_t)(h + 1) * cp - 1) / plan.narrow_per - (int64_t)h * cp / plan.narrow_per) + 1;
             }
         }
@@ -855,14 +856,15 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         j -= own;
         if (j >= more) return -1;
         if (!plan.tiles) {
-            const int64_t blk = h + (int64_t)h * ((p.P + 31) >> 5) / plan.narrow_per + j;
+            const int64_t blk = h + (int64_t)h * narrow_length(p.P) / plan.narrow_per + j;
             row = (int)packed0 & 31;
             return blk < p.narrow_blocks ? p.joint_blocks + p.packed_blocks + blk : -1;
         }
         const int s = j / spread_pre, k = j - s * spread_pre, pt = (int)(packed0 / WROWS), blocks = min(plan.super, plan.nbp - s * plan.super);
-        const int64_t a = (int64_t)h * plan.tiles * plan.nbp * 64 + (int64_t)s * plan.tiles * plan.super * 64 + (int64_t)pt * blocks * 64;
+        const int length = blocks * 64 + WIDE_EDGE;
+        const int64_t a = h * plan.head + (int64_t)s * plan.tiles * (plan.super * 64 + WIDE_EDGE) + (int64_t)pt * length;
         const int64_t w = a / plan.wide_per + k;
-        if (w > (a + blocks * 64 - 1) / plan.wide_per) return -1;
+        if (w > (a + length - 1) / plan.wide_per) return -1;
         row = (int)packed0 & 31;
         const int64_t blk = ((int64_t)(h * plan.supers + s) * plan.tiles + pt + w) * 4;
         return blk + 4 <= p.packed_blocks ? p.joint_blocks + blk + ((packed0 % WROWS) >> 5) : -1;
