@@ -661,9 +661,14 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
                 if (k + 2 < k1) page = page_of(k + 2);
             }
         };
+        // A CU's older wavefronts go first when both want the same unit, and its older workgroup would end long before the
+        // younger: they take turns block by block.
+        const int turn = blockIdx.x >= attn_wgs<D>() / 2;
         if (wave * 32 < rows) {
             for (int k = k0; k < k1; ++k) {
                 next(k);
+                if ((k ^ turn) & 1) __builtin_amdgcn_s_setprio(1);
+                else __builtin_amdgcn_s_setprio(0);
                 const uint32_t buffer = lds_at(lds) + (k & 1) * 2 * TILE;
                 const bool pre = k < n_prefix;
                 const int j0 = (pre ? k + first_block : k - n_prefix) * 64;
@@ -675,6 +680,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
                 weigh<D, 2>(st, s, p.c);
                 gather<D, 2>(st, s, f, buffer + TILE + vl);
             }
+            __builtin_amdgcn_s_setprio(0);
         } else {
             for (int k = k0; k < k1; ++k) next(k);
         }
@@ -773,6 +779,7 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
         return i < run ? xcd * run + i : -1;
     };
     const bool swap = blockIdx.x >= attn_wgs<D>() / 2;
+
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
         if ((turn == 0) == swap) {
@@ -786,16 +793,18 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
 }
 
 // ---- the segments of a row, joined ------------------------------------------------------------------------------------------------
-// D/4 lanes a row, four channels each.  A lane first reads base and weight of one segment, so up to D/4 of them arrive together.
-template <int D>
+// A wavefront joins H = 1 or 4 rows (heads) of a token.  First 64 / H lanes a row find one segment each and read its base and
+// weight; then D/4 lanes hold four channels each of a row's sums: all groups of lanes share one row's segments (H = 1: few
+// rows, of many segments), or have rows of their own (H = 4: more rows than the card holds wavefronts).
+template <int D, int H>
 __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnArgs p) {
-    constexpr int LANES = D / 4, RPW = 64 / LANES;
-    const int lane = threadIdx.x & 63, sub = lane / LANES, l = lane % LANES;
-    const int per_token = (p.Hq + RPW - 1) / RPW;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    constexpr int LANES = D / 4, GRP = 64 / LANES, S = 64 / H, ROWS = H == 1 ? 1 : H / GRP, STEP = H == 1 ? GRP : 1;
+    const int lane = threadIdx.x & 63, sub = lane / LANES, l = lane % LANES, jl = lane % S;
+    const int per_token = (p.Hq + H - 1) / H;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + uni((int)(threadIdx.x >> 6));
     const int t = (int)(unit / per_token);
     if (t >= p.T) return;
-    const int head = (int)(unit - (int64_t)t * per_token) * RPW + sub;
+    const int head0 = (int)(unit - (int64_t)t * per_token) * H;
     int lo = 0, hi = p.B + 1;  // the last request that starts at or before t
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64, at = lo + lane * step;
@@ -804,106 +813,125 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         lo += (n - 1) * step;
         hi = min(hi, lo + step);
     }
-    const int b = lo;
-    if (b >= p.B || head >= p.Hq) return;
+    const int b = uni(lo);
+    if (b >= p.B) return;
     const Request rq = request(p, b);
     const int i = t - rq.q0;
     if (i < 0 || i >= rq.n) return;
-    const Plan& plan = *p.plan;
+    const Plan plan = *p.plan;
     const int64_t* rec = p.records + (int64_t)b * 4;
-    const int h = head / p.G, g = head - h * p.G, r = i * p.G + g;
-
-    // `count` segments at most; segment j's block and the row in it, or no block
-    int64_t s0, s1, first, packed0 = 0;
-    int own, more = 0, tile = 0, at_row, spread_pre = 0;
     const bool joint = is_long(p, rq.n);
+    const int cp = narrow_length(p.P);
+    const int pre_pieces = plan.tiles ? (int)((plan.super * 64 + WIDE_EDGE - 1) / plan.wide_per) + 2 : 0;  // of a piece of the prefix, at most
+
+    // this lane's row: `own` segments of its request's tile, the first at `first`; then up to `more` of the prefix
+    const int head = min(head0 + lane / S, p.Hq - 1), h = head / p.G, r = i * p.G + head - h * p.G;
+    const int64_t packed = rec[2] + r;
+    int64_t first;
+    int own, more = 0, row;
     if (joint) {
         const int64_t seen = wide_seen(p, rq);
-        tile = i / p.tpt;
-        s0 = plan.wide0 + rec[3] + h * wide_sum(p, seen, wide_tiles(p, rq.n)) + wide_sum(p, seen, tile);
-        s1 = s0 + seen + (int64_t)(tile + 1) * p.tpt;
+        const int tile = i / p.tpt;
+        const int64_t s0 = plan.wide0 + rec[3] + h * wide_sum(p, seen, wide_tiles(p, rq.n)) + wide_sum(p, seen, tile);
         first = s0 / plan.wide_per;
-        own = (int)((s1 - 1) / plan.wide_per - first) + 1;
-        if (own == 1) return;  // written by the first kernel
-        at_row = r - tile * p.tpt * p.G;
+        own = (int)((s0 + seen + (int64_t)(tile + 1) * p.tpt - 1) / plan.wide_per - first) + 1;
+        row = r - tile * p.tpt * p.G;
     } else {
         const int length = narrow_length(rq.L);
-        const int64_t k = (int64_t)h * narrow_tiles(p, rq.n) + r / 32;
-        s0 = plan.narrow0 + rec[0] + k * length;
-        s1 = s0 + length;
+        const int64_t k = (int64_t)h * narrow_tiles(p, rq.n) + r / 32, s0 = plan.narrow0 + rec[0] + k * length;
         first = s0 / plan.narrow_per;
-        own = (int)((s1 - 1) / plan.narrow_per - first) + 1;
-        if (own == 1 && p.P == 0) return;
-        at_row = r & 31;
+        own = (int)((s0 + length - 1) / plan.narrow_per - first) + 1;
+        row = r & 31;
         first += plan.items0 + rec[1] + k;  // its block in the narrow part
-        packed0 = rec[2] + r;
-        if (p.P) {
-            if (plan.tiles) {
-                spread_pre = (int)((plan.super * 64 + WIDE_EDGE - 1) / plan.wide_per) + 2;
-                more = plan.supers * spread_pre;
-            } else {
-                const int cp = narrow_length(p.P);
-                more = (int)(((int64_t)(h + 1) * cp - 1) / plan.narrow_per - (int64_t)h * cp / plan.narrow_per) + 1;
-            }
-        }
+        if (p.P) more = plan.tiles ? plan.supers * pre_pieces : (int)(((int64_t)(h + 1) * cp - 1) / plan.narrow_per - (int64_t)h * cp / plan.narrow_per) + 1;
     }
-    auto block_of = [&](int j, int& row) -> int64_t {
+    const bool done = own == 1 && more == 0 && (joint || p.P == 0);  // written by the first kernel
+    const int count = done ? 0 : own + more;
+    int most = count;
+#pragma unroll
+    for (int d = S; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
+    most = uni(most);
+    // segment j's place, or -1 where there is none
+    auto place = [&](int j, int& at_row) -> int64_t {
+        at_row = row & 31;
+        if (j >= count) return -1;
         if (j < own) {
-            row = at_row & 31;
-            if (joint) return (2 * (first + j) + (j == 0)) * 4 + (at_row >> 5);
+            if (joint) return (2 * (first + j) + (j == 0)) * 4 + (row >> 5);
             return first + j < p.narrow_blocks ? p.joint_blocks + p.packed_blocks + first + j : -1;
         }
         j -= own;
-        if (j >= more) return -1;
+        at_row = (int)packed & 31;
         if (!plan.tiles) {
-            const int64_t blk = h + (int64_t)h * narrow_length(p.P) / plan.narrow_per + j;
-            row = (int)packed0 & 31;
+            const int64_t blk = h + (int64_t)h * cp / plan.narrow_per + j;
             return blk < p.narrow_blocks ? p.joint_blocks + p.packed_blocks + blk : -1;
         }
-        const int s = j / spread_pre, k = j - s * spread_pre, pt = (int)(packed0 / WROWS), blocks = min(plan.super, plan.nbp - s * plan.super);
-        const int length = blocks * 64 + WIDE_EDGE;
-        const int64_t a = h * plan.head + (int64_t)s * plan.tiles * (plan.super * 64 + WIDE_EDGE) + (int64_t)pt * length;
-        const int64_t w = a / plan.wide_per + k;
-        if (w > (a + length - 1) / plan.wide_per) return -1;
-        row = (int)packed0 & 31;
+        const int s = j / pre_pieces, pt = (int)(packed / WROWS), len = min(plan.super, plan.nbp - s * plan.super) * 64 + WIDE_EDGE;
+        const int64_t a = h * plan.head + (int64_t)s * plan.tiles * (plan.super * 64 + WIDE_EDGE) + (int64_t)pt * len;
+        const int64_t w = a / plan.wide_per + j - s * pre_pieces;
+        if (w > (a + len - 1) / plan.wide_per) return -1;
         const int64_t blk = ((int64_t)(h * plan.supers + s) * plan.tiles + pt + w) * 4;
-        return blk + 4 <= p.packed_blocks ? p.joint_blocks + blk + ((packed0 % WROWS) >> 5) : -1;
+        return blk + 4 <= p.packed_blocks ? p.joint_blocks + blk + ((packed % WROWS) >> 5) : -1;
     };
     float base = -INFINITY, sum = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    const int count = own + more;
-    for (int j0 = 0; j0 < count; j0 += LANES) {
-        int row = 0;
-        const int64_t blk = block_of(j0 + l, row);
-        float bs = -INFINITY, wt = 0.0f;
-        const uint8_t* at = p.blocks + (blk < 0 ? 0 : blk) * block_bytes<D>();
-        if (blk >= 0) {
-            const float2 z = *reinterpret_cast<const float2*>(at + (32 * D + row * 2) * 4);
-            bs = z.x, wt = z.y;
-        }
+    float4 acc[ROWS];
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) acc[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int j0 = 0; j0 < most; j0 += S) {
+        int at_row = 0;
+        const int64_t blk = place(j0 + jl, at_row), at = blk < 0 ? 0 : blk * block_bytes<D>();
+        const float2 z = *reinterpret_cast<const float2*>(p.blocks + at + (32 * D + at_row * 2) * 4);
+        const float bs = blk < 0 ? -INFINITY : z.x, wt = blk < 0 ? 0.0f : z.y;
         float top = bs;
 #pragma unroll
-        for (int d = 1; d < LANES; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        for (int d = 1; d < S; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
         const float next = fmaxf(base, top), fade = next == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(base - next);
-        acc.x *= fade, acc.y *= fade, acc.z *= fade, acc.w *= fade;
-        sum *= fade;
+        const float f = wt > 0.0f ? __builtin_amdgcn_exp2f(bs - next) : 0.0f;
         base = next;
-        const float f = wt > 0.0f ? __builtin_amdgcn_exp2f(bs - base) : 0.0f;  // a segment without weight may not have left sums
-        const int64_t off = (at - p.blocks) + row * D * 4;
-        const int m = min(LANES, count - j0);
-        for (int j = 0; j < m; ++j) {
-            const float fj = __shfl(f, sub * LANES + j), wj = __shfl(wt, sub * LANES + j);
-            const int64_t oj = __shfl(off, sub * LANES + j);
-            if (fj > 0.0f) {
-                const float4 z = *reinterpret_cast<const float4*>(p.blocks + oj + l * 16);
-                acc.x = fmaf(fj, z.x, acc.x), acc.y = fmaf(fj, z.y, acc.y), acc.z = fmaf(fj, z.z, acc.z), acc.w = fmaf(fj, z.w, acc.w);
-                sum = fmaf(fj, wj, sum);
+        sum = fmaf(f, wt, sum * fade);
+        const int64_t off = at + at_row * D * 4;
+        const int m = min(S, most - j0);
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+            const int lane0 = H == 1 ? 0 : (sub * ROWS + q) * S;
+            const float fd = __shfl(fade, lane0);
+            acc[q].x *= fd, acc[q].y *= fd, acc[q].z *= fd, acc[q].w *= fd;
+            for (int j = 0; j < m; j += 4 * STEP) {  // four loads of a lane on their way
+                float4 y[4];
+                float fy[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int at_j = j + k * STEP + (H == 1 ? sub : 0), from = lane0 + min(at_j, S - 1);
+                    const float g = __shfl(f, from);
+                    fy[k] = at_j < m ? g : 0.0f;
+                    y[k] = *reinterpret_cast<const float4*>(p.blocks + __shfl(off, from) + l * 16);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {  // a segment without weight may not have left sums
+                    const bool has = fy[k] > 0.0f;
+                    acc[q].x = has ? fmaf(fy[k], y[k].x, acc[q].x) : acc[q].x, acc[q].y = has ? fmaf(fy[k], y[k].y, acc[q].y) : acc[q].y;
+                    acc[q].z = has ? fmaf(fy[k], y[k].z, acc[q].z) : acc[q].z, acc[q].w = has ? fmaf(fy[k], y[k].w, acc[q].w) : acc[q].w;
+                }
             }
         }
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    *reinterpret_cast<uint2*>(p.O + (int64_t)t * p.ldo + head * D + l * 4) = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
-    if (p.lse && l == 0) p.lse[(int64_t)t * p.Hq + head] = lse_of(base, sum);
+#pragma unroll
+    for (int d = 1; d < S; d <<= 1) sum += __shfl_xor(sum, d);
+    if (H == 1) {
+#pragma unroll
+        for (int d = LANES; d < 64; d <<= 1)
+            acc[0].x += __shfl_xor(acc[0].x, d), acc[0].y += __shfl_xor(acc[0].y, d), acc[0].z += __shfl_xor(acc[0].z, d), acc[0].w += __shfl_xor(acc[0].w, d);
+    }
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) {
+        const int u = H == 1 ? 0 : sub * ROWS + q;
+        const float total = __shfl(sum, u * S);
+        const bool write = __shfl((int)done, u * S) == 0 && head0 + u < p.Hq && (H != 1 || sub == 0);
+        const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+        if (write)
+            *reinterpret_cast<uint2*>(p.O + (int64_t)t * p.ldo + (head0 + u) * D + l * 4) =
+                make_uint2(pack2(acc[q].x * inv, acc[q].y * inv), pack2(acc[q].z * inv, acc[q].w * inv));
+    }
+    if (p.lse && jl == 0 && !done && head0 + lane / S < p.Hq) p.lse[(int64_t)t * p.Hq + head] = lse_of(base, sum);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------------
@@ -935,10 +963,12 @@ static int launch(const AttnArgs& p, hipStream_t st) {
     constexpr size_t lds = 8 * 32 * D * 2 + sizeof(AttnShared);
     const int rc = reserve_lds((const void*)prefix_attention_kernel<D>, lds, r);
     if (rc) return rc;
-    constexpr int rows = 64 / (D / 4);
-    const int64_t waves = p.T * ((p.Hq + rows - 1) / rows), wgs = (waves + 3) / 4;
     prefix_attention_kernel<D><<<dim3(attn_wgs<D>()), WG, lds, st>>>(p);
-    prefix_attention_join_kernel<D><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
+    // a wavefront a row while the card holds them at once, four rows beyond that
+    const bool few = p.T * p.Hq <= 8192;
+    const int64_t wgs = (p.T * (few ? p.Hq : (p.Hq + 3) / 4) + 3) / 4;
+    if (few) prefix_attention_join_kernel<D, 1><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
+    else prefix_attention_join_kernel<D, 4><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
     return check_launch("osc_prefix_attention");
 }
 

@@ -283,6 +283,15 @@ def test_attention_prompts(osc):
     check_attention(osc, make(14, 3, 0, [333, 1, 700], [333, 1, 200], 5, 1, 64, 32))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_many_rows(osc, D):
+    """more rows than are joined one a wavefront: few segments each, and many (a short prefix and a long one)"""
+    n = [1] * 150 + [60, 130]
+    kv = [b % 37 for b in range(150)] + [75, 200]
+    check_attention(osc, make(17, 152, 20, kv, n, 30, 5, D, 16))
+    check_attention(osc, make(18, 152, 700, kv, n, 30, 5, D, 16))
+
+
 def test_attention_many_heads_a_key_head(osc):
     check_attention(osc, make(15, 3, 70, [40, 3, 100], [3, 1, 2], 128, 1, 64, 16))
     check_attention(osc, make(16, 3, 0, [40, 3, 100], [3, 1, 2], 100, 1, 128, 16))
