@@ -30,9 +30,11 @@ constexpr int WG = 256, WROWS = 128, GROUPS = 256;
 // Workgroups: two on a CU (LDS for their tiles), three where heads are small.
 template <int D>
 constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
-// The smallest pieces of the two lines
-constexpr int MIN_NARROW = 1, MIN_WIDE = 512, WIDE_EDGE = 128;
+// The line of 32-row tiles is measured in tiles of 32 tokens, that of 128-row tiles in tokens.  Starting and ending a segment costs
+// about as much as the EDGEs; no piece is smaller than the MINs.
+constexpr int NARROW_EDGE = 4, MIN_NARROW = 8, WIDE_EDGE = 128, MIN_WIDE = 512;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
+constexpr int LONG_PREFIX = 256, LONG = 33;  // rows of a long request, with a prefix and without
 
 struct AttnArgs {
     const uint16_t* Q;
@@ -48,6 +50,7 @@ struct AttnArgs {
     int max_kv;  // tokens that a row of the table can name
     const int32_t *kv_lens, *q_offsets;
     int B, per;  // per: requests of a group
+    int ns, ws;  // a step on the line of 32-row (128-row) tiles is 2^ns (2^ws) of its units: 0 unless the lines could pass 2^30
     float c;     // scale * log2(e): scores leave the matrix core unscaled, and powers are of two
     uint16_t* O;
     int64_t ldo;
@@ -55,7 +58,7 @@ struct AttnArgs {
     // workspace: the plan, one record a request, segments in blocks of 32 rows: of long requests (two places a workgroup), of packed
     // tiles, of short requests
     struct Plan* plan;
-    int64_t* records;
+    int* records;
     uint8_t* blocks;
     int64_t joint_blocks, packed_blocks, narrow_blocks;
 };
@@ -63,99 +66,118 @@ template <int D>
 constexpr int block_bytes() { return 32 * (D + 2) * 4; }  // [32][D] sums, [32] base and weight
 
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int64_t uni(int64_t v) {
-    return (int64_t)((uint64_t)(uint32_t)uni((int)(v >> 32)) << 32 | (uint32_t)uni((int)v));
-}
 
 // ---- where things are on the two lines -----------------------------------------------------------------------------------
 struct Request {
     int q0, n, L;
 };
 struct Extent {  // of one request, or of all before one
-    int64_t narrow, items, rows, wide;
+    int narrow, items, rows, wide;
 };
 __device__ __forceinline__ Request request(const AttnArgs& p, int b) {
     Request r;
-    const int T = (int)p.T;
-    r.q0 = min(max(p.q_offsets[b], 0), T);
-    r.n = max(min(p.q_offsets[b + 1], T) - r.q0, 0);
+    r.q0 = p.q_offsets[b];  // checked before anything is looked up
+    r.n = p.q_offsets[b + 1] - r.q0;
     r.L = min(max(p.kv_lens[b], 0), p.max_kv);
     return r;
 }
-__device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? 256 : 33); }
+__device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? LONG_PREFIX : LONG); }
 __device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (n * p.G + 31) >> 5; }
-// The line of 32-row tiles is measured in 128 tokens (a tile a wavefront), and starting and ending a segment costs about half of that
-__device__ __forceinline__ int narrow_length(int L) { return (L + 191) >> 7; }
-__device__ __forceinline__ int narrow_tile(int64_t y) { return max(0, (int)(4 * y) - 2); }  // where place y of an item is, in tiles of 32
-// tokens that the first k tiles of a long request walk: each sees `seen` and tpt more than the one before it
-__device__ __forceinline__ int64_t wide_sum(const AttnArgs& p, int64_t seen, int64_t k) { return k * seen + p.tpt * (k * (k + 1) / 2); }
-// and what starting and ending a segment costs, as tokens
-__device__ __forceinline__ int64_t wide_seen(const AttnArgs& p, const Request& r) { return WIDE_EDGE + p.P + max(r.L - r.n, 0); }
+__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, bool aligned) {
+    const int n = (((L + 31) >> 5) + NARROW_EDGE + (1 << p.ns) - 1) >> p.ns;
+    return aligned ? (n + MIN_NARROW - 1) / MIN_NARROW * MIN_NARROW : n;
+}
+__device__ __forceinline__ int narrow_tile(const AttnArgs& p, int y) { return max(0, (y << p.ns) - NARROW_EDGE); }  // the first tile at place y of an item
+// the first k tiles of a long request on their line: each sees `seen` and a tile's tokens more than the one before it
+__device__ __forceinline__ int wide_sum(const AttnArgs& p, int seen, int k) { return k * seen + (p.tpt >> p.ws) * (k * (k + 1) / 2); }
+__device__ __forceinline__ int wide_seen(const AttnArgs& p, const Request& r) { return ((WIDE_EDGE + p.P + max(r.L - r.n, 0)) >> p.ws) + 1; }
+__device__ __forceinline__ int wide_length(const AttnArgs& p, int seen, int tile) { return seen + (tile + 1) * (p.tpt >> p.ws); }
 __device__ __forceinline__ int wide_tiles(const AttnArgs& p, int n) { return (n + p.tpt - 1) / p.tpt; }
-__device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r) {
+__device__ __forceinline__ int packed_length(const AttnArgs& p, int blocks) { return ((blocks * 64 + WIDE_EDGE) >> p.ws) + 1; }
+__device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, bool aligned) {
     Extent e{0, 0, 0, 0};
     if (r.n == 0) return e;
     if (is_long(p, r.n)) {
         e.wide = p.Hkv * wide_sum(p, wide_seen(p, r), wide_tiles(p, r.n));
     } else {
-        e.items = (int64_t)narrow_tiles(p, r.n) * p.Hkv;
-        e.narrow = e.items * narrow_length(r.L);
+        e.items = narrow_tiles(p, r.n) * p.Hkv;
+        e.narrow = e.items * narrow_length(p, r.L, aligned);
         if (p.P) e.rows = r.n * p.G;
     }
     return e;
 }
 
-// What follows from the totals: the packed tiles at the start of their line, and the pieces' lengths.
+// What follows from the totals: the prefix's items, which come first on their line, and the pieces.
+// Wide pieces are equal; the first `with_wide` workgroups have one.  These take narrow pieces of length `a`, the others of length
+// `b`, so that all have the same to do: a wide block of 64 tokens takes about as long as 5/4 narrow tiles (1.9 us where a CU
+// has two workgroups at it, a narrow tile 1.5 us of HBM).  Where there are more workgroups than pieces of the least length,
+// items are rounded up to whole pieces (`aligned`): none is cut, and no workgroup has two.
 struct Plan {
-    int64_t narrow, wide;        // lengths of the lines
-    int64_t narrow0, items0;     // of which the prefix's narrow items are the first
-    int64_t wide0, head;         // of which the packed tiles are the first, `head` for every key/value head
-    int64_t narrow_per, wide_per;
-    int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; blocks of 64 tokens: of a piece of the prefix, of the prefix
+    int narrow, wide;      // lengths of the lines
+    int narrow0, items0;   // of which the prefix's narrow items are the first
+    int wide0, head;       // of which the packed tiles are the first, `head` for every key/value head
+    int wide_per, a, b, cut;
+    int with_wide, aligned;
+    int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; pieces of the prefix, blocks of 64 tokens in one, in the prefix
+    int valid;  // offsets are in order
 };
-// The prefix's blocks are cut into pieces that stay in an XCD's L2 while all packed tiles walk them.
+// Many packed tiles walk the prefix in pieces that stay in an XCD's L2 meanwhile.
 __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
     const int64_t n = (P + SUPER - 1) / SUPER;
     return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
 }
 template <int D>
-__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int64_t narrow, int64_t rows, int64_t wide) {
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rounded, int rows, int wide) {
+    constexpr int N = attn_wgs<D>();
     Plan a;
-    a.rows = (int)min(rows, p.T * p.G);
+    a.valid = 1;
+    a.rows = rows;
     a.nbp = (p.P + 63) >> 6;
     a.narrow0 = a.items0 = a.wide0 = a.head = 0;
     a.tiles = a.supers = a.super = 0;
-    if (a.rows > 32) {
-        a.tiles = (a.rows + WROWS - 1) / WROWS;
-        a.supers = super_count(p.P, a.tiles);
+    const bool narrow_prefix = rows > 0 && rows <= 32;
+    if (narrow_prefix) rounded += p.Hkv * narrow_length(p, p.P, true);
+    a.aligned = rounded <= N * MIN_NARROW;
+    if (a.aligned) narrow = rounded;
+    if (narrow_prefix) {
+        a.items0 = p.Hkv;
+        a.narrow0 = p.Hkv * narrow_length(p, p.P, a.aligned);
+        if (!a.aligned) narrow += a.narrow0;
+    }
+    a.wide_per = 0;
+    if (rows > 32) {
+        a.tiles = (rows + WROWS - 1) / WROWS;
+        const int th = p.Hkv * a.tiles;
+        const bool whole = wide == 0 && th <= N;  // nothing else on the line: an item a piece, in one round
+        a.supers = whole ? max(1, min(N / th, a.nbp * 64 / MIN_WIDE)) : super_count(p.P, a.tiles);
         a.super = (a.nbp + a.supers - 1) / a.supers;
         a.supers = (a.nbp + a.super - 1) / a.super;
-        a.head = (int64_t)a.tiles * (a.nbp * 64 + a.supers * WIDE_EDGE);
+        a.head = a.tiles * a.supers * packed_length(p, a.super);
         a.wide0 = p.Hkv * a.head;
-    } else if (a.rows > 0) {
-        a.items0 = p.Hkv;
-        a.narrow0 = (int64_t)p.Hkv * narrow_length(p.P);
+        if (whole) a.wide_per = packed_length(p, a.super);
     }
-    a.narrow = a.narrow0 + narrow;
+    a.narrow = narrow;
     a.wide = a.wide0 + wide;
-    constexpr int N = attn_wgs<D>();
-    a.narrow_per = max((a.narrow + N - 1) / N, (int64_t)MIN_NARROW);
-    a.wide_per = max((a.wide + N - 1) / N, (int64_t)MIN_WIDE);
+    if (!a.wide_per) a.wide_per = max((a.wide + N - 1) / N, max(MIN_WIDE >> p.ws, 1));
+    a.with_wide = ((a.wide + a.wide_per - 1) / a.wide_per + 7) / 8 * 8;  // as many on every XCD
+    const int others = N - a.with_wide, cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 4)) >> p.ns, (int64_t)1 << 20);
+    a.b = (narrow + N - 1) / N + (a.with_wide * cost + N - 1) / N;
+    a.a = a.b - cost;
+    if (others == 0) a.a = max((narrow + N - 1) / N, MIN_NARROW);
+    else if (a.aligned) a.b = MIN_NARROW, a.a = others * MIN_NARROW >= narrow ? 0 : MIN_NARROW;
+    else if (a.a < MIN_NARROW) a.a = 0, a.b = max((narrow + others - 1) / others, MIN_NARROW);
+    a.cut = a.a * a.with_wide;
     return a;
 }
-
-// what all lanes read from LDS, as the scalars that it is
-__device__ __forceinline__ Plan uni(const Plan& a) {
-    return Plan{uni(a.narrow), uni(a.wide), uni(a.narrow0), uni(a.items0), uni(a.wide0), uni(a.head), uni(a.narrow_per), uni(a.wide_per),
-                uni(a.rows), uni(a.tiles), uni(a.supers), uni(a.super), uni(a.nbp)};
-}
+// the workgroup (in the order of the pieces) that has place x of the narrow line
+__device__ __forceinline__ int narrow_piece_of(const Plan& a, int x) { return x < a.cut ? x / a.a : a.with_wide + (x - a.cut) / a.b; }
 
 // Running sums over groups of `per` requests, in LDS: what a place on a line or a packed row is searched in.
 struct Sums {
-    int64_t narrow[GROUPS], items[GROUPS], rows[GROUPS], wide[GROUPS];
+    int narrow[GROUPS], items[GROUPS], rows[GROUPS], wide[GROUPS];
 };
 // the last group whose sum does not exceed x (x below the total)
-__device__ __forceinline__ int find_group(const int64_t (&sums)[GROUPS], int64_t x, int lane) {
+__device__ __forceinline__ int find_group(const int (&sums)[GROUPS], int x, int lane) {
     int n = 0;
 #pragma unroll
     for (int k = 0; k < GROUPS / 64; ++k) n += __popcll(__ballot(sums[k * 64 + lane] <= x));
@@ -163,20 +185,20 @@ __device__ __forceinline__ int find_group(const int64_t (&sums)[GROUPS], int64_t
 }
 // The request that holds place x of a line: its number and what is before it.  All lanes of a wavefront take part.
 template <bool WIDE>
-__device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, int64_t x, int lane, Extent& before) {
+__device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, bool aligned, int x, int lane, Extent& before) {
     const int g = uni(find_group(WIDE ? s.wide : s.narrow, x, lane));
     before = Extent{uni(s.narrow[g]), uni(s.items[g]), uni(s.rows[g]), uni(s.wide[g])};
     int b = g * p.per;
     if (p.per > 1) {  // at most 32 requests of a group: one a lane
         Extent e{0, 0, 0, 0};
-        if (lane < p.per && b + lane < p.B) e = extent(p, request(p, b + lane));
+        if (lane < p.per && b + lane < p.B) e = extent(p, request(p, b + lane), aligned);
         Extent sum = e;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int64_t n = __shfl_up(sum.narrow, d), i = __shfl_up(sum.items, d), r = __shfl_up(sum.rows, d), w = __shfl_up(sum.wide, d);
+            const int n = __shfl_up(sum.narrow, d), i = __shfl_up(sum.items, d), r = __shfl_up(sum.rows, d), w = __shfl_up(sum.wide, d);
             if (lane >= d) sum.narrow += n, sum.items += i, sum.rows += r, sum.wide += w;
         }
-        const int64_t end = WIDE ? before.wide + sum.wide : before.narrow + sum.narrow;
+        const int end = WIDE ? before.wide + sum.wide : before.narrow + sum.narrow;
         const int k = uni(__ffsll((unsigned long long)__ballot(end > x)) - 1);  // lanes past the group repeat its end, which is above x
         before.narrow += uni(__shfl(sum.narrow - e.narrow, k));
         before.items += uni(__shfl(sum.items - e.items, k));
@@ -194,17 +216,17 @@ __device__ __forceinline__ void packed_row(const AttnArgs& p, const Sums& s, int
         if (s.rows[mid] <= r) lo = mid;
         else hi = mid;
     }
-    int64_t at = s.rows[lo];
+    int at = s.rows[lo];
     int b = lo * p.per;
     Request q = request(p, b);
     for (int last = min(p.B, b + p.per) - 1; b < last; q = request(p, ++b)) {
-        const int64_t n = extent(p, q).rows;
+        const int n = extent(p, q, false).rows;
         if (at + n > r) break;
         at += n;
     }
-    const int i = min((int)(r - at) / p.G, max(q.n - 1, 0));
-    t = min(q.q0 + i, (int)p.T - 1);
-    g = min((int)(r - at) - i * p.G, p.G - 1);
+    const int i = (r - at) / p.G;
+    t = q.q0 + i;
+    g = r - at - i * p.G;
 }
 
 __device__ __forceinline__ uint32_t lds_at(const uint8_t* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p; }
@@ -405,41 +427,40 @@ __device__ __forceinline__ void lds_barrier() {
 // asked for once this tile's scores are there, values once they are summed, so half a tile or more is on its way at any time and
 // no wavefront waits for another before the segment's end.
 template <int D>
-__device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_lds, const Sums& sums, uint8_t* lds, float* stats, int64_t w) {
-    const Plan plan = uni(in_lds);
+__device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, float* stats, int w) {
     constexpr int TILE = 32 * D * 2, NI = D / 16;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // what follows from it is made here, not kept in registers from the kernel's start
     const int lane = tid & 63, wave = uni(tid >> 6);
     const int64_t to_v = p.V - p.K;
     const uint32_t kt = lds_at(lds) + wave * 2 * TILE, vt = kt + TILE, kl = kt + key_lane<D>(lane), vl = vt + value_lane<D>(lane);
-    int64_t x = w * plan.narrow_per;
-    const int64_t end = min(x + plan.narrow_per, plan.narrow);
+    const bool with_wide = w < plan.with_wide;
+    int x = with_wide ? w * plan.a : plan.cut + (w - plan.with_wide) * plan.b;
+    const int end = min(x + (with_wide ? plan.a : plan.b), plan.narrow);
     while (x < end) {
         // the item at x: its start and length on the line, its rows, its tokens
-        int64_t start, item;
-        int length, h, r0, rows, tokens, seen = 0, clear_to, b = -1;
+        int start, item, length, h, r0, rows, tokens, seen = 0, clear_to, b = -1;
         Request rq{0, 0, 0};
         const int32_t* pages;
         if (x < plan.narrow0) {
-            length = narrow_length(p.P);
-            h = (int)(x / length);
-            start = (int64_t)h * length, item = h;
+            length = narrow_length(p, p.P, plan.aligned);
+            h = x / length;
+            start = h * length, item = h;
             r0 = 0, rows = plan.rows, tokens = p.P, clear_to = p.P, pages = p.prefix_pages;
         } else {
             Extent before;
-            b = find_request<false>(p, sums, x - plan.narrow0, lane, before);
+            b = find_request<false>(p, sums, plan.aligned, x - plan.narrow0, lane, before);
             rq = request(p, b);
-            length = narrow_length(rq.L);
-            const int nt = narrow_tiles(p, rq.n), k = (int)((x - plan.narrow0 - before.narrow) / length);
-            start = plan.narrow0 + before.narrow + (int64_t)k * length, item = plan.items0 + before.items + k;
+            length = narrow_length(p, rq.L, plan.aligned);
+            const int nt = narrow_tiles(p, rq.n), k = (x - plan.narrow0 - before.narrow) / length;
+            start = plan.narrow0 + before.narrow + k * length, item = plan.items0 + before.items + k;
             h = k / nt;
             r0 = (k - h * nt) * 32, rows = rq.n * p.G;
             tokens = max(0, rq.L - rq.n + min(r0 + 31, rows - 1) / p.G + 1), clear_to = rq.L - rq.n + r0 / p.G + 1;
             pages = p.table + (int64_t)b * p.ldt;
         }
-        const int64_t stop = min(end, start + length);
-        const int t0 = narrow_tile(x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(stop - start), (tokens + 31) >> 5);
+        const int stop = min(end, start + length);
+        const int t0 = narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), (tokens + 31) >> 5);
         const bool whole = x == start && stop == start + length;
         x = stop;
 
@@ -515,7 +536,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
         __syncthreads();
         const int row = tid >> 3, part = tid & 7;
         const bool direct = p.P == 0 && whole;
-        const int64_t slot = item + w;
+        const int slot = item + w;
         if (r0 + row < rows && (direct || slot < p.narrow_blocks)) {
             float base = -INFINITY, f[4], sum = 0.0f;
 #pragma unroll
@@ -556,39 +577,36 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& in_l
 // ---- a piece of the line of 128-row tiles -----------------------------------------------------------------------------------------
 // Every wavefront has 32 rows; all read the same 64 tokens from LDS, of which each has asked for 16, a block ahead.
 template <int D>
-__device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds, const Sums& sums, uint8_t* lds, int64_t w) {
-    const Plan plan = uni(in_lds);
+__device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, int w) {
     constexpr int TILE = 64 * D * 2;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // what follows from it is made here, not kept in registers from the kernel's start
     const int lane = tid & 63, wave = uni(tid >> 6);
     const int64_t to_v = p.V - p.K;
     const uint32_t kl = key_lane<D>(lane), vl = value_lane<D>(lane);
-    int64_t x = w * plan.wide_per;
-    const int64_t end = min(x + plan.wide_per, plan.wide);
+    int x = w * plan.wide_per;
+    const int end = min(x + plan.wide_per, plan.wide);
     while (x < end) {
-        int64_t start, length, slot;
-        int h, rows, n_prefix, n_own, b = -1, first_block = 0, own = 0, r0 = 0, t_base = 0;
+        int64_t slot;
+        int start, length, h, rows, n_prefix, n_own, b = -1, first_block = 0, own = 0, r0 = 0, t_base = 0;
         Request rq{0, 0, 0};
         if (x < plan.wide0) {
             // head, then piece of the prefix, then tile
-            const int64_t piece = (int64_t)plan.tiles * (plan.super * 64 + WIDE_EDGE);
-            h = (int)(x / plan.head);
-            const int64_t y = x - h * plan.head;
-            const int s = (int)(y / piece), blocks = min(plan.super, plan.nbp - s * plan.super);
-            length = blocks * 64 + WIDE_EDGE;
-            const int tile = (int)((y - s * piece) / length);
-            start = h * plan.head + s * piece + tile * length;
+            length = packed_length(p, plan.super);
+            h = x / plan.head;
+            const int y = x - h * plan.head, item = y / length, s = item / plan.tiles, tile = item - s * plan.tiles;
+            const int blocks = min(plan.super, plan.nbp - s * plan.super);
+            start = h * plan.head + item * length;
             r0 = tile * WROWS, rows = plan.rows - r0;
             first_block = s * plan.super, n_prefix = blocks, n_own = 0;
             slot = p.joint_blocks + ((int64_t)(h * plan.supers + s) * plan.tiles + tile + w) * 4;
         } else {
             Extent before;
-            b = find_request<true>(p, sums, x - plan.wide0, lane, before);
+            b = find_request<true>(p, sums, false, x - plan.wide0, lane, before);
             rq = request(p, b);
             const int nt = wide_tiles(p, rq.n);
-            const int64_t seen = wide_seen(p, rq), head = wide_sum(p, seen, nt), y = x - plan.wide0 - before.wide;
-            h = (int)(y / head);
+            const int seen = wide_seen(p, rq), head = wide_sum(p, seen, nt), y = x - plan.wide0 - before.wide;
+            h = y / head;
             int lo = 0, hi = nt;  // the last tile that starts at or before y
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -596,7 +614,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
                 else hi = mid;
             }
             start = plan.wide0 + before.wide + h * head + wide_sum(p, seen, lo);
-            length = seen + (int64_t)(lo + 1) * p.tpt;
+            length = wide_length(p, seen, lo);
             t_base = lo * p.tpt;
             const int tokens = min(p.tpt, rq.n - t_base);
             rows = tokens * p.G;
@@ -604,12 +622,16 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
             n_prefix = plan.nbp, n_own = (own + 63) >> 6;
             slot = 0;
         }
-        const int64_t stop = min(end, start + length);
+        const int stop = min(end, start + length);
         const int blocks = n_prefix + n_own;
-        auto block_at = [&](int64_t y) { return y >= length ? blocks : (int)(max(y - WIDE_EDGE, (int64_t)0) * blocks / (length - WIDE_EDGE)); };
+        constexpr int EDGE = WIDE_EDGE;
+        auto block_at = [&](int y) {  // the same for both workgroups at a cut, and not falling: all that is asked of it
+            const int edge = EDGE >> p.ws;
+            return y >= length ? blocks : min(blocks, (int)((float)max(y - edge, 0) * (float)blocks / (float)(length - edge)));
+        };
         const int k0 = block_at(x - start), k1 = block_at(stop - start);
         const bool whole = x == start && stop == start + length;
-        if (b >= 0) slot = (2 * w + (x == start)) * 4;
+        if (b >= 0) slot = (2 * (int64_t)w + (x == start)) * 4;
         x = stop;
 
         const int r = wave * 32 + (lane & 31), rc = min(r, rows - 1);
@@ -716,8 +738,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& in_lds
 
 struct AttnShared {
     Sums sums;
-    Plan plan;
-    int64_t part[4][4];
+    int part[4][5];
     float stats[256];
 };
 
@@ -726,32 +747,40 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     AttnShared& sh = *reinterpret_cast<AttnShared*>(lds + 8 * 32 * D * 2);  // behind the tiles, which start at 0
     Sums& sums = sh.sums;
-    Plan& plan = sh.plan;
     float* stats = sh.stats;
     auto& part = sh.part;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    Extent mine{0, 0, 0, 0};
+    const int T = (int)p.T;
+    constexpr int NV = 5;  // narrow, narrow rounded up, items, rows, wide
+    int mine[NV] = {0, 0, 0, 0, 0}, v[NV], total[NV];
+    bool wrong = false;
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
     for (int b = b0; b < b1; ++b) {
-        const Extent e = extent(p, request(p, b));
-        mine.narrow += e.narrow, mine.items += e.items, mine.rows += e.rows, mine.wide += e.wide;
+        const Request r = request(p, b);
+        wrong |= r.q0 < 0 || r.n < 0 || r.q0 > T - r.n;
+        if (wrong) break;
+        const Extent e = extent(p, r, false);
+        mine[0] += e.narrow, mine[1] += e.items * narrow_length(p, r.L, true), mine[2] += e.items, mine[3] += e.rows, mine[4] += e.wide;
     }
-    int64_t v[4] = {mine.narrow, mine.items, mine.rows, mine.wide}, total[4];
-    const int64_t own[4] = {mine.narrow, mine.items, mine.rows, mine.wide};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) v[k] = mine[k];
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t u = __shfl_up(v[k], d);
+        for (int k = 0; k < NV; ++k) {
+            const int u = __shfl_up(v[k], d);
             if (lane >= d) v[k] += u;
         }
     if (lane == 63)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) part[wave][k] = v[k];
-    __syncthreads();
+        for (int k = 0; k < NV; ++k) part[wave][k] = v[k];
+    if (__syncthreads_or(wrong)) {  // offsets that fall or name rows that are not there: nothing is read or written
+        if (blockIdx.x == 0 && tid == 0) p.plan->valid = 0;
+        return;
+    }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        v[k] -= own[k];
+    for (int k = 0; k < NV; ++k) {
+        v[k] -= mine[k];
         total[k] = 0;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -759,36 +788,31 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
             total[k] += part[u][k];
         }
     }
-    sums.narrow[tid] = v[0], sums.items[tid] = v[1], sums.rows[tid] = v[2], sums.wide[tid] = v[3];
+    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[3]), uni(total[4]));
+    const bool aligned = plan.aligned;
+    if (aligned) v[0] = v[1];
+    sums.narrow[tid] = v[0], sums.items[tid] = v[2], sums.rows[tid] = v[3], sums.wide[tid] = v[4];
     if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
-        if (tid == 0) *p.plan = make_plan<D>(p, total[0], total[2], total[3]);
+        if (tid == 0) *p.plan = plan;
         for (int b = b0; b < b1; ++b) {
-            const Extent e = extent(p, request(p, b));
-            int64_t* r = p.records + (int64_t)b * 4;
-            r[0] = v[0], r[1] = v[1], r[2] = v[2], r[3] = v[3];
-            v[0] += e.narrow, v[1] += e.items, v[2] += e.rows, v[3] += e.wide;
+            const Extent e = extent(p, request(p, b), aligned);
+            int* r = p.records + (int64_t)b * 4;
+            r[0] = v[0], r[1] = v[2], r[2] = v[3], r[3] = v[4];
+            v[0] += e.narrow, v[2] += e.items, v[3] += e.rows, v[4] += e.wide;
         }
     }
-    if (tid == 0) plan = make_plan<D>(p, total[0], total[2], total[3]);
     __syncthreads();
 
-    // Workgroups are dealt to the XCDs in turn: each XCD takes a run of pieces, whose items are neighbours and share keys and values.
-    const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
-    auto piece = [&](int64_t all, int64_t per) -> int64_t {
-        const int64_t used = (all + per - 1) / per, run = (used + 7) / 8;
-        return i < run ? xcd * run + i : -1;
-    };
-    const bool swap = blockIdx.x >= attn_wgs<D>() / 2;
-
+    // Workgroups are dealt to the XCDs in turn: each XCD takes a run of wide pieces, whose items are neighbours and share keys and
+    // values; narrow ones share nothing.
+    // Those that a CU gets second take their narrow piece first: the two lists are bound by different things.
+    constexpr int N = attn_wgs<D>();
+    const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3, run = plan.with_wide >> 3;
+    const bool with_wide = i < run, swap = blockIdx.x >= N / 2;
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
-        if ((turn == 0) == swap) {
-            const int64_t w = piece(uni(plan.narrow), uni(plan.narrow_per));
-            if (w >= 0) narrow_piece<D>(p, plan, sums, lds, stats, w);
-        } else {
-            const int64_t w = piece(uni(plan.wide), uni(plan.wide_per));
-            if (w >= 0) wide_piece<D>(p, plan, sums, lds, w);
-        }
+        if ((turn == 0) == swap) narrow_piece<D>(p, plan, sums, lds, stats, (int)blockIdx.x);
+        else if (with_wide) wide_piece<D>(p, plan, sums, lds, xcd * run + i);
     }
 }
 
@@ -815,35 +839,34 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
     }
     const int b = uni(lo);
     if (b >= p.B) return;
+    const Plan plan = *p.plan;
+    if (!plan.valid) return;
     const Request rq = request(p, b);
     const int i = t - rq.q0;
     if (i < 0 || i >= rq.n) return;
-    const Plan plan = *p.plan;
-    const int64_t* rec = p.records + (int64_t)b * 4;
+    const int* rec = p.records + (int64_t)b * 4;
     const bool joint = is_long(p, rq.n);
-    const int cp = narrow_length(p.P);
-    const int pre_pieces = plan.tiles ? (int)((plan.super * 64 + WIDE_EDGE - 1) / plan.wide_per) + 2 : 0;  // of a piece of the prefix, at most
+    const int cp = narrow_length(p, p.P, plan.aligned), packed_item = packed_length(p, plan.super);
+    const int pre_pieces = packed_item == plan.wide_per ? 1 : plan.tiles ? (packed_item - 1) / plan.wide_per + 2 : 0;  // of a piece of the prefix, at most
 
     // this lane's row: `own` segments of its request's tile, the first at `first`; then up to `more` of the prefix
     const int head = min(head0 + lane / S, p.Hq - 1), h = head / p.G, r = i * p.G + head - h * p.G;
-    const int64_t packed = rec[2] + r;
-    int64_t first;
-    int own, more = 0, row;
+    const int packed = rec[2] + r;
+    int own, more = 0, row, first;
     if (joint) {
-        const int64_t seen = wide_seen(p, rq);
-        const int tile = i / p.tpt;
-        const int64_t s0 = plan.wide0 + rec[3] + h * wide_sum(p, seen, wide_tiles(p, rq.n)) + wide_sum(p, seen, tile);
+        const int seen = wide_seen(p, rq), tile = i / p.tpt;
+        const int s0 = plan.wide0 + rec[3] + h * wide_sum(p, seen, wide_tiles(p, rq.n)) + wide_sum(p, seen, tile);
         first = s0 / plan.wide_per;
-        own = (int)((s0 + seen + (int64_t)(tile + 1) * p.tpt - 1) / plan.wide_per - first) + 1;
+        own = (s0 + wide_length(p, seen, tile) - 1) / plan.wide_per - first + 1;
         row = r - tile * p.tpt * p.G;
     } else {
-        const int length = narrow_length(rq.L);
-        const int64_t k = (int64_t)h * narrow_tiles(p, rq.n) + r / 32, s0 = plan.narrow0 + rec[0] + k * length;
-        first = s0 / plan.narrow_per;
-        own = (int)((s0 + length - 1) / plan.narrow_per - first) + 1;
+        const int length = narrow_length(p, rq.L, plan.aligned);
+        const int k = h * narrow_tiles(p, rq.n) + r / 32, s0 = plan.narrow0 + rec[0] + k * length;
+        first = narrow_piece_of(plan, s0);
+        own = narrow_piece_of(plan, s0 + length - 1) - first + 1;
         row = r & 31;
         first += plan.items0 + rec[1] + k;  // its block in the narrow part
-        if (p.P) more = plan.tiles ? plan.supers * pre_pieces : (int)(((int64_t)(h + 1) * cp - 1) / plan.narrow_per - (int64_t)h * cp / plan.narrow_per) + 1;
+        if (p.P) more = plan.tiles ? plan.supers * pre_pieces : narrow_piece_of(plan, (h + 1) * cp - 1) - narrow_piece_of(plan, h * cp) + 1;
     }
     const bool done = own == 1 && more == 0 && (joint || p.P == 0);  // written by the first kernel
     const int count = done ? 0 : own + more;
@@ -856,20 +879,19 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         at_row = row & 31;
         if (j >= count) return -1;
         if (j < own) {
-            if (joint) return (2 * (first + j) + (j == 0)) * 4 + (row >> 5);
+            if (joint) return (2 * (int64_t)(first + j) + (j == 0)) * 4 + (row >> 5);
             return first + j < p.narrow_blocks ? p.joint_blocks + p.packed_blocks + first + j : -1;
         }
         j -= own;
-        at_row = (int)packed & 31;
+        at_row = packed & 31;
         if (!plan.tiles) {
-            const int64_t blk = h + (int64_t)h * cp / plan.narrow_per + j;
+            const int blk = h + narrow_piece_of(plan, h * cp) + j;
             return blk < p.narrow_blocks ? p.joint_blocks + p.packed_blocks + blk : -1;
         }
-        const int s = j / pre_pieces, pt = (int)(packed / WROWS), len = min(plan.super, plan.nbp - s * plan.super) * 64 + WIDE_EDGE;
-        const int64_t a = h * plan.head + (int64_t)s * plan.tiles * (plan.super * 64 + WIDE_EDGE) + (int64_t)pt * len;
-        const int64_t w = a / plan.wide_per + j - s * pre_pieces;
-        if (w > (a + len - 1) / plan.wide_per) return -1;
-        const int64_t blk = ((int64_t)(h * plan.supers + s) * plan.tiles + pt + w) * 4;
+        const int s = j / pre_pieces, item = s * plan.tiles + packed / WROWS, a = h * plan.head + item * packed_item;
+        const int w = a / plan.wide_per + j - s * pre_pieces;
+        if (w > (a + packed_item - 1) / plan.wide_per) return -1;
+        const int64_t blk = ((int64_t)h * plan.supers * plan.tiles + item + w) * 4;
         return blk + 4 <= p.packed_blocks ? p.joint_blocks + blk + ((packed % WROWS) >> 5) : -1;
     };
     float base = -INFINITY, sum = 0.0f;
@@ -941,14 +963,14 @@ struct AttnSpace {
 };
 static AttnSpace attn_space(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t P) {
     const int64_t G = Hq / Hkv, rows = T * G, wgs = D == 128 ? attn_wgs<128>() : attn_wgs<64>(), some = std::min<int64_t>(B, T);
-    const int64_t is_short = P ? std::min<int64_t>(rows, 255 * (int64_t)B) : 0;  // rows that walk the prefix packed, at most
+    const int64_t is_short = P ? std::min<int64_t>(rows, (LONG_PREFIX - 1) * (int64_t)B) : 0;  // rows that walk the prefix packed, at most
     AttnSpace a;
-    a.joint = rows >= (P ? 256 : 33) ? 2 * wgs * 4 : 0;
+    a.joint = rows >= (P ? LONG_PREFIX : LONG) ? 2 * wgs * 4 : 0;
     const int64_t tiles = (is_short + WROWS - 1) / WROWS;
-    a.packed = is_short > 32 ? (Hkv * tiles * super_count(P, tiles) + wgs) * 4 : 0;
+    a.packed = is_short > 32 ? (std::max(Hkv * tiles * super_count(P, tiles), wgs) + wgs) * 4 : 0;
     a.narrow = Hkv * (1 + (P ? is_short / 32 + some : some)) + wgs;
     a.records = 256;
-    a.blocks = align_up(a.records + (size_t)B * 32, 256);
+    a.blocks = align_up(a.records + (size_t)B * 16, 256);
     a.total = a.blocks + (size_t)(a.joint + a.packed + a.narrow) * (32 * (D + 2) * 4);
     return a;
 }
@@ -982,9 +1004,16 @@ int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
     p.kv_lens = a.kv_lens, p.q_offsets = a.q_offsets, p.B = a.B, p.per = (a.B + GROUPS - 1) / GROUPS, p.c = a.scale * 1.44269504088896341f;
     p.O = static_cast<uint16_t*>(a.O), p.ldo = a.ldo, p.lse = a.lse;
     const AttnSpace s = attn_space(a.T, a.B, a.Hq, a.Hkv, a.D, a.prefix_len);
-    p.plan = reinterpret_cast<Plan*>(a.workspace), p.records = reinterpret_cast<int64_t*>(a.workspace + s.records);
+    p.plan = reinterpret_cast<Plan*>(a.workspace), p.records = reinterpret_cast<int*>(a.workspace + s.records);
     p.blocks = a.workspace + s.blocks;
     p.joint_blocks = s.joint, p.packed_blocks = s.packed, p.narrow_blocks = s.narrow;
+    // the longest that the lines can be
+    const int64_t rows = a.T * p.G, is_long = rows / (p.P ? LONG_PREFIX : LONG), tiles = rows / WROWS + 1, some = std::min<int64_t>(a.B, a.T);
+    const int64_t wide = (int64_t)p.Hkv * (a.T / p.tpt + is_long) * (WIDE_EDGE + p.P + (int64_t)p.max_kv + a.T + WROWS) +
+                         (int64_t)p.Hkv * tiles * 2 * (p.P + (WIDE_EDGE + 64) * MAX_SUPER);
+    const int64_t narrow = (int64_t)p.Hkv * (rows / 32 + some + 1) * (std::max<int64_t>(p.P, p.max_kv) / 32 + NARROW_EDGE + 2 * MIN_NARROW);
+    for (p.ws = 0; wide >> p.ws > 1 << 30;) ++p.ws;
+    for (p.ns = 0; narrow >> p.ns > 1 << 30;) ++p.ns;
     return a.D == 64 ? launch<64>(p, st) : launch<128>(p, st);
 }
 
