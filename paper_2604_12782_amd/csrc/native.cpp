@@ -5,6 +5,7 @@
 // which 3.3 are the launch itself.
 #include <Python.h>
 
+#include <ATen/core/Tensor.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -411,22 +412,30 @@ PyObject* page_slots(PyObject* const* a) {
     const int64_t pool = count(a[2]);
     const int32_t* pn = ints(a[3], 1, kv, "n_free: int32 [1]");
     const at::Tensor& table = tensor(a[4]);
-    if (!(table.dim() == 2 && table.scalar_type() == at::kInt && table.size(0) == B && table.stride(1) == 1 && table.device() == kv.device()))
-        reject("block_table: int32 [B, pages]");
-    // a row's width, not its pitch, is what a request may use; the pitch places the rows
-    const int64_t width = table.size(1), pitch_t = B > 1 ? table.stride(0) : width;
-    if (pitch_t != width) reject("block_table: rows one behind the other");
+    if (!(table.dim() == 2 && table.scalar_type() == at::kInt && table.size(0) == B && table.is_contiguous() && table.device() == kv.device()))
+        reject("block_table: contiguous int32 [B, pages]");
+    const int64_t width = table.size(1);
     Ref lens, offs, pos, slots, info;
     const Outs outs(a[8], 5);
     if (outs) {
         Ref* r[5] = {&lens, &offs, &pos, &slots, &info};
         for (int i = 0; i < 5; ++i) r[i]->share(outs.item[i]);
     } else {
-        lens.own(fresh(kv, {B}, at::kInt));
-        offs.own(fresh(kv, {B + 1}, at::kInt));
-        pos.own(fresh(kv, {T < 0 ? 0 : T}, at::kInt));
-        slots.own(fresh(kv, {T < 0 ? 0 : T}, at::kInt));
-        info.own(fresh(kv, {4}, at::kInt));
+        // one allocation, five tensors in it: five took longer than the kernel
+        Ref all;
+        const int64_t t = T < 0 ? 0 : T, sizes[5] = {B, B + 1, t, t, 4};
+        int64_t at[6] = {0};
+        for (int i = 0; i < 5; ++i) at[i + 1] = at[i] + (sizes[i] + 15) / 16 * 16;
+        all.own(fresh(kv, {at[5]}, at::kInt));
+        const at::Tensor& whole = tensor(all.o);
+        Ref* r[5] = {&lens, &offs, &pos, &slots, &info};
+        for (int i = 0; i < 5; ++i) {
+            at::Tensor part = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+            part.unsafeGetTensorImpl()->set_storage_offset(at[i]);
+            part.unsafeGetTensorImpl()->set_sizes_contiguous({sizes[i]});
+            r[i]->own(THPVariable_Wrap(part));
+            if (!r[i]->o) throw PyFailed();
+        }
     }
     int32_t *o0 = ints(lens.o, B, kv, "lengths: int32 [B]"), *o1 = ints(offs.o, B + 1, kv, "q_offsets: int32 [B + 1]"),
             *o2 = ints(pos.o, T, kv, "positions: int32 [T]"), *o3 = ints(slots.o, T, kv, "slots: int32 [T]"), *o4 = ints(info.o, 4, kv, "info: int32 [4]");

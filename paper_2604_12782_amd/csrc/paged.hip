@@ -9,9 +9,10 @@ namespace osc {
 // Two running sums over the requests place everything: q_off[b] = sum of the new tokens before b, need_off[b] = sum of the new
 // pages before b.  A workgroup computes both for all requests in LDS (a request costs it 8 bytes from L2) and then serves its
 // share of the tokens: a binary search in q_off finds the request, need_off the page.  So the step is one launch with
-// no word passed between workgroups; the first token of a new page writes that page's table entry.
+// no word passed between workgroups; the first token of a new page writes that page's table entry.  Sums stop at 2^32 - 1,
+// which keeps them in order: what lies past 2^31 - 1 tokens or past the free pages needs no exact number.
 // Bound by latency: the lengths' read, the two sums, the table's read and the store depend on one another.
-template <int NT>
+template <int NT, int PER>
 __global__ __launch_bounds__(NT) void page_slots_kernel(const int32_t* __restrict__ kv_lens, const int32_t* __restrict__ q_lens, int B, int lg,
                                                         const int32_t* __restrict__ free_pages, int64_t n_pool,
                                                         const int32_t* __restrict__ n_free_ptr, int32_t* table, int64_t ldt, int pos_base,
@@ -19,72 +20,78 @@ __global__ __launch_bounds__(NT) void page_slots_kernel(const int32_t* __restric
                                                         int32_t* __restrict__ positions, int32_t* __restrict__ slots, int32_t* __restrict__ info) {
     extern __shared__ int32_t lds[];
     int32_t *q_off = lds, *need_off = lds + B, *kv_at = lds + 2 * B;  // need_off: -1 for a refused request
-    __shared__ int64_t part[NT / 64][2];
+    __shared__ uint32_t part[NT / 64][2];
     __shared__ int32_t sums[2];  // pages taken, requests refused
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t ps1 = ((int64_t)1 << lg) - 1;
-    int n_free = *n_free_ptr;
-    n_free = max(0, (int)min((int64_t)n_free, n_pool));
+    const uint32_t ps1 = (1u << lg) - 1;
+    const uint32_t n_free = (uint32_t)max(0, (int)min((int64_t)*n_free_ptr, n_pool));
     if (tid < 2) sums[tid] = 0;
 
-    const int per = (B + NT - 1) / NT, b0 = min(B, tid * per), b1 = min(B, b0 + per);
-    int64_t my_q = 0, my_need = 0;
-    auto lengths = [&](int b, int64_t& kv, int64_t& q, int64_t& need) {
-        kv = max(kv_lens[b], 0);
-        q = max(q_lens[b], 0);
-        const int64_t pages = (kv + q + ps1) >> lg;
-        const bool fits = pages <= ldt && kv + q <= 0x7fffffff;
-        need = fits ? pages - ((kv + ps1) >> lg) : -1;
-    };
-    for (int b = b0; b < b1; ++b) {
-        int64_t kv, q, need;
-        lengths(b, kv, q, need);
-        my_q += q;
-        my_need += max(need, (int64_t)0);
+    const int b0 = tid * PER;
+    uint32_t kv[PER], q[PER], need[PER], my_q = 0, my_need = 0;
+    bool fits[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const bool there = b0 + k < B;
+        kv[k] = there ? max(kv_lens[b0 + k], 0) : 0;
+        q[k] = there ? max(q_lens[b0 + k], 0) : 0;
     }
-    int64_t sq = my_q, sn = my_need;  // inclusive over the wavefront's lanes
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const uint32_t all = kv[k] + q[k], pages = (uint32_t)(((uint64_t)all + ps1) >> lg);  // below 2^32
+        fits[k] = all <= 0x7fffffffu && pages <= (uint64_t)ldt;
+        need[k] = fits[k] ? pages - ((kv[k] + ps1) >> lg) : 0;
+        my_q = __builtin_elementwise_add_sat(my_q, q[k]);
+        my_need = __builtin_elementwise_add_sat(my_need, need[k]);
+    }
+    uint32_t sq = my_q, sn = my_need;  // over the lanes below and this one
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int64_t uq = __shfl_up(sq, d), un = __shfl_up(sn, d);
-        if (lane >= d) sq += uq, sn += un;
+        const uint32_t uq = __shfl_up(sq, d), un = __shfl_up(sn, d);
+        if (lane >= d) sq = __builtin_elementwise_add_sat(sq, uq), sn = __builtin_elementwise_add_sat(sn, un);
     }
     if (lane == 63) part[wave][0] = sq, part[wave][1] = sn;
+    sq = __shfl_up(sq, 1), sn = __shfl_up(sn, 1);
+    if (lane == 0) sq = sn = 0;
     __syncthreads();
-    int64_t total = 0;
-    sq -= my_q;
-    sn -= my_need;
+    uint32_t total = 0, before_q = 0, before_n = 0;
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-        if (w < wave) sq += part[w][0], sn += part[w][1];
-        total += part[w][0];
+        const uint32_t pq = part[w][0], pn = part[w][1];
+        if (w < wave) before_q = __builtin_elementwise_add_sat(before_q, pq), before_n = __builtin_elementwise_add_sat(before_n, pn);
+        total = __builtin_elementwise_add_sat(total, pq);
     }
+    sq = __builtin_elementwise_add_sat(before_q, sq), sn = __builtin_elementwise_add_sat(before_n, sn);
     int taken = 0, refused = 0;
     const bool first = blockIdx.x == 0;
-    for (int b = b0; b < b1; ++b) {
-        int64_t kv, q, need;
-        lengths(b, kv, q, need);
-        const bool ok = need == 0 || (need > 0 && sn + need <= n_free);
-        q_off[b] = (int32_t)min(sq, (int64_t)0x7fffffff);
-        need_off[b] = ok ? (int32_t)min(sn, (int64_t)0x7fffffff) : -1;
-        kv_at[b] = (int32_t)kv;
-        if (first) {
-            q_offsets[b] = q_off[b];
-            kv_out[b] = (int32_t)(ok ? kv + q : kv);
-            if (ok) taken += (int)need;
-            else ++refused;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int b = b0 + k;
+        const uint32_t to = __builtin_elementwise_add_sat(sn, need[k]);
+        if (b < B) {
+            const bool ok = fits[k] && (need[k] == 0 || to <= n_free);
+            q_off[b] = (int32_t)min(sq, 0x7fffffffu);
+            need_off[b] = ok ? (int32_t)min(sn, 0x7fffffffu) : -1;
+            kv_at[b] = (int32_t)kv[k];
+            if (first) {
+                q_offsets[b] = q_off[b];
+                kv_out[b] = (int32_t)(ok ? kv[k] + q[k] : kv[k]);
+                if (ok) taken += (int)need[k];
+                else ++refused;
+            }
         }
-        sq += q;
-        sn += max(need, (int64_t)0);
+        sq = __builtin_elementwise_add_sat(sq, q[k]);
+        sn = to;
     }
     if (first) {
         if (taken) atomicAdd(&sums[0], taken);  // integers in LDS: no order shows
         if (refused) atomicAdd(&sums[1], refused);
     }
     __syncthreads();
-    const int tokens = (int)min(total, (int64_t)0x7fffffff);
+    const int tokens = (int)min(total, 0x7fffffffu);
     if (first && tid == 0) {
         q_offsets[B] = tokens;
-        info[0] = n_free - sums[0];
+        info[0] = (int)n_free - sums[0];
         info[1] = sums[0];
         info[2] = sums[1];
         info[3] = tokens;
@@ -98,10 +105,10 @@ __global__ __launch_bounds__(NT) void page_slots_kernel(const int32_t* __restric
                 if (q_off[mid] <= t) lo = mid;
                 else hi = mid;
             }
-            const int64_t kv = kv_at[lo], p = kv + (t - q_off[lo]);
+            const int64_t have_kv = kv_at[lo], p = have_kv + (t - q_off[lo]);
             pos = (int)min((int64_t)pos_base + p, (int64_t)0x7fffffff);
             if (need_off[lo] >= 0) {
-                const int64_t i = p >> lg, have = (kv + ps1) >> lg;
+                const int64_t i = p >> lg, have = (have_kv + ps1) >> lg;
                 int32_t* entry = table + (int64_t)lo * ldt + i;
                 int page;
                 if (i < have) page = *entry;
@@ -120,24 +127,25 @@ __global__ __launch_bounds__(NT) void page_slots_kernel(const int32_t* __restric
 int launch_page_slots(const int32_t* kv_lens, const int32_t* q_lens, int32_t B, int lg, const int32_t* free_pages, int64_t n_pool,
                       const int32_t* n_free, int32_t* table, int64_t ldt, int32_t pos_base, int64_t T, int32_t* kv_out, int32_t* q_offsets,
                       int32_t* positions, int32_t* slots, int32_t* info, hipStream_t st) {
-    const size_t lds = (size_t)B * 12 + 4;
+    const size_t lds = (size_t)B * 12;
     const int64_t most = 4 * (int64_t)cu_count();
     if (most <= 0) return fail(OSC_ERR_HIP, "osc_page_slots: cannot read the device");
-    static LdsReserved r256, r1024;
-#define LAUNCH(NT, R)                                                                                                          \
-    {                                                                                                                          \
-        if (lds > 48 * 1024) {                                                                                                 \
-            const int rc = reserve_lds((const void*)page_slots_kernel<NT>, lds, R);                                            \
-            if (rc) return rc;                                                                                                 \
-        }                                                                                                                      \
-        int64_t wgs = (T + NT - 1) / NT;                                                                                       \
-        wgs = wgs < 1 ? 1 : wgs > most ? most : wgs;                                                                           \
-        page_slots_kernel<NT><<<dim3((unsigned)wgs), NT, lds, st>>>(kv_lens, q_lens, B, lg, free_pages, n_pool, n_free, table, \
-                                                                    ldt, pos_base, T, kv_out, q_offsets, positions, slots, info); \
-    }
-    if (B <= 256) LAUNCH(256, r256) else LAUNCH(1024, r1024)
-#undef LAUNCH
-    return check_launch("osc_page_slots");
+    auto go = [&](auto kernel, int nt, LdsReserved& r) {
+        if (lds > 48 * 1024) {
+            const int rc = reserve_lds((const void*)kernel, lds, r);
+            if (rc) return rc;
+        }
+        int64_t wgs = (T + nt - 1) / nt;
+        wgs = wgs < 1 ? 1 : wgs > most ? most : wgs;
+        kernel<<<dim3((unsigned)wgs), nt, lds, st>>>(kv_lens, q_lens, B, lg, free_pages, n_pool, n_free, table, ldt, pos_base, T, kv_out, q_offsets,
+                                                     positions, slots, info);
+        return check_launch("osc_page_slots");
+    };
+    static LdsReserved r256, r1, r2, r8;
+    if (B <= 256) return go(page_slots_kernel<256, 1>, 256, r256);
+    if (B <= 1024) return go(page_slots_kernel<1024, 1>, 1024, r1);
+    if (B <= 2048) return go(page_slots_kernel<1024, 2>, 1024, r2);
+    return go(page_slots_kernel<1024, 8>, 1024, r8);
 }
 
 // ---- rotation angles -------------------------------------------------------------------------------------------
