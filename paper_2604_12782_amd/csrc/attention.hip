@@ -31,10 +31,18 @@ constexpr int WG = 256, WROWS = 128, GROUPS = 256;
 template <int D>
 constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
 // The line of 32-row tiles is measured in tiles of 32 tokens, that of 128-row tiles in tokens.  Starting and ending a segment costs
-// about as much as the EDGEs; no piece is smaller than the MINs.
-constexpr int NARROW_EDGE = 4, MIN_NARROW = 8, WIDE_EDGE = 128, MIN_WIDE = 512;
+// about as much as the EDGEs; no piece is smaller than the MINs (MIN_WIDE where workgroups have little to do, and twice that where
+// they have more than 16 narrow tiles each: us with 256 against 512, 32 heads on 8, 32 requests behind 1000 tokens 21.0 / 25.4, 20 behind
+// 9000 26.0 / 28.5; 100 behind 3000 40.7 / 37.0, 64 behind 8192 with 400 of their own 53.9 / 45.4).
+constexpr int NARROW_EDGE = 4, MIN_NARROW = 8, WIDE_EDGE = 128, MIN_WIDE = 256;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
 constexpr int LONG_PREFIX = 256, LONG = 33;  // rows of a long request, with a prefix and without
+// The narrow line is cut where pieces end; or its items are whole pieces each; or (SOLO) every item is a workgroup's and walks the prefix too, so
+// that nothing is left to join: where there are no more items than workgroups and no request sees more than SOLO_FEW tokens, or
+// SOLO_MANY where a quarter of the workgroups or more have an item.  us, cut against solo, 32 heads on 8: 4 requests that see 300 tokens
+// 14.7 / 13.7, 700 15.8 / 16.7; 32 requests 340 20.4 / 13.8, 1090 25.4 / 20.4; 60 requests 1090 25.8 / 23.8.
+enum { CUT = 0, ALIGNED = 1, SOLO = 2 };
+constexpr int SOLO_FEW = 512, SOLO_MANY = 1024;
 
 struct AttnArgs {
     const uint16_t* Q;
@@ -83,9 +91,9 @@ __device__ __forceinline__ Request request(const AttnArgs& p, int b) {
 }
 __device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? LONG_PREFIX : LONG); }
 __device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (n * p.G + 31) >> 5; }
-__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, bool aligned) {
+__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int mode) {
     const int n = (((L + 31) >> 5) + NARROW_EDGE + (1 << p.ns) - 1) >> p.ns;
-    return aligned ? (n + MIN_NARROW - 1) / MIN_NARROW * MIN_NARROW : n;
+    return mode == CUT ? n : mode == ALIGNED ? (n + MIN_NARROW - 1) / MIN_NARROW * MIN_NARROW : 1;
 }
 __device__ __forceinline__ int narrow_tile(const AttnArgs& p, int y) { return max(0, (y << p.ns) - NARROW_EDGE); }  // the first tile at place y of an item
 // the first k tiles of a long request on their line: each sees `seen` and a tile's tokens more than the one before it
@@ -94,14 +102,14 @@ __device__ __forceinline__ int wide_seen(const AttnArgs& p, const Request& r) { 
 __device__ __forceinline__ int wide_length(const AttnArgs& p, int seen, int tile) { return seen + (tile + 1) * (p.tpt >> p.ws); }
 __device__ __forceinline__ int wide_tiles(const AttnArgs& p, int n) { return (n + p.tpt - 1) / p.tpt; }
 __device__ __forceinline__ int packed_length(const AttnArgs& p, int blocks) { return ((blocks * 64 + WIDE_EDGE) >> p.ws) + 1; }
-__device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, bool aligned) {
+__device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, int mode) {
     Extent e{0, 0, 0, 0};
     if (r.n == 0) return e;
     if (is_long(p, r.n)) {
         e.wide = p.Hkv * wide_sum(p, wide_seen(p, r), wide_tiles(p, r.n));
     } else {
         e.items = narrow_tiles(p, r.n) * p.Hkv;
-        e.narrow = e.items * narrow_length(p, r.L, aligned);
+        e.narrow = e.items * narrow_length(p, r.L, mode);
         if (p.P) e.rows = r.n * p.G;
     }
     return e;
@@ -111,13 +119,13 @@ __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, bo
 // Wide pieces are equal; the first `with_wide` workgroups have one.  These take narrow pieces of length `a`, the others of length
 // `b`, so that all have the same to do: a wide block of 64 tokens takes about as long as 5/4 narrow tiles (1.9 us where a CU
 // has two workgroups at it, a narrow tile 1.5 us of HBM).  Where there are more workgroups than pieces of the least length,
-// items are rounded up to whole pieces (`aligned`): none is cut, and no workgroup has two.
+// items are rounded up to whole pieces (ALIGNED): no workgroup has parts of two.
 struct Plan {
     int narrow, wide;      // lengths of the lines
     int narrow0, items0;   // of which the prefix's narrow items are the first
     int wide0, head;       // of which the packed tiles are the first, `head` for every key/value head
     int wide_per, a, b, cut;
-    int with_wide, aligned;
+    int with_wide, mode;
     int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; pieces of the prefix, blocks of 64 tokens in one, in the prefix
     int valid;  // offsets are in order
 };
@@ -127,29 +135,32 @@ __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
     return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
 }
 template <int D>
-__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rounded, int rows, int wide) {
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rounded, int items, int rows, int wide, int small) {
     constexpr int N = attn_wgs<D>();
     Plan a;
     a.valid = 1;
+    const bool solo = items <= N && (items < N / 4 ? small & 1 : small >> 1);
+    if (solo) narrow = items, rows = 0;
     a.rows = rows;
     a.nbp = (p.P + 63) >> 6;
     a.narrow0 = a.items0 = a.wide0 = a.head = 0;
     a.tiles = a.supers = a.super = 0;
     const bool narrow_prefix = rows > 0 && rows <= 32;
-    if (narrow_prefix) rounded += p.Hkv * narrow_length(p, p.P, true);
-    a.aligned = rounded <= N * MIN_NARROW;
-    if (a.aligned) narrow = rounded;
+    if (narrow_prefix) rounded += p.Hkv * narrow_length(p, p.P, ALIGNED);
+    a.mode = solo ? SOLO : rounded <= N * MIN_NARROW ? ALIGNED : CUT;
+    if (a.mode == ALIGNED) narrow = rounded;
     if (narrow_prefix) {
         a.items0 = p.Hkv;
-        a.narrow0 = p.Hkv * narrow_length(p, p.P, a.aligned);
-        if (!a.aligned) narrow += a.narrow0;
+        a.narrow0 = p.Hkv * narrow_length(p, p.P, a.mode);
+        if (a.mode == CUT) narrow += a.narrow0;
     }
     a.wide_per = 0;
     if (rows > 32) {
         a.tiles = (rows + WROWS - 1) / WROWS;
         const int th = p.Hkv * a.tiles;
         const bool whole = wide == 0 && th <= N;  // nothing else on the line: an item a piece, in one round
-        a.supers = whole ? max(1, min(N / th, a.nbp * 64 / MIN_WIDE)) : super_count(p.P, a.tiles);
+        const int load = (narrow + (int)min((int64_t)th * a.nbp * 5 / 4, (int64_t)1 << 29)) / N;
+        a.supers = whole ? max(1, min(N / th, a.nbp * 64 / (load < 16 ? MIN_WIDE : 2 * MIN_WIDE))) : super_count(p.P, a.tiles);
         a.super = (a.nbp + a.supers - 1) / a.supers;
         a.supers = (a.nbp + a.super - 1) / a.super;
         a.head = a.tiles * a.supers * packed_length(p, a.super);
@@ -158,13 +169,14 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rou
     }
     a.narrow = narrow;
     a.wide = a.wide0 + wide;
-    if (!a.wide_per) a.wide_per = max((a.wide + N - 1) / N, max(MIN_WIDE >> p.ws, 1));
+    if (!a.wide_per) a.wide_per = max((a.wide + N - 1) / N, max(2 * MIN_WIDE >> p.ws, 1));
     a.with_wide = ((a.wide + a.wide_per - 1) / a.wide_per + 7) / 8 * 8;  // as many on every XCD
     const int others = N - a.with_wide, cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 4)) >> p.ns, (int64_t)1 << 20);
     a.b = (narrow + N - 1) / N + (a.with_wide * cost + N - 1) / N;
     a.a = a.b - cost;
-    if (others == 0) a.a = max((narrow + N - 1) / N, MIN_NARROW);
-    else if (a.aligned) a.b = MIN_NARROW, a.a = others * MIN_NARROW >= narrow ? 0 : MIN_NARROW;
+    if (solo) a.a = 0, a.b = 1;  // no wide work
+    else if (others == 0) a.a = max((narrow + N - 1) / N, MIN_NARROW);
+    else if (a.mode == ALIGNED) a.b = MIN_NARROW, a.a = others * MIN_NARROW >= narrow ? 0 : MIN_NARROW;
     else if (a.a < MIN_NARROW) a.a = 0, a.b = max((narrow + others - 1) / others, MIN_NARROW);
     a.cut = a.a * a.with_wide;
     return a;
@@ -185,13 +197,13 @@ __device__ __forceinline__ int find_group(const int (&sums)[GROUPS], int x, int 
 }
 // The request that holds place x of a line: its number and what is before it.  All lanes of a wavefront take part.
 template <bool WIDE>
-__device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, bool aligned, int x, int lane, Extent& before) {
+__device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, int mode, int x, int lane, Extent& before) {
     const int g = uni(find_group(WIDE ? s.wide : s.narrow, x, lane));
     before = Extent{uni(s.narrow[g]), uni(s.items[g]), uni(s.rows[g]), uni(s.wide[g])};
     int b = g * p.per;
     if (p.per > 1) {  // at most 32 requests of a group: one a lane
         Extent e{0, 0, 0, 0};
-        if (lane < p.per && b + lane < p.B) e = extent(p, request(p, b + lane), aligned);
+        if (lane < p.per && b + lane < p.B) e = extent(p, request(p, b + lane), mode);
         Extent sum = e;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -220,7 +232,7 @@ __device__ __forceinline__ void packed_row(const AttnArgs& p, const Sums& s, int
     int b = lo * p.per;
     Request q = request(p, b);
     for (int last = min(p.B, b + p.per) - 1; b < last; q = request(p, ++b)) {
-        const int n = extent(p, q, false).rows;
+        const int n = extent(p, q, CUT).rows;
         if (at + n > r) break;
         at += n;
     }
@@ -439,28 +451,27 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
     const int end = min(x + (with_wide ? plan.a : plan.b), plan.narrow);
     while (x < end) {
         // the item at x: its start and length on the line, its rows, its tokens
-        int start, item, length, h, r0, rows, tokens, seen = 0, clear_to, b = -1;
+        int start, item, length, h, r0, rows, n_prefix, tokens = 0, seen = 0, clear_to = 0, b = -1;  // tiles of the prefix, then own tokens
         Request rq{0, 0, 0};
-        const int32_t* pages;
         if (x < plan.narrow0) {
-            length = narrow_length(p, p.P, plan.aligned);
+            length = narrow_length(p, p.P, plan.mode);
             h = x / length;
             start = h * length, item = h;
-            r0 = 0, rows = plan.rows, tokens = p.P, clear_to = p.P, pages = p.prefix_pages;
+            r0 = 0, rows = plan.rows, n_prefix = (p.P + 31) >> 5;
         } else {
             Extent before;
-            b = find_request<false>(p, sums, plan.aligned, x - plan.narrow0, lane, before);
+            b = find_request<false>(p, sums, plan.mode, x - plan.narrow0, lane, before);
             rq = request(p, b);
-            length = narrow_length(p, rq.L, plan.aligned);
+            length = narrow_length(p, rq.L, plan.mode);
             const int nt = narrow_tiles(p, rq.n), k = (x - plan.narrow0 - before.narrow) / length;
             start = plan.narrow0 + before.narrow + k * length, item = plan.items0 + before.items + k;
             h = k / nt;
             r0 = (k - h * nt) * 32, rows = rq.n * p.G;
             tokens = max(0, rq.L - rq.n + min(r0 + 31, rows - 1) / p.G + 1), clear_to = rq.L - rq.n + r0 / p.G + 1;
-            pages = p.table + (int64_t)b * p.ldt;
+            n_prefix = plan.mode == SOLO ? (p.P + 31) >> 5 : 0;
         }
         const int stop = min(end, start + length);
-        const int t0 = narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), (tokens + 31) >> 5);
+        const int t0 = narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), n_prefix + ((tokens + 31) >> 5));
         const bool whole = x == start && stop == start + length;
         x = stop;
 
@@ -468,7 +479,6 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
         int ti = rc / p.G, g = rc - ti * p.G;
         if (b < 0) {
             packed_row(p, sums, rc, ti, g);
-            seen = p.P;
         } else {
             seen = rq.L - rq.n + ti + 1;
             ti += rq.q0;
@@ -481,14 +491,18 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
         State<D> st;
         clear(st);
         auto runs = [&](int tile, const uint8_t*& a, const uint8_t*& c) {
-            const int j = tile * 32, j2 = min(j + 16, tokens - 1);
-            a = run_of<D>(p, pages[j >> p.lg], h, j);
-            c = run_of<D>(p, pages[j2 >> p.lg], h, j2);
+            const bool pre = tile < n_prefix;
+            const int32_t* pages = pre ? p.prefix_pages : p.table + (int64_t)b * p.ldt;
+            const int j = (pre ? tile : tile - n_prefix) * 32, j2 = min(j + 16, (pre ? p.P : tokens) - 1);
+            const int one = pages[j >> p.lg], two = pages[j2 >> p.lg];
+            a = run_of<D>(p, one, h, j);
+            c = run_of<D>(p, two, h, j2);
         };
         auto fetch = [&](int tile, const uint8_t* a, const uint8_t* c, int64_t shift, uint32_t dst) {
-            const int left = tokens - 1 - tile * 32;
+            const bool pre = tile < n_prefix;
+            const int last = (pre ? p.P : tokens) - 1, left = last - (pre ? tile : tile - n_prefix) * 32;
             fetch16<D>(a + shift, 0, min(left, 15), dst, lane);
-            fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : ((tokens - 1) & 15), dst, lane);
+            fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : last & 15, dst, lane);
         };
         int tile = t0 + wave;
         const uint8_t *ra = nullptr, *rb = nullptr, *na = nullptr, *nb = nullptr;
@@ -508,8 +522,9 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             lds_order();
             __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the keys are read
             if (more) fetch(tile + 4, na, nb, 0, kt);
-            const int j0 = tile * 32;
-            if (j0 + 32 > clear_to) mask<1>(s, lane, seen - j0);
+            const bool pre = tile < n_prefix;
+            const int j0 = (pre ? tile : tile - n_prefix) * 32;
+            if (j0 + 32 > (pre ? p.P : clear_to)) mask<1>(s, lane, (pre ? p.P : seen) - j0);
             weigh<D, 1>(st, s, p.c);
             if (more) wait_vmcnt<NI>();
             else wait_vmcnt<0>();
@@ -535,7 +550,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
         if (lane < 32) stats[wave * 32 + lane] = st.base, stats[128 + wave * 32 + lane] = st.sum;
         __syncthreads();
         const int row = tid >> 3, part = tid & 7;
-        const bool direct = p.P == 0 && whole;
+        const bool direct = whole && (p.P == 0 || plan.mode == SOLO);
         const int slot = item + w;
         if (r0 + row < rows && (direct || slot < p.narrow_blocks)) {
             float base = -INFINITY, f[4], sum = 0.0f;
@@ -602,7 +617,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             slot = p.joint_blocks + ((int64_t)(h * plan.supers + s) * plan.tiles + tile + w) * 4;
         } else {
             Extent before;
-            b = find_request<true>(p, sums, false, x - plan.wide0, lane, before);
+            b = find_request<true>(p, sums, CUT, x - plan.wide0, lane, before);
             rq = request(p, b);
             const int nt = wide_tiles(p, rq.n);
             const int seen = wide_seen(p, rq), head = wide_sum(p, seen, nt), y = x - plan.wide0 - before.wide;
@@ -738,7 +753,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
 
 struct AttnShared {
     Sums sums;
-    int part[4][5];
+    int part[4][6];
     float stats[256];
 };
 
@@ -753,14 +768,16 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     const int T = (int)p.T;
     constexpr int NV = 5;  // narrow, narrow rounded up, items, rows, wide
     int mine[NV] = {0, 0, 0, 0, 0}, v[NV], total[NV];
-    bool wrong = false;
+    bool wrong = false, few = true, many = true;  // no more than SOLO_FEW, SOLO_MANY tokens
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
     for (int b = b0; b < b1; ++b) {
         const Request r = request(p, b);
         wrong |= r.q0 < 0 || r.n < 0 || r.q0 > T - r.n;
         if (wrong) break;
-        const Extent e = extent(p, r, false);
-        mine[0] += e.narrow, mine[1] += e.items * narrow_length(p, r.L, true), mine[2] += e.items, mine[3] += e.rows, mine[4] += e.wide;
+        const Extent e = extent(p, r, CUT);
+        const int sees = is_long(p, r.n) ? SOLO_MANY + 1 : p.P + r.L;
+        few &= sees <= SOLO_FEW, many &= sees <= SOLO_MANY;
+        mine[0] += e.narrow, mine[1] += e.items * narrow_length(p, r.L, ALIGNED), mine[2] += e.items, mine[3] += e.rows, mine[4] += e.wide;
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) v[k] = mine[k];
@@ -774,6 +791,8 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     if (lane == 63)
 #pragma unroll
         for (int k = 0; k < NV; ++k) part[wave][k] = v[k];
+    const int small = (__ballot(!few) == 0) + 2 * (__ballot(!many) == 0);
+    if (lane == 0) part[wave][NV] = small;
     if (__syncthreads_or(wrong)) {  // offsets that fall or name rows that are not there: nothing is read or written
         if (blockIdx.x == 0 && tid == 0) p.plan->valid = 0;
         return;
@@ -788,14 +807,14 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
             total[k] += part[u][k];
         }
     }
-    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[3]), uni(total[4]));
-    const bool aligned = plan.aligned;
-    if (aligned) v[0] = v[1];
+    const int all_small = uni(part[0][NV] & part[1][NV] & part[2][NV] & part[3][NV]);
+    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), all_small);
+    if (plan.mode != CUT) v[0] = plan.mode == ALIGNED ? v[1] : v[2];
     sums.narrow[tid] = v[0], sums.items[tid] = v[2], sums.rows[tid] = v[3], sums.wide[tid] = v[4];
     if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
         if (tid == 0) *p.plan = plan;
         for (int b = b0; b < b1; ++b) {
-            const Extent e = extent(p, request(p, b), aligned);
+            const Extent e = extent(p, request(p, b), plan.mode);
             int* r = p.records + (int64_t)b * 4;
             r[0] = v[0], r[1] = v[2], r[2] = v[3], r[3] = v[4];
             v[0] += e.narrow, v[2] += e.items, v[3] += e.rows, v[4] += e.wide;
@@ -829,6 +848,8 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
     const int t = (int)(unit / per_token);
     if (t >= p.T) return;
     const int head0 = (int)(unit - (int64_t)t * per_token) * H;
+    const Plan plan = *p.plan;
+    if (!plan.valid || plan.mode == SOLO) return;
     int lo = 0, hi = p.B + 1;  // the last request that starts at or before t
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64, at = lo + lane * step;
@@ -839,14 +860,12 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
     }
     const int b = uni(lo);
     if (b >= p.B) return;
-    const Plan plan = *p.plan;
-    if (!plan.valid) return;
     const Request rq = request(p, b);
     const int i = t - rq.q0;
     if (i < 0 || i >= rq.n) return;
     const int* rec = p.records + (int64_t)b * 4;
     const bool joint = is_long(p, rq.n);
-    const int cp = narrow_length(p, p.P, plan.aligned), packed_item = packed_length(p, plan.super);
+    const int cp = narrow_length(p, p.P, plan.mode), packed_item = packed_length(p, plan.super);
     const int pre_pieces = packed_item == plan.wide_per ? 1 : plan.tiles ? (packed_item - 1) / plan.wide_per + 2 : 0;  // of a piece of the prefix, at most
 
     // this lane's row: `own` segments of its request's tile, the first at `first`; then up to `more` of the prefix
@@ -860,7 +879,7 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         own = (s0 + wide_length(p, seen, tile) - 1) / plan.wide_per - first + 1;
         row = r - tile * p.tpt * p.G;
     } else {
-        const int length = narrow_length(p, rq.L, plan.aligned);
+        const int length = narrow_length(p, rq.L, plan.mode);
         const int k = h * narrow_tiles(p, rq.n) + r / 32, s0 = plan.narrow0 + rec[0] + k * length;
         first = narrow_piece_of(plan, s0);
         own = narrow_piece_of(plan, s0 + length - 1) - first + 1;
