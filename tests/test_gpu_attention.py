@@ -170,6 +170,11 @@ def test_rope_forms(osc):
     check_rope(osc, 9, 4, 2, 128, 64, 0, 1, True, scale=2.0 ** 40)     # squares far above, and below, what 16 bits hold
     check_rope(osc, 9, 4, 2, 128, 64, 1, 1, True, scale=2.0 ** -7)
     check_rope(osc, 2000, 6, 2, 128, 128, 0, 1, True, ps=64)
+    check_rope(osc, 9, 4, 2, 128, 128, 0, 3, True, sections=[16, 24, 24])  # whole groups of four pairs an axis
+    for style in (0, 1):  # several groups of heads a wavefront, the last one not full
+        check_rope(osc, 2300, 25, 5, 128, 128, style, 1, True, ps=64)
+        check_rope(osc, 4200, 25, 5, 64, 48, style, 3, True, ps=32)
+        check_rope(osc, 4200, 25, 5, 64, 64, style, 3, False, ps=32, sections=[8, 12, 12])
 
 
 # ---- attention ---------------------------------------------------------------------------------------------------------
