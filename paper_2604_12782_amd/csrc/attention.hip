@@ -599,9 +599,12 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
     const int lane = tid & 63, wave = uni(tid >> 6);
     const int64_t to_v = p.V - p.K;
     const uint32_t kl = key_lane<D>(lane), vl = value_lane<D>(lane);
-    int x = w * plan.wide_per;
-    const int end = min(x + plan.wide_per, plan.wide);
-    while (x < end) {
+    // Segments are taken from the piece's end: the start of a tile first, the rest of the tile before it after that.  So all
+    // workgroups walk the tokens that they share side by side, whatever their pieces' places, and an XCD's L2 reads them once.
+    const int begin = w * plan.wide_per;
+    int stop = min(begin + plan.wide_per, plan.wide);
+    while (stop > begin) {
+        int x = stop - 1;
         int64_t slot;
         int start, length, h, rows, n_prefix, n_own, b = -1, first_block = 0, own = 0, r0 = 0, t_base = 0;
         Request rq{0, 0, 0};
@@ -637,7 +640,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             n_prefix = plan.nbp, n_own = (own + 63) >> 6;
             slot = 0;
         }
-        const int stop = min(end, start + length);
+        x = max(begin, start);
         const int blocks = n_prefix + n_own;
         constexpr int EDGE = WIDE_EDGE;
         auto block_at = [&](int y) {  // the same for both workgroups at a cut, and not falling: all that is asked of it
@@ -647,7 +650,6 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
         const int k0 = block_at(x - start), k1 = block_at(stop - start);
         const bool whole = x == start && stop == start + length;
         if (b >= 0) slot = (2 * (int64_t)w + (x == start)) * 4;
-        x = stop;
 
         const int r = wave * 32 + (lane & 31), rc = min(r, rows - 1);
         int ti = rc / p.G, g = rc - ti * p.G, seen = 0;
@@ -748,6 +750,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             }
         }
         lds_barrier();  // the next item's first block lands where others may still be reading this one's last
+        stop = x;
     }
 }
 

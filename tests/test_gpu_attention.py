@@ -275,6 +275,25 @@ def test_attention_many_requests(osc, B, P):
     check_attention(osc, make(B + P, B, P, kv.tolist(), n.tolist(), 2, 1, 64, 16))
 
 
+def test_attention_most_requests(osc):
+    gen = np.random.default_rng(2)
+    n, kv = gen.integers(0, 2, 8192), gen.integers(0, 20, 8192)
+    n[5000], kv[5000] = 300, 320
+    check_attention(osc, make(20, 8192, 18, kv.tolist(), n.tolist(), 1, 1, 64, 16))
+
+
+@pytest.mark.parametrize("P", [0, 300])
+def test_attention_behind_a_wide_table(osc, P):
+    """rows of the table that could name 2^28 tokens: the work is then counted in larger units"""
+    n = [1] * 290 + [40, 70, 1, 33, 5, 130, 1, 1, 1, 64]
+    kv = [(7 * b) % 150 + 1 for b in range(290)] + [60, 70, 1000, 33, 5, 500, 1, 2, 700, 64]
+    s = make(21 + P, 300, P, kv, n, 8, 8, 64, 256)
+    wide = dict(s, table=torch.zeros((300, 1 << 20), dtype=torch.int32, device=DEV))
+    wide["table"][:, :s["table"].shape[1]] = s["table"]
+    check_attention(osc, s, got=call(osc, wide))
+    check_attention(osc, s)
+
+
 def test_attention_long_prefix(osc):
     """a prefix in several pieces, packed rows of several tiles that cut requests in two"""
     n = [1, 3, 2, 1, 7] * 8
