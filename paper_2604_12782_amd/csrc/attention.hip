@@ -34,15 +34,11 @@ constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
 // about as much as the EDGEs; no piece is smaller than the MINs (MIN_WIDE where workgroups have little to do, and twice that where
 // they have more than 16 narrow tiles each: us with 256 against 512, 32 heads on 8, 32 requests behind 1000 tokens 21.0 / 25.4, 20 behind
 // 9000 26.0 / 28.5; 100 behind 3000 40.7 / 37.0, 64 behind 8192 with 400 of their own 53.9 / 45.4).
-constexpr int NARROW_EDGE = 4, MIN_NARROW = 8, WIDE_EDGE = 128, MIN_WIDE = 256;
+constexpr int NARROW_EDGE = 2, MIN_NARROW = 4, WIDE_EDGE = 128, MIN_WIDE = 256;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
 constexpr int LONG_PREFIX = 256, LONG = 33;  // rows of a long request, with a prefix and without
-// The narrow line is cut where pieces end; or its items are whole pieces each; or (SOLO) every item is a workgroup's and walks the prefix too, so
-// that nothing is left to join: where there are no more items than workgroups and no request sees more than SOLO_FEW tokens, or
-// SOLO_MANY where a quarter of the workgroups or more have an item.  us, cut against solo, 32 heads on 8: 4 requests that see 300 tokens
-// 14.7 / 13.7, 700 15.8 / 16.7; 32 requests 340 20.4 / 13.8, 1090 25.4 / 20.4; 60 requests 1090 25.8 / 23.8.
-enum { CUT = 0, ALIGNED = 1, SOLO = 2 };
-constexpr int SOLO_FEW = 512, SOLO_MANY = 1024;
+// The narrow line is cut where pieces end, or its items are rounded up to whole pieces.
+enum { CUT = 0, ALIGNED = 1 };
 
 struct AttnArgs {
     const uint16_t* Q;
@@ -93,7 +89,7 @@ __device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p
 __device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (n * p.G + 31) >> 5; }
 __device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int mode) {
     const int n = (((L + 31) >> 5) + NARROW_EDGE + (1 << p.ns) - 1) >> p.ns;
-    return mode == CUT ? n : mode == ALIGNED ? (n + MIN_NARROW - 1) / MIN_NARROW * MIN_NARROW : 1;
+    return mode == ALIGNED ? (n + MIN_NARROW - 1) / MIN_NARROW * MIN_NARROW : n;
 }
 __device__ __forceinline__ int narrow_tile(const AttnArgs& p, int y) { return max(0, (y << p.ns) - NARROW_EDGE); }  // the first tile at place y of an item
 // the first k tiles of a long request on their line: each sees `seen` and a tile's tokens more than the one before it
@@ -116,10 +112,10 @@ __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, in
 }
 
 // What follows from the totals: the prefix's items, which come first on their line, and the pieces.
-// Wide pieces are equal; the first `with_wide` workgroups have one.  These take narrow pieces of length `a`, the others of length
-// `b`, so that all have the same to do: a wide block of 64 tokens takes about as long as 5/4 narrow tiles (1.9 us where a CU
-// has two workgroups at it, a narrow tile 1.5 us of HBM).  Where there are more workgroups than pieces of the least length,
-// items are rounded up to whole pieces (ALIGNED): no workgroup has parts of two.
+// Wide pieces are equal; the first `with_wide` workgroups have one.  A narrow piece is a wavefront's: those of these workgroups take
+// pieces of length `a`, the others of length `b`, so that all have the same to do: a wide block of 64 tokens takes about a third
+// of the time of a narrow tile (2 us where a CU has two workgroups at it; 16 KB, 6 us where all wavefronts share 5.5 TB/s).  Where there are
+// more wavefronts than pieces of the least length, items are rounded up to whole pieces (ALIGNED): no wavefront has parts of two.
 struct Plan {
     int narrow, wide;      // lengths of the lines
     int narrow0, items0;   // of which the prefix's narrow items are the first
@@ -128,6 +124,7 @@ struct Plan {
     int with_wide, mode;
     int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; pieces of the prefix, blocks of 64 tokens in one, in the prefix
     int valid;  // offsets are in order
+    int joins;  // anything to join
 };
 // Many packed tiles walk the prefix in pieces that stay in an XCD's L2 meanwhile.
 __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
@@ -135,19 +132,17 @@ __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
     return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
 }
 template <int D>
-__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rounded, int items, int rows, int wide, int small) {
-    constexpr int N = attn_wgs<D>();
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rounded, int items, int rows, int wide) {
+    constexpr int N = attn_wgs<D>(), WAVES = 4 * N;
     Plan a;
     a.valid = 1;
-    const bool solo = items <= N && (items < N / 4 ? small & 1 : small >> 1);
-    if (solo) narrow = items, rows = 0;
     a.rows = rows;
     a.nbp = (p.P + 63) >> 6;
     a.narrow0 = a.items0 = a.wide0 = a.head = 0;
     a.tiles = a.supers = a.super = 0;
     const bool narrow_prefix = rows > 0 && rows <= 32;
     if (narrow_prefix) rounded += p.Hkv * narrow_length(p, p.P, ALIGNED);
-    a.mode = solo ? SOLO : rounded <= N * MIN_NARROW ? ALIGNED : CUT;
+    a.mode = rounded <= WAVES * MIN_NARROW ? ALIGNED : CUT;
     if (a.mode == ALIGNED) narrow = rounded;
     if (narrow_prefix) {
         a.items0 = p.Hkv;
@@ -171,18 +166,19 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rou
     a.wide = a.wide0 + wide;
     if (!a.wide_per) a.wide_per = max((a.wide + N - 1) / N, max(2 * MIN_WIDE >> p.ws, 1));
     a.with_wide = ((a.wide + a.wide_per - 1) / a.wide_per + 7) / 8 * 8;  // as many on every XCD
-    const int others = N - a.with_wide, cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 4)) >> p.ns, (int64_t)1 << 20);
-    a.b = (narrow + N - 1) / N + (a.with_wide * cost + N - 1) / N;
+    const int with = 4 * a.with_wide, others = WAVES - with;
+    const int cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 16)) >> p.ns, (int64_t)1 << 18);
+    a.b = (narrow + WAVES - 1) / WAVES + (with * cost + WAVES - 1) / WAVES;
     a.a = a.b - cost;
-    if (solo) a.a = 0, a.b = 1;  // no wide work
-    else if (others == 0) a.a = max((narrow + N - 1) / N, MIN_NARROW);
+    if (others == 0) a.a = max((narrow + WAVES - 1) / WAVES, MIN_NARROW);
     else if (a.mode == ALIGNED) a.b = MIN_NARROW, a.a = others * MIN_NARROW >= narrow ? 0 : MIN_NARROW;
     else if (a.a < MIN_NARROW) a.a = 0, a.b = max((narrow + others - 1) / others, MIN_NARROW);
-    a.cut = a.a * a.with_wide;
+    a.cut = a.a * with;
+    a.joins = p.P || wide || a.mode == CUT || narrow > items * MIN_NARROW;
     return a;
 }
-// the workgroup (in the order of the pieces) that has place x of the narrow line
-__device__ __forceinline__ int narrow_piece_of(const Plan& a, int x) { return x < a.cut ? x / a.a : a.with_wide + (x - a.cut) / a.b; }
+// the wavefront (in the order of the pieces) that has place x of the narrow line
+__device__ __forceinline__ int narrow_piece_of(const Plan& a, int x) { return x < a.cut ? x / a.a : 4 * a.with_wide + (x - a.cut) / a.b; }
 
 // Running sums over groups of `per` requests, in LDS: what a place on a line or a packed row is searched in.
 struct Sums {
@@ -434,30 +430,54 @@ __device__ __forceinline__ void lds_barrier() {
     lds_order();
 }
 
-// ---- a piece of the line of 32-row tiles ----------------------------------------------------------------------------------------
-// The four wavefronts hold the same rows and take every fourth tile of 32 tokens, each in LDS of its own: keys of the next tile are
-// asked for once this tile's scores are there, values once they are summed, so half a tile or more is on its way at any time and
-// no wavefront waits for another before the segment's end.
+// A row's sums: normalised, as its result, or as they are, to the workspace.
 template <int D>
-__device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, float* stats, int w) {
+__device__ __forceinline__ void leave(const AttnArgs& p, const State<D>& st, bool direct, int64_t t, int head, uint8_t* blk, int row, int hi) {
+    if (direct) {
+        const float inv = st.sum > 0.0f ? 1.0f / st.sum : 0.0f;
+        uint16_t* out = p.O + t * p.ldo + head * D + 4 * hi;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<uint2*>(out + 32 * d + 8 * e) =
+                    make_uint2(pack2(st.o[d][4 * e] * inv, st.o[d][4 * e + 1] * inv), pack2(st.o[d][4 * e + 2] * inv, st.o[d][4 * e + 3] * inv));
+        if (p.lse && hi == 0) p.lse[t * p.Hq + head] = lse_of(st.base, st.sum);
+    } else {
+        float* out = reinterpret_cast<float*>(blk) + row * D + 4 * hi;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<float4*>(out + 32 * d + 8 * e) = make_float4(st.o[d][4 * e], st.o[d][4 * e + 1], st.o[d][4 * e + 2], st.o[d][4 * e + 3]);
+        if (hi == 0) *reinterpret_cast<float2*>(blk + (32 * D + row * 2) * 4) = make_float2(st.base, st.sum);
+    }
+}
+
+// ---- a piece of the line of 32-row tiles ----------------------------------------------------------------------------------------
+// A wavefront's own: tiles of 32 tokens in LDS that no other wavefront uses.  Keys of the next tile are asked for once this tile's
+// scores are there, values once they are summed, so half a tile or more is on its way at any time, and no wavefront waits for another.
+template <int D>
+__device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds) {
     constexpr int TILE = 32 * D * 2, NI = D / 16;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // what follows from it is made here, not kept in registers from the kernel's start
     const int lane = tid & 63, wave = uni(tid >> 6);
     const int64_t to_v = p.V - p.K;
     const uint32_t kt = lds_at(lds) + wave * 2 * TILE, vt = kt + TILE, kl = kt + key_lane<D>(lane), vl = vt + value_lane<D>(lane);
-    const bool with_wide = w < plan.with_wide;
-    int x = with_wide ? w * plan.a : plan.cut + (w - plan.with_wide) * plan.b;
-    const int end = min(x + (with_wide ? plan.a : plan.b), plan.narrow);
+    const int w = blockIdx.x * 4 + wave, with = 4 * plan.with_wide;
+    int x = w < with ? w * plan.a : plan.cut + (w - with) * plan.b;
+    const int end = min(x + (w < with ? plan.a : plan.b), plan.narrow);
     while (x < end) {
         // the item at x: its start and length on the line, its rows, its tokens
-        int start, item, length, h, r0, rows, n_prefix, tokens = 0, seen = 0, clear_to = 0, b = -1;  // tiles of the prefix, then own tokens
+        int start, item, length, h, r0, rows, tokens, seen, clear_to, b = -1;
         Request rq{0, 0, 0};
+        const int32_t* pages;
         if (x < plan.narrow0) {
             length = narrow_length(p, p.P, plan.mode);
             h = x / length;
             start = h * length, item = h;
-            r0 = 0, rows = plan.rows, n_prefix = (p.P + 31) >> 5;
+            r0 = 0, rows = plan.rows, tokens = clear_to = seen = p.P, pages = p.prefix_pages;
         } else {
             Extent before;
             b = find_request<false>(p, sums, plan.mode, x - plan.narrow0, lane, before);
@@ -468,10 +488,10 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             h = k / nt;
             r0 = (k - h * nt) * 32, rows = rq.n * p.G;
             tokens = max(0, rq.L - rq.n + min(r0 + 31, rows - 1) / p.G + 1), clear_to = rq.L - rq.n + r0 / p.G + 1;
-            n_prefix = plan.mode == SOLO ? (p.P + 31) >> 5 : 0;
+            pages = p.table + (int64_t)b * p.ldt;
         }
         const int stop = min(end, start + length);
-        const int t0 = narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), n_prefix + ((tokens + 31) >> 5));
+        const int t0 = narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), (tokens + 31) >> 5);
         const bool whole = x == start && stop == start + length;
         x = stop;
 
@@ -491,20 +511,16 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
         State<D> st;
         clear(st);
         auto runs = [&](int tile, const uint8_t*& a, const uint8_t*& c) {
-            const bool pre = tile < n_prefix;
-            const int32_t* pages = pre ? p.prefix_pages : p.table + (int64_t)b * p.ldt;
-            const int j = (pre ? tile : tile - n_prefix) * 32, j2 = min(j + 16, (pre ? p.P : tokens) - 1);
-            const int one = pages[j >> p.lg], two = pages[j2 >> p.lg];
+            const int j = tile * 32, j2 = min(j + 16, tokens - 1), one = pages[j >> p.lg], two = pages[j2 >> p.lg];
             a = run_of<D>(p, one, h, j);
             c = run_of<D>(p, two, h, j2);
         };
         auto fetch = [&](int tile, const uint8_t* a, const uint8_t* c, int64_t shift, uint32_t dst) {
-            const bool pre = tile < n_prefix;
-            const int last = (pre ? p.P : tokens) - 1, left = last - (pre ? tile : tile - n_prefix) * 32;
+            const int left = tokens - 1 - tile * 32;
             fetch16<D>(a + shift, 0, min(left, 15), dst, lane);
-            fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : last & 15, dst, lane);
+            fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : (tokens - 1) & 15, dst, lane);
         };
-        int tile = t0 + wave;
+        int tile = t0;
         const uint8_t *ra = nullptr, *rb = nullptr, *na = nullptr, *nb = nullptr;
         if (tile < t1) {
             runs(tile, ra, rb);
@@ -512,19 +528,18 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             lds_order();  // the waits below count: keys first
             fetch(tile, ra, rb, to_v, vt);
         }
-        for (; tile < t1; tile += 4) {
-            const bool more = tile + 4 < t1;
-            if (more) runs(tile + 4, na, nb);
+        for (; tile < t1; ++tile) {
+            const bool more = tile + 1 < t1;
+            if (more) runs(tile + 1, na, nb);
             wait_vmcnt<NI>();  // the keys are there; the values may not be
             lds_order();
             v16f s[1];
             scores<D, 1>(s, q, kl);
             lds_order();
             __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the keys are read
-            if (more) fetch(tile + 4, na, nb, 0, kt);
-            const bool pre = tile < n_prefix;
-            const int j0 = (pre ? tile : tile - n_prefix) * 32;
-            if (j0 + 32 > (pre ? p.P : clear_to)) mask<1>(s, lane, (pre ? p.P : seen) - j0);
+            if (more) fetch(tile + 1, na, nb, 0, kt);
+            const int j0 = tile * 32;
+            if (j0 + 32 > clear_to) mask<1>(s, lane, seen - j0);
             weigh<D, 1>(st, s, p.c);
             if (more) wait_vmcnt<NI>();
             else wait_vmcnt<0>();
@@ -534,58 +549,13 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             gather<D, 1>(st, s, f, vl);
             lds_order();
             __builtin_amdgcn_s_waitcnt(0xC07F);
-            if (more) fetch(tile + 4, na, nb, to_v, vt);
+            if (more) fetch(tile + 1, na, nb, to_v, vt);
         }
-        // The four wavefronts' parts: each leaves its sums in its own LDS, [row][channel], pieces of 16 bytes spread by row
         st.sum = half_sum(st.sum);
-        float* parts = reinterpret_cast<float*>(lds);
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = lane & 31, piece = 8 * d + 2 * e + (lane >> 5);
-                *reinterpret_cast<float4*>(parts + wave * 32 * D + row * D + ((piece ^ (row & 7)) << 2)) =
-                    make_float4(st.o[d][4 * e], st.o[d][4 * e + 1], st.o[d][4 * e + 2], st.o[d][4 * e + 3]);
-            }
-        if (lane < 32) stats[wave * 32 + lane] = st.base, stats[128 + wave * 32 + lane] = st.sum;
-        __syncthreads();
-        const int row = tid >> 3, part = tid & 7;
-        const bool direct = whole && (p.P == 0 || plan.mode == SOLO);
-        const int slot = item + w;
-        if (r0 + row < rows && (direct || slot < p.narrow_blocks)) {
-            float base = -INFINITY, f[4], sum = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) base = fmaxf(base, stats[k * 32 + row]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                f[k] = base == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stats[k * 32 + row] - base);
-                sum += f[k] * stats[128 + k * 32 + row];
-            }
-            const float inv = !direct ? 1.0f : sum > 0.0f ? 1.0f / sum : 0.0f;
-            const int to = (r0 + row) / p.G, head = h * p.G + (r0 + row - to * p.G);
-            const int64_t t = rq.q0 + to;
-            uint8_t* blk = p.blocks + (p.joint_blocks + p.packed_blocks + slot) * block_bytes<D>();
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k) {
-                const int piece = k * 8 + part;
-                float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const float4 z = *reinterpret_cast<const float4*>(parts + v * 32 * D + row * D + ((piece ^ (row & 7)) << 2));
-                    y[0] = fmaf(f[v], z.x, y[0]), y[1] = fmaf(f[v], z.y, y[1]), y[2] = fmaf(f[v], z.z, y[2]), y[3] = fmaf(f[v], z.w, y[3]);
-                }
-                if (direct) {
-                    *reinterpret_cast<uint2*>(p.O + t * p.ldo + head * D + piece * 4) = make_uint2(pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv));
-                } else {
-                    *reinterpret_cast<float4*>(blk + (row * D + piece * 4) * 4) = make_float4(y[0], y[1], y[2], y[3]);
-                }
-            }
-            if (part == 0) {
-                if (!direct) *reinterpret_cast<float2*>(blk + (32 * D + row * 2) * 4) = make_float2(base, sum);
-                else if (p.lse) p.lse[t * p.Hq + head] = lse_of(base, sum);
-            }
-        }
-        lds_barrier();
+        const bool direct = whole && p.P == 0;
+        const int slot = item + w, row = lane & 31;
+        if (r0 + row < rows && (direct || slot < p.narrow_blocks))
+            leave<D>(p, st, direct, (int64_t)ti, h * p.G + g, p.blocks + (p.joint_blocks + p.packed_blocks + slot) * block_bytes<D>(), row, lane >> 5);
     }
 }
 
@@ -725,30 +695,8 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
         }
         st.sum = half_sum(st.sum);
         const bool direct = whole && b >= 0;
-        const int hi = lane >> 5;
-        if (r < rows) {
-            if (direct) {
-                const float inv = st.sum > 0.0f ? 1.0f / st.sum : 0.0f;
-                uint16_t* out = p.O + (int64_t)ti * p.ldo + (h * p.G + g) * D;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<uint2*>(out + 32 * d + 8 * e + 4 * hi) =
-                            make_uint2(pack2(st.o[d][4 * e] * inv, st.o[d][4 * e + 1] * inv), pack2(st.o[d][4 * e + 2] * inv, st.o[d][4 * e + 3] * inv));
-                if (p.lse && hi == 0) p.lse[(int64_t)ti * p.Hq + h * p.G + g] = lse_of(st.base, st.sum);
-            } else if (slot + 4 <= p.joint_blocks + (b < 0 ? p.packed_blocks : 0)) {
-                uint8_t* blk = p.blocks + (slot + wave) * block_bytes<D>();
-                const int row = lane & 31;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<float4*>(blk + (row * D + 32 * d + 8 * e + 4 * hi) * 4) =
-                            make_float4(st.o[d][4 * e], st.o[d][4 * e + 1], st.o[d][4 * e + 2], st.o[d][4 * e + 3]);
-                if (hi == 0) *reinterpret_cast<float2*>(blk + (32 * D + row * 2) * 4) = make_float2(st.base, st.sum);
-            }
-        }
+        if (r < rows && (direct || slot + 4 <= p.joint_blocks + (b < 0 ? p.packed_blocks : 0)))
+            leave<D>(p, st, direct, (int64_t)ti, h * p.G + g, p.blocks + (slot + wave) * block_bytes<D>(), lane & 31, lane >> 5);
         lds_barrier();  // the next item's first block lands where others may still be reading this one's last
         stop = x;
     }
@@ -756,8 +704,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
 
 struct AttnShared {
     Sums sums;
-    int part[4][6];
-    float stats[256];
+    int part[4][5];
 };
 
 template <int D>
@@ -765,21 +712,18 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     AttnShared& sh = *reinterpret_cast<AttnShared*>(lds + 8 * 32 * D * 2);  // behind the tiles, which start at 0
     Sums& sums = sh.sums;
-    float* stats = sh.stats;
     auto& part = sh.part;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int T = (int)p.T;
     constexpr int NV = 5;  // narrow, narrow rounded up, items, rows, wide
     int mine[NV] = {0, 0, 0, 0, 0}, v[NV], total[NV];
-    bool wrong = false, few = true, many = true;  // no more than SOLO_FEW, SOLO_MANY tokens
+    bool wrong = false;
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
     for (int b = b0; b < b1; ++b) {
         const Request r = request(p, b);
         wrong |= r.q0 < 0 || r.n < 0 || r.q0 > T - r.n;
         if (wrong) break;
         const Extent e = extent(p, r, CUT);
-        const int sees = is_long(p, r.n) ? SOLO_MANY + 1 : p.P + r.L;
-        few &= sees <= SOLO_FEW, many &= sees <= SOLO_MANY;
         mine[0] += e.narrow, mine[1] += e.items * narrow_length(p, r.L, ALIGNED), mine[2] += e.items, mine[3] += e.rows, mine[4] += e.wide;
     }
 #pragma unroll
@@ -794,8 +738,6 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     if (lane == 63)
 #pragma unroll
         for (int k = 0; k < NV; ++k) part[wave][k] = v[k];
-    const int small = (__ballot(!few) == 0) + 2 * (__ballot(!many) == 0);
-    if (lane == 0) part[wave][NV] = small;
     if (__syncthreads_or(wrong)) {  // offsets that fall or name rows that are not there: nothing is read or written
         if (blockIdx.x == 0 && tid == 0) p.plan->valid = 0;
         return;
@@ -810,9 +752,8 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
             total[k] += part[u][k];
         }
     }
-    const int all_small = uni(part[0][NV] & part[1][NV] & part[2][NV] & part[3][NV]);
-    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), all_small);
-    if (plan.mode != CUT) v[0] = plan.mode == ALIGNED ? v[1] : v[2];
+    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]));
+    if (plan.mode == ALIGNED) v[0] = v[1];
     sums.narrow[tid] = v[0], sums.items[tid] = v[2], sums.rows[tid] = v[3], sums.wide[tid] = v[4];
     if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
         if (tid == 0) *p.plan = plan;
@@ -833,8 +774,10 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     const bool with_wide = i < run, swap = blockIdx.x >= N / 2;
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
-        if ((turn == 0) == swap) narrow_piece<D>(p, plan, sums, lds, stats, (int)blockIdx.x);
-        else if (with_wide) wide_piece<D>(p, plan, sums, lds, xcd * run + i);
+        if ((turn == 0) == swap) {
+            narrow_piece<D>(p, plan, sums, lds);
+            if (turn == 0 && with_wide) lds_barrier();  // the tiles of both are in the same place
+        } else if (with_wide) wide_piece<D>(p, plan, sums, lds, xcd * run + i);
     }
 }
 
@@ -852,7 +795,7 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
     if (t >= p.T) return;
     const int head0 = (int)(unit - (int64_t)t * per_token) * H;
     const Plan plan = *p.plan;
-    if (!plan.valid || plan.mode == SOLO) return;
+    if (!plan.valid || !plan.joins) return;
     int lo = 0, hi = p.B + 1;  // the last request that starts at or before t
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64, at = lo + lane * step;
@@ -990,7 +933,7 @@ static AttnSpace attn_space(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32
     a.joint = rows >= (P ? LONG_PREFIX : LONG) ? 2 * wgs * 4 : 0;
     const int64_t tiles = (is_short + WROWS - 1) / WROWS;
     a.packed = is_short > 32 ? (std::max(Hkv * tiles * super_count(P, tiles), wgs) + wgs) * 4 : 0;
-    a.narrow = Hkv * (1 + (P ? is_short / 32 + some : some)) + wgs;
+    a.narrow = Hkv * (1 + (P ? is_short / 32 + some : some)) + 4 * wgs;
     a.records = 256;
     a.blocks = align_up(a.records + (size_t)B * 16, 256);
     a.total = a.blocks + (size_t)(a.joint + a.packed + a.narrow) * (32 * (D + 2) * 4);
@@ -1009,7 +952,7 @@ static int launch(const AttnArgs& p, hipStream_t st) {
     if (rc) return rc;
     prefix_attention_kernel<D><<<dim3(attn_wgs<D>()), WG, lds, st>>>(p);
     // a wavefront a row while the card holds them at once, four rows beyond that
-    const bool few = p.T * p.Hq <= 8192;
+    const bool few = p.T * p.Hq <= 4096;
     const int64_t wgs = (p.T * (few ? p.Hq : (p.Hq + 3) / 4) + 3) / 4;
     if (few) prefix_attention_join_kernel<D, 1><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
     else prefix_attention_join_kernel<D, 4><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
