@@ -30,15 +30,18 @@ constexpr int WG = 256, WROWS = 128, GROUPS = 256;
 // Workgroups: two on a CU (LDS for their tiles), three where heads are small.
 template <int D>
 constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
+// The narrow line is cut where pieces end (CUT), or its items are rounded up to whole pieces of one of these lengths.
+enum { CUT = 0 };
+constexpr int PIECE1 = 3, PIECE2 = 6, PIECE3 = 12;
+// Short requests walk the prefix themselves, tile after tile of their own items, where that is no more than this many tiles a wavefront
+constexpr int INLINE_TILES = 6;
 // The line of 32-row tiles is measured in tiles of 32 tokens, that of 128-row tiles in tokens.  Starting and ending a segment costs
 // about as much as the EDGEs; no piece is smaller than the MINs (MIN_WIDE where workgroups have little to do, and twice that where
 // they have more than 16 narrow tiles each: us with 256 against 512, 32 heads on 8, 32 requests behind 1000 tokens 21.0 / 25.4, 20 behind
 // 9000 26.0 / 28.5; 100 behind 3000 40.7 / 37.0, 64 behind 8192 with 400 of their own 53.9 / 45.4).
-constexpr int NARROW_EDGE = 2, MIN_NARROW = 4, WIDE_EDGE = 128, MIN_WIDE = 256;
+constexpr int NARROW_EDGE = 1, MIN_NARROW = PIECE1, WIDE_EDGE = 128, MIN_WIDE = 256;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
 constexpr int LONG_PREFIX = 256, LONG = 33;  // rows of a long request, with a prefix and without
-// The narrow line is cut where pieces end, or its items are rounded up to whole pieces.
-enum { CUT = 0, ALIGNED = 1 };
 
 struct AttnArgs {
     const uint16_t* Q;
@@ -54,6 +57,7 @@ struct AttnArgs {
     int max_kv;  // tokens that a row of the table can name
     const int32_t *kv_lens, *q_offsets;
     int B, per;  // per: requests of a group
+    int pre_tiles;  // tiles of the prefix that short requests' items start with, or 0: their rows are packed
     int ns, ws;  // a step on the line of 32-row (128-row) tiles is 2^ns (2^ws) of its units: 0 unless the lines could pass 2^30
     float c;     // scale * log2(e): scores leave the matrix core unscaled, and powers are of two
     uint16_t* O;
@@ -87,10 +91,10 @@ __device__ __forceinline__ Request request(const AttnArgs& p, int b) {
 }
 __device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? LONG_PREFIX : LONG); }
 __device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (n * p.G + 31) >> 5; }
-__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int mode) {
-    const int n = (((L + 31) >> 5) + NARROW_EDGE + (1 << p.ns) - 1) >> p.ns;
-    return mode == ALIGNED ? (n + MIN_NARROW - 1) / MIN_NARROW * MIN_NARROW : n;
-}
+// `piece`: CUT or the length that items are rounded up to
+__device__ __forceinline__ int narrow_units(const AttnArgs& p, int L) { return (((L + 31) >> 5) + NARROW_EDGE + (1 << p.ns) - 1) >> p.ns; }
+__device__ __forceinline__ int rounded(int n, int piece) { return piece ? (n + piece - 1) / piece * piece : n; }
+__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int piece) { return rounded(narrow_units(p, L) + p.pre_tiles, piece); }
 __device__ __forceinline__ int narrow_tile(const AttnArgs& p, int y) { return max(0, (y << p.ns) - NARROW_EDGE); }  // the first tile at place y of an item
 // the first k tiles of a long request on their line: each sees `seen` and a tile's tokens more than the one before it
 __device__ __forceinline__ int wide_sum(const AttnArgs& p, int seen, int k) { return k * seen + (p.tpt >> p.ws) * (k * (k + 1) / 2); }
@@ -98,15 +102,15 @@ __device__ __forceinline__ int wide_seen(const AttnArgs& p, const Request& r) { 
 __device__ __forceinline__ int wide_length(const AttnArgs& p, int seen, int tile) { return seen + (tile + 1) * (p.tpt >> p.ws); }
 __device__ __forceinline__ int wide_tiles(const AttnArgs& p, int n) { return (n + p.tpt - 1) / p.tpt; }
 __device__ __forceinline__ int packed_length(const AttnArgs& p, int blocks) { return ((blocks * 64 + WIDE_EDGE) >> p.ws) + 1; }
-__device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, int mode) {
+__device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, int piece) {
     Extent e{0, 0, 0, 0};
     if (r.n == 0) return e;
     if (is_long(p, r.n)) {
         e.wide = p.Hkv * wide_sum(p, wide_seen(p, r), wide_tiles(p, r.n));
     } else {
         e.items = narrow_tiles(p, r.n) * p.Hkv;
-        e.narrow = e.items * narrow_length(p, r.L, mode);
-        if (p.P) e.rows = r.n * p.G;
+        e.narrow = e.items * narrow_length(p, r.L, piece);
+        if (p.P && !p.pre_tiles) e.rows = r.n * p.G;
     }
     return e;
 }
@@ -115,13 +119,14 @@ __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, in
 // Wide pieces are equal; the first `with_wide` workgroups have one.  A narrow piece is a wavefront's: those of these workgroups take
 // pieces of length `a`, the others of length `b`, so that all have the same to do: a wide block of 64 tokens takes about a third
 // of the time of a narrow tile (2 us where a CU has two workgroups at it; 16 KB, 6 us where all wavefronts share 5.5 TB/s).  Where there are
-// more wavefronts than pieces of the least length, items are rounded up to whole pieces (ALIGNED): no wavefront has parts of two.
+// wavefronts enough for pieces of 3, 6 or 12 tiles, items are rounded up to whole ones: a wavefront has parts of one item, and most
+// items are in one piece.
 struct Plan {
     int narrow, wide;      // lengths of the lines
     int narrow0, items0;   // of which the prefix's narrow items are the first
     int wide0, head;       // of which the packed tiles are the first, `head` for every key/value head
     int wide_per, a, b, cut;
-    int with_wide, mode;
+    int with_wide, piece;
     int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; pieces of the prefix, blocks of 64 tokens in one, in the prefix
     int valid;  // offsets are in order
     int joins;  // anything to join
@@ -132,7 +137,7 @@ __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
     return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
 }
 template <int D>
-__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rounded, int items, int rows, int wide) {
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int pieces1, int pieces2, int pieces3, int items, int rows, int wide) {
     constexpr int N = attn_wgs<D>(), WAVES = 4 * N;
     Plan a;
     a.valid = 1;
@@ -140,15 +145,15 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rou
     a.nbp = (p.P + 63) >> 6;
     a.narrow0 = a.items0 = a.wide0 = a.head = 0;
     a.tiles = a.supers = a.super = 0;
-    const bool narrow_prefix = rows > 0 && rows <= 32;
-    if (narrow_prefix) rounded += p.Hkv * narrow_length(p, p.P, ALIGNED);
-    a.mode = rounded <= WAVES * MIN_NARROW ? ALIGNED : CUT;
-    if (a.mode == ALIGNED) narrow = rounded;
-    if (narrow_prefix) {
+    if (rows > 0 && rows <= 32) {
+        const int n = narrow_units(p, p.P);
         a.items0 = p.Hkv;
-        a.narrow0 = p.Hkv * narrow_length(p, p.P, a.mode);
-        if (a.mode == CUT) narrow += a.narrow0;
+        narrow += p.Hkv * n;
+        pieces1 += p.Hkv * ((n + PIECE1 - 1) / PIECE1), pieces2 += p.Hkv * ((n + PIECE2 - 1) / PIECE2), pieces3 += p.Hkv * ((n + PIECE3 - 1) / PIECE3);
     }
+    a.piece = pieces1 <= WAVES ? PIECE1 : pieces2 <= WAVES ? PIECE2 : pieces3 <= WAVES ? PIECE3 : CUT;
+    if (a.piece) narrow = a.piece * (a.piece == PIECE1 ? pieces1 : a.piece == PIECE2 ? pieces2 : pieces3);
+    if (a.items0) a.narrow0 = p.Hkv * rounded(narrow_units(p, p.P), a.piece);
     a.wide_per = 0;
     if (rows > 32) {
         a.tiles = (rows + WROWS - 1) / WROWS;
@@ -170,11 +175,11 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int rou
     const int cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 16)) >> p.ns, (int64_t)1 << 18);
     a.b = (narrow + WAVES - 1) / WAVES + (with * cost + WAVES - 1) / WAVES;
     a.a = a.b - cost;
-    if (others == 0) a.a = max((narrow + WAVES - 1) / WAVES, MIN_NARROW);
-    else if (a.mode == ALIGNED) a.b = MIN_NARROW, a.a = others * MIN_NARROW >= narrow ? 0 : MIN_NARROW;
+    if (others == 0) a.a = a.piece ? a.piece : max((narrow + WAVES - 1) / WAVES, MIN_NARROW);
+    else if (a.piece) a.b = a.piece, a.a = others * a.piece >= narrow ? 0 : a.piece;
     else if (a.a < MIN_NARROW) a.a = 0, a.b = max((narrow + others - 1) / others, MIN_NARROW);
     a.cut = a.a * with;
-    a.joins = p.P || wide || a.mode == CUT || narrow > items * MIN_NARROW;
+    a.joins = a.wide > 0 || a.items0 > 0 || !a.piece || narrow > items * a.piece;
     return a;
 }
 // the wavefront (in the order of the pieces) that has place x of the narrow line
@@ -193,13 +198,13 @@ __device__ __forceinline__ int find_group(const int (&sums)[GROUPS], int x, int 
 }
 // The request that holds place x of a line: its number and what is before it.  All lanes of a wavefront take part.
 template <bool WIDE>
-__device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, int mode, int x, int lane, Extent& before) {
+__device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, int piece, int x, int lane, Extent& before) {
     const int g = uni(find_group(WIDE ? s.wide : s.narrow, x, lane));
     before = Extent{uni(s.narrow[g]), uni(s.items[g]), uni(s.rows[g]), uni(s.wide[g])};
     int b = g * p.per;
     if (p.per > 1) {  // at most 32 requests of a group: one a lane
         Extent e{0, 0, 0, 0};
-        if (lane < p.per && b + lane < p.B) e = extent(p, request(p, b + lane), mode);
+        if (lane < p.per && b + lane < p.B) e = extent(p, request(p, b + lane), piece);
         Extent sum = e;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -470,28 +475,27 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
     const int end = min(x + (w < with ? plan.a : plan.b), plan.narrow);
     while (x < end) {
         // the item at x: its start and length on the line, its rows, its tokens
-        int start, item, length, h, r0, rows, tokens, seen, clear_to, b = -1;
+        int start, item, length, h, r0, rows, n_prefix, tokens = 0, seen = 0, clear_to = 0, b = -1;  // tiles of the prefix, then own tokens
         Request rq{0, 0, 0};
-        const int32_t* pages;
         if (x < plan.narrow0) {
-            length = narrow_length(p, p.P, plan.mode);
+            length = rounded(narrow_units(p, p.P), plan.piece);
             h = x / length;
             start = h * length, item = h;
-            r0 = 0, rows = plan.rows, tokens = clear_to = seen = p.P, pages = p.prefix_pages;
+            r0 = 0, rows = plan.rows, n_prefix = (p.P + 31) >> 5;
         } else {
             Extent before;
-            b = find_request<false>(p, sums, plan.mode, x - plan.narrow0, lane, before);
+            b = find_request<false>(p, sums, plan.piece, x - plan.narrow0, lane, before);
             rq = request(p, b);
-            length = narrow_length(p, rq.L, plan.mode);
+            length = narrow_length(p, rq.L, plan.piece);
             const int nt = narrow_tiles(p, rq.n), k = (x - plan.narrow0 - before.narrow) / length;
             start = plan.narrow0 + before.narrow + k * length, item = plan.items0 + before.items + k;
             h = k / nt;
             r0 = (k - h * nt) * 32, rows = rq.n * p.G;
             tokens = max(0, rq.L - rq.n + min(r0 + 31, rows - 1) / p.G + 1), clear_to = rq.L - rq.n + r0 / p.G + 1;
-            pages = p.table + (int64_t)b * p.ldt;
+            n_prefix = p.pre_tiles;
         }
         const int stop = min(end, start + length);
-        const int t0 = narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), (tokens + 31) >> 5);
+        const int t0 = narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), n_prefix + ((tokens + 31) >> 5));
         const bool whole = x == start && stop == start + length;
         x = stop;
 
@@ -511,14 +515,17 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
         State<D> st;
         clear(st);
         auto runs = [&](int tile, const uint8_t*& a, const uint8_t*& c) {
-            const int j = tile * 32, j2 = min(j + 16, tokens - 1), one = pages[j >> p.lg], two = pages[j2 >> p.lg];
+            const bool pre = tile < n_prefix;
+            const int32_t* pages = pre ? p.prefix_pages : p.table + (int64_t)b * p.ldt;
+            const int j = (pre ? tile : tile - n_prefix) * 32, j2 = min(j + 16, (pre ? p.P : tokens) - 1), one = pages[j >> p.lg], two = pages[j2 >> p.lg];
             a = run_of<D>(p, one, h, j);
             c = run_of<D>(p, two, h, j2);
         };
         auto fetch = [&](int tile, const uint8_t* a, const uint8_t* c, int64_t shift, uint32_t dst) {
-            const int left = tokens - 1 - tile * 32;
+            const bool pre = tile < n_prefix;
+            const int last = (pre ? p.P : tokens) - 1, left = last - (pre ? tile : tile - n_prefix) * 32;
             fetch16<D>(a + shift, 0, min(left, 15), dst, lane);
-            fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : (tokens - 1) & 15, dst, lane);
+            fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : last & 15, dst, lane);
         };
         int tile = t0;
         const uint8_t *ra = nullptr, *rb = nullptr, *na = nullptr, *nb = nullptr;
@@ -538,8 +545,9 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             lds_order();
             __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the keys are read
             if (more) fetch(tile + 1, na, nb, 0, kt);
-            const int j0 = tile * 32;
-            if (j0 + 32 > clear_to) mask<1>(s, lane, seen - j0);
+            const bool pre = tile < n_prefix;
+            const int j0 = (pre ? tile : tile - n_prefix) * 32;
+            if (j0 + 32 > (pre ? p.P : clear_to)) mask<1>(s, lane, (pre ? p.P : seen) - j0);
             weigh<D, 1>(st, s, p.c);
             if (more) wait_vmcnt<NI>();
             else wait_vmcnt<0>();
@@ -552,7 +560,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             if (more) fetch(tile + 1, na, nb, to_v, vt);
         }
         st.sum = half_sum(st.sum);
-        const bool direct = whole && p.P == 0;
+        const bool direct = whole && (p.P == 0 || p.pre_tiles);
         const int slot = item + w, row = lane & 31;
         if (r0 + row < rows && (direct || slot < p.narrow_blocks))
             leave<D>(p, st, direct, (int64_t)ti, h * p.G + g, p.blocks + (p.joint_blocks + p.packed_blocks + slot) * block_bytes<D>(), row, lane >> 5);
@@ -704,7 +712,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
 
 struct AttnShared {
     Sums sums;
-    int part[4][5];
+    int part[4][7];
 };
 
 template <int D>
@@ -715,8 +723,8 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     auto& part = sh.part;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int T = (int)p.T;
-    constexpr int NV = 5;  // narrow, narrow rounded up, items, rows, wide
-    int mine[NV] = {0, 0, 0, 0, 0}, v[NV], total[NV];
+    constexpr int NV = 7;  // narrow, pieces of the three lengths, items, rows, wide
+    int mine[NV] = {0, 0, 0, 0, 0, 0, 0}, v[NV], total[NV];
     bool wrong = false;
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
     for (int b = b0; b < b1; ++b) {
@@ -724,7 +732,9 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
         wrong |= r.q0 < 0 || r.n < 0 || r.q0 > T - r.n;
         if (wrong) break;
         const Extent e = extent(p, r, CUT);
-        mine[0] += e.narrow, mine[1] += e.items * narrow_length(p, r.L, ALIGNED), mine[2] += e.items, mine[3] += e.rows, mine[4] += e.wide;
+const int n = narrow_length(p, r.L, CUT);
+        mine[0] += e.narrow, mine[4] += e.items, mine[5] += e.rows, mine[6] += e.wide;
+        mine[1] += e.items * ((n + PIECE1 - 1) / PIECE1), mine[2] += e.items * ((n + PIECE2 - 1) / PIECE2), mine[3] += e.items * ((n + PIECE3 - 1) / PIECE3);
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) v[k] = mine[k];
@@ -752,16 +762,16 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
             total[k] += part[u][k];
         }
     }
-    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]));
-    if (plan.mode == ALIGNED) v[0] = v[1];
-    sums.narrow[tid] = v[0], sums.items[tid] = v[2], sums.rows[tid] = v[3], sums.wide[tid] = v[4];
+    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), uni(total[5]), uni(total[6]));
+    if (plan.piece) v[0] = plan.piece * (plan.piece == PIECE1 ? v[1] : plan.piece == PIECE2 ? v[2] : v[3]);
+    sums.narrow[tid] = v[0], sums.items[tid] = v[4], sums.rows[tid] = v[5], sums.wide[tid] = v[6];
     if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
         if (tid == 0) *p.plan = plan;
         for (int b = b0; b < b1; ++b) {
-            const Extent e = extent(p, request(p, b), plan.mode);
+            const Extent e = extent(p, request(p, b), plan.piece);
             int* r = p.records + (int64_t)b * 4;
-            r[0] = v[0], r[1] = v[2], r[2] = v[3], r[3] = v[4];
-            v[0] += e.narrow, v[2] += e.items, v[3] += e.rows, v[4] += e.wide;
+            r[0] = v[0], r[1] = v[4], r[2] = v[5], r[3] = v[6];
+            v[0] += e.narrow, v[4] += e.items, v[5] += e.rows, v[6] += e.wide;
         }
     }
     __syncthreads();
@@ -811,7 +821,7 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
     if (i < 0 || i >= rq.n) return;
     const int* rec = p.records + (int64_t)b * 4;
     const bool joint = is_long(p, rq.n);
-    const int cp = narrow_length(p, p.P, plan.mode), packed_item = packed_length(p, plan.super);
+    const int cp = rounded(narrow_units(p, p.P), plan.piece), packed_item = packed_length(p, plan.super);
     const int pre_pieces = packed_item == plan.wide_per ? 1 : plan.tiles ? (packed_item - 1) / plan.wide_per + 2 : 0;  // of a piece of the prefix, at most
 
     // this lane's row: `own` segments of its request's tile, the first at `first`; then up to `more` of the prefix
@@ -825,15 +835,15 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         own = (s0 + wide_length(p, seen, tile) - 1) / plan.wide_per - first + 1;
         row = r - tile * p.tpt * p.G;
     } else {
-        const int length = narrow_length(p, rq.L, plan.mode);
+        const int length = narrow_length(p, rq.L, plan.piece);
         const int k = h * narrow_tiles(p, rq.n) + r / 32, s0 = plan.narrow0 + rec[0] + k * length;
         first = narrow_piece_of(plan, s0);
         own = narrow_piece_of(plan, s0 + length - 1) - first + 1;
         row = r & 31;
         first += plan.items0 + rec[1] + k;  // its block in the narrow part
-        if (p.P) more = plan.tiles ? plan.supers * pre_pieces : narrow_piece_of(plan, (h + 1) * cp - 1) - narrow_piece_of(plan, h * cp) + 1;
+        if (p.P && !p.pre_tiles) more = plan.tiles ? plan.supers * pre_pieces : narrow_piece_of(plan, (h + 1) * cp - 1) - narrow_piece_of(plan, h * cp) + 1;
     }
-    const bool done = own == 1 && more == 0 && (joint || p.P == 0);  // written by the first kernel
+    const bool done = own == 1 && more == 0 && (joint || p.P == 0 || p.pre_tiles);  // written by the first kernel
     const int count = done ? 0 : own + more;
     int most = count;
 #pragma unroll
@@ -922,18 +932,23 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------------
+// Tiles of the prefix that short requests' items start with: all of them, or none where that would be too many.
+static int inline_tiles(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t P) {
+    const int64_t items = Hkv * (T * (Hq / Hkv) / 32 + std::min<int64_t>(B, T)), waves = 4 * (D == 128 ? attn_wgs<128>() : attn_wgs<64>());
+    return P && items * ((P + 31) / 32) <= INLINE_TILES * waves ? (int)((P + 31) / 32) : 0;
+}
 struct AttnSpace {
     int64_t joint, packed, narrow;  // blocks
     size_t records, blocks, total;  // offsets
 };
 static AttnSpace attn_space(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t P) {
     const int64_t G = Hq / Hkv, rows = T * G, wgs = D == 128 ? attn_wgs<128>() : attn_wgs<64>(), some = std::min<int64_t>(B, T);
-    const int64_t is_short = P ? std::min<int64_t>(rows, (LONG_PREFIX - 1) * (int64_t)B) : 0;  // rows that walk the prefix packed, at most
+    const int64_t is_short = P && !inline_tiles(T, B, Hq, Hkv, D, P) ? std::min<int64_t>(rows, (LONG_PREFIX - 1) * (int64_t)B) : 0;  // rows that walk the prefix packed, at most
     AttnSpace a;
     a.joint = rows >= (P ? LONG_PREFIX : LONG) ? 2 * wgs * 4 : 0;
     const int64_t tiles = (is_short + WROWS - 1) / WROWS;
     a.packed = is_short > 32 ? (std::max(Hkv * tiles * super_count(P, tiles), wgs) + wgs) * 4 : 0;
-    a.narrow = Hkv * (1 + (P ? is_short / 32 + some : some)) + 4 * wgs;
+    a.narrow = Hkv * (1 + (P ? std::min<int64_t>(rows, (LONG_PREFIX - 1) * (int64_t)B) / 32 + some : some)) + 4 * wgs;
     a.records = 256;
     a.blocks = align_up(a.records + (size_t)B * 16, 256);
     a.total = a.blocks + (size_t)(a.joint + a.packed + a.narrow) * (32 * (D + 2) * 4);
@@ -968,6 +983,7 @@ int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
     p.max_kv = (int)std::min<int64_t>(a.ldt << a.lg, 0x3fffffff);
     p.kv_lens = a.kv_lens, p.q_offsets = a.q_offsets, p.B = a.B, p.per = (a.B + GROUPS - 1) / GROUPS, p.c = a.scale * 1.44269504088896341f;
     p.O = static_cast<uint16_t*>(a.O), p.ldo = a.ldo, p.lse = a.lse;
+    p.pre_tiles = inline_tiles(a.T, a.B, a.Hq, a.Hkv, a.D, a.prefix_len);
     const AttnSpace s = attn_space(a.T, a.B, a.Hq, a.Hkv, a.D, a.prefix_len);
     p.plan = reinterpret_cast<Plan*>(a.workspace), p.records = reinterpret_cast<int*>(a.workspace + s.records);
     p.blocks = a.workspace + s.blocks;
@@ -976,7 +992,7 @@ int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
     const int64_t rows = a.T * p.G, is_long = rows / (p.P ? LONG_PREFIX : LONG), tiles = rows / WROWS + 1, some = std::min<int64_t>(a.B, a.T);
     const int64_t wide = (int64_t)p.Hkv * (a.T / p.tpt + is_long) * (WIDE_EDGE + p.P + (int64_t)p.max_kv + a.T + WROWS) +
                          (int64_t)p.Hkv * tiles * 2 * (p.P + (WIDE_EDGE + 64) * MAX_SUPER);
-    const int64_t narrow = (int64_t)p.Hkv * (rows / 32 + some + 1) * (std::max<int64_t>(p.P, p.max_kv) / 32 + NARROW_EDGE + 2 * MIN_NARROW);
+    const int64_t narrow = (int64_t)p.Hkv * (rows / 32 + some + 1) * (std::max<int64_t>(p.P, p.max_kv) / 32 + p.pre_tiles + NARROW_EDGE + PIECE3 + 1);
     for (p.ws = 0; wide >> p.ws > 1 << 30;) ++p.ws;
     for (p.ns = 0; narrow >> p.ns > 1 << 30;) ++p.ns;
     return a.D == 64 ? launch<64>(p, st) : launch<128>(p, st);

@@ -302,6 +302,26 @@ def test_attention_long_prefix(osc):
     check_attention(osc, make(12, 40, 4097, kv, n, 6, 1, 128, 128))
 
 
+@pytest.mark.parametrize("D,P", [(128, 6500), (64, 9001)])
+def test_attention_few_rows_behind_a_long_prefix(osc, D, P):
+    """the rows of all requests in one tile of 32 that walks the prefix"""
+    check_attention(osc, make(31, 8, P, [5, 200, 33, 1, 64, 90, 17, 40], [1] * 8, 32, 8, D, 64))
+    check_attention(osc, make(32, 7, P, [5, 200, 33, 1, 64, 90, 17], [1, 1, 0, 1, 1, 1, 1], 24, 8, D, 128))
+
+
+@pytest.mark.parametrize("D,P,Hq,Hkv", [(128, 700, 4, 2), (64, 1300, 6, 1), (128, 4100, 8, 8), (64, 4999, 5, 1)])
+def test_attention_packed_rows(osc, D, P, Hq, Hkv):
+    """the rows of many requests in tiles of 128 that walk the prefix; idle requests between them, and long ones that walk it themselves"""
+    gen = np.random.default_rng(P)
+    B = 600 if Hkv == 1 else 300 if Hkv == 2 else 60
+    n, kv = np.ones(B, int), gen.integers(1, 90, B)
+    n[gen.random(B) < 0.1] = 0
+    check_attention(osc, make(33, B, P, kv.tolist(), n.tolist(), Hq, Hkv, D, 32))
+    n[5], kv[5] = 9, 12
+    n[B // 2], kv[B // 2] = 256 * Hkv // Hq + 3, 300
+    check_attention(osc, make(34, B, P, np.maximum(kv, n).tolist(), n.tolist(), Hq, Hkv, D, 16))
+
+
 def test_attention_prompts(osc):
     check_attention(osc, make(13, 2, 100, [500, 410], [500, 300], 4, 2, 128, 16))
     check_attention(osc, make(14, 3, 0, [333, 1, 700], [333, 1, 200], 5, 1, 64, 32))
