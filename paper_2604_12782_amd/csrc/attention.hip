@@ -30,9 +30,11 @@ constexpr int WG = 256, WROWS = 128, GROUPS = 256;
 // Workgroups: two on a CU (LDS for their tiles), three where heads are small.
 template <int D>
 constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
-// The narrow line is cut where pieces end (CUT), or its items are rounded up to whole pieces of one of these lengths.
-enum { CUT = 0 };
-constexpr int PIECE1 = 3, PIECE2 = 6, PIECE3 = 12;
+// The narrow line is cut where pieces end (CUT), or its items are rounded up to whole pieces of one of these lengths, or (SOLO) a workgroup has
+// one item and nothing is joined: where there is no wide work, no more items than workgroups, and no request sees more than
+// SOLO_FEW tokens, or SOLO_MANY where a quarter of the workgroups or more have an item.
+enum { CUT = 0, SOLO = -1 };
+constexpr int PIECE1 = 3, PIECE2 = 6, PIECE3 = 12, SOLO_FEW = 512, SOLO_MANY = 1024;
 // Short requests walk the prefix themselves, tile after tile of their own items, where that is no more than this many tiles a wavefront
 constexpr int INLINE_TILES = 6;
 // The line of 32-row tiles is measured in tiles of 32 tokens, that of 128-row tiles in tokens.  Starting and ending a segment costs
@@ -94,7 +96,7 @@ __device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (
 // `piece`: CUT or the length that items are rounded up to
 __device__ __forceinline__ int narrow_units(const AttnArgs& p, int L) { return (((L + 31) >> 5) + NARROW_EDGE + (1 << p.ns) - 1) >> p.ns; }
 __device__ __forceinline__ int rounded(int n, int piece) { return piece ? (n + piece - 1) / piece * piece : n; }
-__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int piece) { return rounded(narrow_units(p, L) + p.pre_tiles, piece); }
+__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int piece) { return piece == SOLO ? 1 : rounded(narrow_units(p, L) + p.pre_tiles, piece); }
 __device__ __forceinline__ int narrow_tile(const AttnArgs& p, int y) { return max(0, (y << p.ns) - NARROW_EDGE); }  // the first tile at place y of an item
 // the first k tiles of a long request on their line: each sees `seen` and a tile's tokens more than the one before it
 __device__ __forceinline__ int wide_sum(const AttnArgs& p, int seen, int k) { return k * seen + (p.tpt >> p.ws) * (k * (k + 1) / 2); }
@@ -117,7 +119,7 @@ __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, in
 
 // What follows from the totals: the prefix's items, which come first on their line, and the pieces.
 // Wide pieces are equal; the first `with_wide` workgroups have one.  A narrow piece is a wavefront's: those of these workgroups take
-// pieces of length `a`, the others of length `b`, so that all have the same to do: a wide block of 64 tokens takes about a third
+// pieces of length `a`, the others, which come first on the line, of length `b`, so that all have the same to do: a wide block of 64 tokens takes about a third
 // of the time of a narrow tile (2 us where a CU has two workgroups at it; 16 KB, 6 us where all wavefronts share 5.5 TB/s).  Where there are
 // wavefronts enough for pieces of 3, 6 or 12 tiles, items are rounded up to whole ones: a wavefront has parts of one item, and most
 // items are in one piece.
@@ -126,7 +128,7 @@ struct Plan {
     int narrow0, items0;   // of which the prefix's narrow items are the first
     int wide0, head;       // of which the packed tiles are the first, `head` for every key/value head
     int wide_per, a, b, cut;
-    int with_wide, piece;
+    int with_wide, others, piece;
     int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; pieces of the prefix, blocks of 64 tokens in one, in the prefix
     int valid;  // offsets are in order
     int joins;  // anything to join
@@ -137,7 +139,7 @@ __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
     return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
 }
 template <int D>
-__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int pieces1, int pieces2, int pieces3, int items, int rows, int wide) {
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int pieces1, int pieces2, int pieces3, int items, int rows, int wide, int small) {
     constexpr int N = attn_wgs<D>(), WAVES = 4 * N;
     Plan a;
     a.valid = 1;
@@ -151,8 +153,12 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int pie
         narrow += p.Hkv * n;
         pieces1 += p.Hkv * ((n + PIECE1 - 1) / PIECE1), pieces2 += p.Hkv * ((n + PIECE2 - 1) / PIECE2), pieces3 += p.Hkv * ((n + PIECE3 - 1) / PIECE3);
     }
-    a.piece = pieces1 <= WAVES ? PIECE1 : pieces2 <= WAVES ? PIECE2 : pieces3 <= WAVES ? PIECE3 : CUT;
-    if (a.piece) narrow = a.piece * (a.piece == PIECE1 ? pieces1 : a.piece == PIECE2 ? pieces2 : pieces3);
+    // all in one piece of the second length, and nothing else: nothing to join, which takes longer than three tiles
+    const bool alone = rows == 0 && wide == 0 && pieces2 == items && items <= WAVES;
+    a.piece = alone ? PIECE2 : pieces1 <= WAVES ? PIECE1 : pieces2 <= WAVES ? PIECE2 : pieces3 <= WAVES ? PIECE3 : CUT;
+    if (rows == 0 && wide == 0 && items <= N && (items < N / 4 ? small & 1 : small >> 1)) a.piece = SOLO;
+    if (a.piece == SOLO) narrow = items;
+    else if (a.piece) narrow = a.piece * (a.piece == PIECE1 ? pieces1 : a.piece == PIECE2 ? pieces2 : pieces3);
     if (a.items0) a.narrow0 = p.Hkv * rounded(narrow_units(p, p.P), a.piece);
     a.wide_per = 0;
     if (rows > 32) {
@@ -175,15 +181,17 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int pie
     const int cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 16)) >> p.ns, (int64_t)1 << 18);
     a.b = (narrow + WAVES - 1) / WAVES + (with * cost + WAVES - 1) / WAVES;
     a.a = a.b - cost;
-    if (others == 0) a.a = a.piece ? a.piece : max((narrow + WAVES - 1) / WAVES, MIN_NARROW);
-    else if (a.piece) a.b = a.piece, a.a = others * a.piece >= narrow ? 0 : a.piece;
-    else if (a.a < MIN_NARROW) a.a = 0, a.b = max((narrow + others - 1) / others, MIN_NARROW);
-    a.cut = a.a * with;
-    a.joins = a.wide > 0 || a.items0 > 0 || !a.piece || narrow > items * a.piece;
+    if (a.piece == SOLO) a.a = a.b = 1;
+    else if (a.piece) a.a = a.b = a.piece;
+    else if (others == 0) a.a = max((narrow + WAVES - 1) / WAVES, MIN_NARROW);
+    else if (a.a < MIN_NARROW) a.a = MIN_NARROW, a.b = max((narrow + others - 1) / others, MIN_NARROW);
+    a.others = others;
+    a.cut = a.b * others;
+    a.joins = a.wide > 0 || a.items0 > 0 || (a.piece != SOLO && (!a.piece || narrow > items * a.piece));
     return a;
 }
-// the wavefront (in the order of the pieces) that has place x of the narrow line
-__device__ __forceinline__ int narrow_piece_of(const Plan& a, int x) { return x < a.cut ? x / a.a : 4 * a.with_wide + (x - a.cut) / a.b; }
+// the wavefront, in the order of the pieces, that has place x of the narrow line: those without a wide piece come first
+__device__ __forceinline__ int narrow_piece_of(const Plan& a, int x) { return x < a.cut ? x / a.b : a.others + (x - a.cut) / a.a; }
 
 // Running sums over groups of `per` requests, in LDS: what a place on a line or a packed row is searched in.
 struct Sums {
@@ -459,20 +467,60 @@ __device__ __forceinline__ void leave(const AttnArgs& p, const State<D>& st, boo
     }
 }
 
+// The four wavefronts' parts of the same rows, each in its own LDS as [row][channel], pieces of 16 bytes spread by row; then eight lanes a row.
+template <int D>
+__device__ __forceinline__ void merge(const AttnArgs& p, const State<D>& st, uint8_t* lds, float* stats, int tid, int wave, int lane, int rows, int64_t t, int head) {
+    float* parts = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = lane & 31, piece = 8 * d + 2 * e + (lane >> 5);
+            *reinterpret_cast<float4*>(parts + wave * 32 * D + row * D + ((piece ^ (row & 7)) << 2)) =
+                make_float4(st.o[d][4 * e], st.o[d][4 * e + 1], st.o[d][4 * e + 2], st.o[d][4 * e + 3]);
+        }
+    if (lane < 32) stats[wave * 32 + lane] = st.base, stats[128 + wave * 32 + lane] = st.sum;
+    lds_barrier();
+    const int row = tid >> 3, part = tid & 7;
+    if (row >= rows) return;
+    float base = -INFINITY, f[4], sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) base = fmaxf(base, stats[k * 32 + row]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        f[k] = base == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stats[k * 32 + row] - base);
+        sum += f[k] * stats[128 + k * 32 + row];
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) {
+        const int piece = k * 8 + part;
+        float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float4 z = *reinterpret_cast<const float4*>(parts + v * 32 * D + row * D + ((piece ^ (row & 7)) << 2));
+            y[0] = fmaf(f[v], z.x, y[0]), y[1] = fmaf(f[v], z.y, y[1]), y[2] = fmaf(f[v], z.z, y[2]), y[3] = fmaf(f[v], z.w, y[3]);
+        }
+        *reinterpret_cast<uint2*>(p.O + t * p.ldo + head * D + piece * 4) = make_uint2(pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv));
+    }
+    if (part == 0 && p.lse) p.lse[t * p.Hq + head] = lse_of(base, sum);
+}
+
 // ---- a piece of the line of 32-row tiles ----------------------------------------------------------------------------------------
 // A wavefront's own: tiles of 32 tokens in LDS that no other wavefront uses.  Keys of the next tile are asked for once this tile's
 // scores are there, values once they are summed, so half a tile or more is on its way at any time, and no wavefront waits for another.
 template <int D>
-__device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds) {
+__device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, float* stats) {
     constexpr int TILE = 32 * D * 2, NI = D / 16;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // what follows from it is made here, not kept in registers from the kernel's start
     const int lane = tid & 63, wave = uni(tid >> 6);
     const int64_t to_v = p.V - p.K;
     const uint32_t kt = lds_at(lds) + wave * 2 * TILE, vt = kt + TILE, kl = kt + key_lane<D>(lane), vl = vt + value_lane<D>(lane);
-    const int w = blockIdx.x * 4 + wave, with = 4 * plan.with_wide;
-    int x = w < with ? w * plan.a : plan.cut + (w - with) * plan.b;
-    const int end = min(x + (w < with ? plan.a : plan.b), plan.narrow);
+    const bool solo = plan.piece == SOLO;
+    const int wg = blockIdx.x, w = (wg < plan.with_wide ? plan.others + wg * 4 : (wg - plan.with_wide) * 4) + wave;  // in the order of the pieces
+    int x = solo ? wg : w < plan.others ? w * plan.b : plan.cut + (w - plan.others) * plan.a;
+    const int end = min(x + (solo ? 1 : w < plan.others ? plan.b : plan.a), plan.narrow);
     while (x < end) {
         // the item at x: its start and length on the line, its rows, its tokens
         int start, item, length, h, r0, rows, n_prefix, tokens = 0, seen = 0, clear_to = 0, b = -1;  // tiles of the prefix, then own tokens
@@ -495,7 +543,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             n_prefix = p.pre_tiles;
         }
         const int stop = min(end, start + length);
-        const int t0 = narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), n_prefix + ((tokens + 31) >> 5));
+        const int step = solo ? 4 : 1, t0 = solo ? wave : narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), n_prefix + ((tokens + 31) >> 5));
         const bool whole = x == start && stop == start + length;
         x = stop;
 
@@ -535,16 +583,16 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             lds_order();  // the waits below count: keys first
             fetch(tile, ra, rb, to_v, vt);
         }
-        for (; tile < t1; ++tile) {
-            const bool more = tile + 1 < t1;
-            if (more) runs(tile + 1, na, nb);
+        for (; tile < t1; tile += step) {
+            const bool more = tile + step < t1;
+            if (more) runs(tile + step, na, nb);
             wait_vmcnt<NI>();  // the keys are there; the values may not be
             lds_order();
             v16f s[1];
             scores<D, 1>(s, q, kl);
             lds_order();
             __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the keys are read
-            if (more) fetch(tile + 1, na, nb, 0, kt);
+            if (more) fetch(tile + step, na, nb, 0, kt);
             const bool pre = tile < n_prefix;
             const int j0 = (pre ? tile : tile - n_prefix) * 32;
             if (j0 + 32 > (pre ? p.P : clear_to)) mask<1>(s, lane, (pre ? p.P : seen) - j0);
@@ -557,13 +605,18 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             gather<D, 1>(st, s, f, vl);
             lds_order();
             __builtin_amdgcn_s_waitcnt(0xC07F);
-            if (more) fetch(tile + 1, na, nb, to_v, vt);
+            if (more) fetch(tile + step, na, nb, to_v, vt);
         }
         st.sum = half_sum(st.sum);
-        const bool direct = whole && (p.P == 0 || p.pre_tiles);
-        const int slot = item + w, row = lane & 31;
-        if (r0 + row < rows && (direct || slot < p.narrow_blocks))
-            leave<D>(p, st, direct, (int64_t)ti, h * p.G + g, p.blocks + (p.joint_blocks + p.packed_blocks + slot) * block_bytes<D>(), row, lane >> 5);
+        if (solo) {
+            const int row = r0 + (tid >> 3);
+            merge<D>(p, st, lds, stats, tid, wave, lane, rows - r0, rq.q0 + row / p.G, h * p.G + row % p.G);
+        } else {
+            const bool direct = whole && (p.P == 0 || p.pre_tiles);
+            const int slot = item + w, row = lane & 31;
+            if (r0 + row < rows && (direct || slot < p.narrow_blocks))
+                leave<D>(p, st, direct, (int64_t)ti, h * p.G + g, p.blocks + (p.joint_blocks + p.packed_blocks + slot) * block_bytes<D>(), row, lane >> 5);
+        }
     }
 }
 
@@ -712,7 +765,8 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
 
 struct AttnShared {
     Sums sums;
-    int part[4][7];
+    int part[4][8];
+    float stats[256];
 };
 
 template <int D>
@@ -725,14 +779,15 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     const int T = (int)p.T;
     constexpr int NV = 7;  // narrow, pieces of the three lengths, items, rows, wide
     int mine[NV] = {0, 0, 0, 0, 0, 0, 0}, v[NV], total[NV];
-    bool wrong = false;
+    bool wrong = false, few = true, many = true;  // no more than SOLO_FEW, SOLO_MANY tokens
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
     for (int b = b0; b < b1; ++b) {
         const Request r = request(p, b);
         wrong |= r.q0 < 0 || r.n < 0 || r.q0 > T - r.n;
         if (wrong) break;
         const Extent e = extent(p, r, CUT);
-const int n = narrow_length(p, r.L, CUT);
+        few &= p.P + r.L <= SOLO_FEW, many &= p.P + r.L <= SOLO_MANY;
+        const int n = narrow_length(p, r.L, CUT);
         mine[0] += e.narrow, mine[4] += e.items, mine[5] += e.rows, mine[6] += e.wide;
         mine[1] += e.items * ((n + PIECE1 - 1) / PIECE1), mine[2] += e.items * ((n + PIECE2 - 1) / PIECE2), mine[3] += e.items * ((n + PIECE3 - 1) / PIECE3);
     }
@@ -748,6 +803,8 @@ const int n = narrow_length(p, r.L, CUT);
     if (lane == 63)
 #pragma unroll
         for (int k = 0; k < NV; ++k) part[wave][k] = v[k];
+    const int small = (__ballot(!few) == 0) + 2 * (__ballot(!many) == 0);
+    if (lane == 0) part[wave][NV] = small;
     if (__syncthreads_or(wrong)) {  // offsets that fall or name rows that are not there: nothing is read or written
         if (blockIdx.x == 0 && tid == 0) p.plan->valid = 0;
         return;
@@ -762,8 +819,10 @@ const int n = narrow_length(p, r.L, CUT);
             total[k] += part[u][k];
         }
     }
-    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), uni(total[5]), uni(total[6]));
-    if (plan.piece) v[0] = plan.piece * (plan.piece == PIECE1 ? v[1] : plan.piece == PIECE2 ? v[2] : v[3]);
+    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), uni(total[5]), uni(total[6]),
+                                   uni(part[0][NV] & part[1][NV] & part[2][NV] & part[3][NV]));
+    if (plan.piece == SOLO) v[0] = v[4];
+    else if (plan.piece) v[0] = plan.piece * (plan.piece == PIECE1 ? v[1] : plan.piece == PIECE2 ? v[2] : v[3]);
     sums.narrow[tid] = v[0], sums.items[tid] = v[4], sums.rows[tid] = v[5], sums.wide[tid] = v[6];
     if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
         if (tid == 0) *p.plan = plan;
@@ -785,7 +844,7 @@ const int n = narrow_length(p, r.L, CUT);
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
         if ((turn == 0) == swap) {
-            narrow_piece<D>(p, plan, sums, lds);
+            narrow_piece<D>(p, plan, sums, lds, sh.stats);
             if (turn == 0 && with_wide) lds_barrier();  // the tiles of both are in the same place
         } else if (with_wide) wide_piece<D>(p, plan, sums, lds, xcd * run + i);
     }
