@@ -30,18 +30,21 @@ constexpr int WG = 256, WROWS = 128, GROUPS = 256;
 // Workgroups: two on a CU (LDS for their tiles), three where heads are small.
 template <int D>
 constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
-// The narrow line is cut where pieces end (CUT), or its items are rounded up to whole pieces of one of these lengths, or (SOLO) a workgroup has
-// one item and nothing is joined: where there is no wide work, no more items than workgroups, and no request sees more than
-// SOLO_FEW tokens, or SOLO_MANY where a quarter of the workgroups or more have an item.
-enum { CUT = 0, SOLO = -1 };
-constexpr int PIECE1 = 3, PIECE2 = 6, PIECE3 = 12, SOLO_FEW = 512, SOLO_MANY = 1024;
+// How the narrow line is dealt out.  By workgroups, whose wavefronts take every fourth tile and merge their sums in LDS:
+//   SOLO  an item a workgroup, nothing joined: no wide work, no more items than workgroups, and no request that sees more than SOLO_FEW
+//         tokens, or SOLO_MANY where a quarter of the workgroups or more have an item
+//   TEAM  few items: rounded up to pieces of TEAM tiles, as many as workgroups at most
+//   CUT   long lines, cut where the workgroups' pieces end
+// By wavefronts, each its own: items rounded up to pieces of 3, 6 or 12 tiles, the shortest that the wavefronts can take at once.
+enum { CUT = 0, SOLO = -1, TEAM = 5, PIECE1 = 3, PIECE2 = 6, PIECE3 = 12 };
+constexpr int SOLO_FEW = 512, SOLO_MANY = 1024;
 // Short requests walk the prefix themselves, tile after tile of their own items, where that is no more than this many tiles a wavefront
-constexpr int INLINE_TILES = 6;
+constexpr int INLINE_TILES = 4;
 // The line of 32-row tiles is measured in tiles of 32 tokens, that of 128-row tiles in tokens.  Starting and ending a segment costs
 // about as much as the EDGEs; no piece is smaller than the MINs (MIN_WIDE where workgroups have little to do, and twice that where
 // they have more than 16 narrow tiles each: us with 256 against 512, 32 heads on 8, 32 requests behind 1000 tokens 21.0 / 25.4, 20 behind
 // 9000 26.0 / 28.5; 100 behind 3000 40.7 / 37.0, 64 behind 8192 with 400 of their own 53.9 / 45.4).
-constexpr int NARROW_EDGE = 1, MIN_NARROW = PIECE1, WIDE_EDGE = 128, MIN_WIDE = 256;
+constexpr int CUT_EDGE = 4, PIECE_EDGE = 1, MIN_NARROW = 8, WIDE_EDGE = 128, MIN_WIDE = 256;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
 constexpr int LONG_PREFIX = 256, LONG = 33;  // rows of a long request, with a prefix and without
 
@@ -94,10 +97,11 @@ __device__ __forceinline__ Request request(const AttnArgs& p, int b) {
 __device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? LONG_PREFIX : LONG); }
 __device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (n * p.G + 31) >> 5; }
 // `piece`: CUT or the length that items are rounded up to
-__device__ __forceinline__ int narrow_units(const AttnArgs& p, int L) { return (((L + 31) >> 5) + NARROW_EDGE + (1 << p.ns) - 1) >> p.ns; }
+__device__ __forceinline__ int narrow_edge(int piece) { return piece == CUT ? CUT_EDGE : PIECE_EDGE; }
+__device__ __forceinline__ int narrow_units(const AttnArgs& p, int L, int piece) { return (((L + 31) >> 5) + narrow_edge(piece) + (1 << p.ns) - 1) >> p.ns; }
 __device__ __forceinline__ int rounded(int n, int piece) { return piece ? (n + piece - 1) / piece * piece : n; }
-__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int piece) { return piece == SOLO ? 1 : rounded(narrow_units(p, L) + p.pre_tiles, piece); }
-__device__ __forceinline__ int narrow_tile(const AttnArgs& p, int y) { return max(0, (y << p.ns) - NARROW_EDGE); }  // the first tile at place y of an item
+__device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int piece) { return piece == SOLO ? 1 : rounded(narrow_units(p, L, piece) + p.pre_tiles, piece); }
+__device__ __forceinline__ int narrow_tile(const AttnArgs& p, int y, int piece) { return max(0, (y << p.ns) - narrow_edge(piece)); }  // the first tile at place y of an item
 // the first k tiles of a long request on their line: each sees `seen` and a tile's tokens more than the one before it
 __device__ __forceinline__ int wide_sum(const AttnArgs& p, int seen, int k) { return k * seen + (p.tpt >> p.ws) * (k * (k + 1) / 2); }
 __device__ __forceinline__ int wide_seen(const AttnArgs& p, const Request& r) { return ((WIDE_EDGE + p.P + max(r.L - r.n, 0)) >> p.ws) + 1; }
@@ -128,7 +132,7 @@ struct Plan {
     int narrow0, items0;   // of which the prefix's narrow items are the first
     int wide0, head;       // of which the packed tiles are the first, `head` for every key/value head
     int wide_per, a, b, cut;
-    int with_wide, others, piece;
+    int with_wide, others, piece, team;
     int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; pieces of the prefix, blocks of 64 tokens in one, in the prefix
     int valid;  // offsets are in order
     int joins;  // anything to join
@@ -139,7 +143,7 @@ __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
     return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
 }
 template <int D>
-__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int pieces1, int pieces2, int pieces3, int items, int rows, int wide, int small) {
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int teams, int pieces1, int pieces2, int pieces3, int items, int rows, int wide, int small) {
     constexpr int N = attn_wgs<D>(), WAVES = 4 * N;
     Plan a;
     a.valid = 1;
@@ -148,18 +152,20 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int pie
     a.narrow0 = a.items0 = a.wide0 = a.head = 0;
     a.tiles = a.supers = a.super = 0;
     if (rows > 0 && rows <= 32) {
-        const int n = narrow_units(p, p.P);
+        const int n = narrow_units(p, p.P, TEAM);
         a.items0 = p.Hkv;
-        narrow += p.Hkv * n;
+        narrow += p.Hkv * narrow_units(p, p.P, CUT);
+        teams += p.Hkv * ((n + TEAM - 1) / TEAM);
         pieces1 += p.Hkv * ((n + PIECE1 - 1) / PIECE1), pieces2 += p.Hkv * ((n + PIECE2 - 1) / PIECE2), pieces3 += p.Hkv * ((n + PIECE3 - 1) / PIECE3);
     }
     // all in one piece of the second length, and nothing else: nothing to join, which takes longer than three tiles
     const bool alone = rows == 0 && wide == 0 && pieces2 == items && items <= WAVES;
-    a.piece = alone ? PIECE2 : pieces1 <= WAVES ? PIECE1 : pieces2 <= WAVES ? PIECE2 : pieces3 <= WAVES ? PIECE3 : CUT;
-    if (rows == 0 && wide == 0 && items <= N && (items < N / 4 ? small & 1 : small >> 1)) a.piece = SOLO;
-    if (a.piece == SOLO) narrow = items;
-    else if (a.piece) narrow = a.piece * (a.piece == PIECE1 ? pieces1 : a.piece == PIECE2 ? pieces2 : pieces3);
-    if (a.items0) a.narrow0 = p.Hkv * rounded(narrow_units(p, p.P), a.piece);
+    const bool solo = rows == 0 && wide == 0 && items <= N && (items < N / 4 ? small & 1 : small >> 1);
+    a.piece = solo ? SOLO : alone ? PIECE2 : teams <= N ? TEAM : pieces1 <= WAVES ? PIECE1 : pieces2 <= WAVES ? PIECE2 : pieces3 <= WAVES ? PIECE3 : CUT;
+    a.team = a.piece == SOLO || a.piece == TEAM || a.piece == CUT;
+    if (solo) narrow = items;
+    else if (a.piece) narrow = a.piece * (a.piece == TEAM ? teams : a.piece == PIECE1 ? pieces1 : a.piece == PIECE2 ? pieces2 : pieces3);
+    if (a.items0) a.narrow0 = p.Hkv * rounded(narrow_units(p, p.P, a.piece), a.piece);
     a.wide_per = 0;
     if (rows > 32) {
         a.tiles = (rows + WROWS - 1) / WROWS;
@@ -177,20 +183,20 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int pie
     a.wide = a.wide0 + wide;
     if (!a.wide_per) a.wide_per = max((a.wide + N - 1) / N, max(2 * MIN_WIDE >> p.ws, 1));
     a.with_wide = ((a.wide + a.wide_per - 1) / a.wide_per + 7) / 8 * 8;  // as many on every XCD
-    const int with = 4 * a.with_wide, others = WAVES - with;
-    const int cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 16)) >> p.ns, (int64_t)1 << 18);
-    a.b = (narrow + WAVES - 1) / WAVES + (with * cost + WAVES - 1) / WAVES;
+    const int all = a.team ? N : WAVES, with = all / N * a.with_wide, others = all - with;
+    const int cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 4) * N / all) >> p.ns, (int64_t)1 << 18);
+    a.b = (narrow + all - 1) / all + (with * cost + all - 1) / all;
     a.a = a.b - cost;
     if (a.piece == SOLO) a.a = a.b = 1;
     else if (a.piece) a.a = a.b = a.piece;
-    else if (others == 0) a.a = max((narrow + WAVES - 1) / WAVES, MIN_NARROW);
+    else if (others == 0) a.a = max((narrow + all - 1) / all, MIN_NARROW);
     else if (a.a < MIN_NARROW) a.a = MIN_NARROW, a.b = max((narrow + others - 1) / others, MIN_NARROW);
     a.others = others;
     a.cut = a.b * others;
     a.joins = a.wide > 0 || a.items0 > 0 || (a.piece != SOLO && (!a.piece || narrow > items * a.piece));
     return a;
 }
-// the wavefront, in the order of the pieces, that has place x of the narrow line: those without a wide piece come first
+// the workgroup or wavefront, in the order of the pieces, that has place x of the narrow line: those without a wide piece come first
 __device__ __forceinline__ int narrow_piece_of(const Plan& a, int x) { return x < a.cut ? x / a.b : a.others + (x - a.cut) / a.a; }
 
 // Running sums over groups of `per` requests, in LDS: what a place on a line or a packed row is searched in.
@@ -469,7 +475,8 @@ __device__ __forceinline__ void leave(const AttnArgs& p, const State<D>& st, boo
 
 // The four wavefronts' parts of the same rows, each in its own LDS as [row][channel], pieces of 16 bytes spread by row; then eight lanes a row.
 template <int D>
-__device__ __forceinline__ void merge(const AttnArgs& p, const State<D>& st, uint8_t* lds, float* stats, int tid, int wave, int lane, int rows, int64_t t, int head) {
+__device__ __forceinline__ void merge(const AttnArgs& p, const State<D>& st, uint8_t* lds, float* stats, int tid, int wave, int lane, int rows, bool direct, int64_t t, int head,
+                                      uint8_t* blk) {
     float* parts = reinterpret_cast<float*>(lds);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -482,33 +489,40 @@ __device__ __forceinline__ void merge(const AttnArgs& p, const State<D>& st, uin
     if (lane < 32) stats[wave * 32 + lane] = st.base, stats[128 + wave * 32 + lane] = st.sum;
     lds_barrier();
     const int row = tid >> 3, part = tid & 7;
-    if (row >= rows) return;
-    float base = -INFINITY, f[4], sum = 0.0f;
+    if (row < rows) {
+        float base = -INFINITY, f[4], sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) base = fmaxf(base, stats[k * 32 + row]);
+        for (int k = 0; k < 4; ++k) base = fmaxf(base, stats[k * 32 + row]);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        f[k] = base == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stats[k * 32 + row] - base);
-        sum += f[k] * stats[128 + k * 32 + row];
-    }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) {
-        const int piece = k * 8 + part;
-        float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const float4 z = *reinterpret_cast<const float4*>(parts + v * 32 * D + row * D + ((piece ^ (row & 7)) << 2));
-            y[0] = fmaf(f[v], z.x, y[0]), y[1] = fmaf(f[v], z.y, y[1]), y[2] = fmaf(f[v], z.z, y[2]), y[3] = fmaf(f[v], z.w, y[3]);
+        for (int k = 0; k < 4; ++k) {
+            f[k] = base == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stats[k * 32 + row] - base);
+            sum += f[k] * stats[128 + k * 32 + row];
         }
-        *reinterpret_cast<uint2*>(p.O + t * p.ldo + head * D + piece * 4) = make_uint2(pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv));
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            const int piece = k * 8 + part;
+            float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float4 z = *reinterpret_cast<const float4*>(parts + v * 32 * D + row * D + ((piece ^ (row & 7)) << 2));
+                y[0] = fmaf(f[v], z.x, y[0]), y[1] = fmaf(f[v], z.y, y[1]), y[2] = fmaf(f[v], z.z, y[2]), y[3] = fmaf(f[v], z.w, y[3]);
+            }
+            if (direct) *reinterpret_cast<uint2*>(p.O + t * p.ldo + head * D + piece * 4) = make_uint2(pack2(y[0] * inv, y[1] * inv), pack2(y[2] * inv, y[3] * inv));
+            else *reinterpret_cast<float4*>(blk + (row * D + piece * 4) * 4) = make_float4(y[0], y[1], y[2], y[3]);
+        }
+        if (part == 0) {
+            if (!direct) *reinterpret_cast<float2*>(blk + (32 * D + row * 2) * 4) = make_float2(base, sum);
+            else if (p.lse) p.lse[t * p.Hq + head] = lse_of(base, sum);
+        }
     }
-    if (part == 0 && p.lse) p.lse[t * p.Hq + head] = lse_of(base, sum);
+    lds_barrier();  // the next item's tiles land where these parts are
 }
 
 // ---- a piece of the line of 32-row tiles ----------------------------------------------------------------------------------------
-// A wavefront's own: tiles of 32 tokens in LDS that no other wavefront uses.  Keys of the next tile are asked for once this tile's
-// scores are there, values once they are summed, so half a tile or more is on its way at any time, and no wavefront waits for another.
+// A wavefront's tiles of 32 tokens are in LDS that no other wavefront uses.  Keys of the next tile are asked for once this tile's
+// scores are there, values once they are summed, so half a tile or more is on its way at any time, and no wavefront
+// waits for another before a team's sums are merged.
 template <int D>
 __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, float* stats) {
     constexpr int TILE = 32 * D * 2, NI = D / 16;
@@ -517,16 +531,16 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
     const int lane = tid & 63, wave = uni(tid >> 6);
     const int64_t to_v = p.V - p.K;
     const uint32_t kt = lds_at(lds) + wave * 2 * TILE, vt = kt + TILE, kl = kt + key_lane<D>(lane), vl = vt + value_lane<D>(lane);
-    const bool solo = plan.piece == SOLO;
-    const int wg = blockIdx.x, w = (wg < plan.with_wide ? plan.others + wg * 4 : (wg - plan.with_wide) * 4) + wave;  // in the order of the pieces
-    int x = solo ? wg : w < plan.others ? w * plan.b : plan.cut + (w - plan.others) * plan.a;
-    const int end = min(x + (solo ? 1 : w < plan.others ? plan.b : plan.a), plan.narrow);
+    const bool team = plan.team;
+    const int wg = blockIdx.x, order = wg < plan.with_wide ? attn_wgs<D>() - plan.with_wide + wg : wg - plan.with_wide, w = team ? order : order * 4 + wave;
+    int x = w < plan.others ? w * plan.b : plan.cut + (w - plan.others) * plan.a;
+    const int end = min(x + (w < plan.others ? plan.b : plan.a), plan.narrow);
     while (x < end) {
         // the item at x: its start and length on the line, its rows, its tokens
         int start, item, length, h, r0, rows, n_prefix, tokens = 0, seen = 0, clear_to = 0, b = -1;  // tiles of the prefix, then own tokens
         Request rq{0, 0, 0};
         if (x < plan.narrow0) {
-            length = rounded(narrow_units(p, p.P), plan.piece);
+            length = rounded(narrow_units(p, p.P, plan.piece), plan.piece);
             h = x / length;
             start = h * length, item = h;
             r0 = 0, rows = plan.rows, n_prefix = (p.P + 31) >> 5;
@@ -543,7 +557,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             n_prefix = p.pre_tiles;
         }
         const int stop = min(end, start + length);
-        const int step = solo ? 4 : 1, t0 = solo ? wave : narrow_tile(p, x - start), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start), n_prefix + ((tokens + 31) >> 5));
+        const int step = team ? 4 : 1, t0 = narrow_tile(p, x - start, plan.piece) + (team ? wave : 0), t1 = min(stop == start + length ? 0x7fffffff : narrow_tile(p, stop - start, plan.piece), n_prefix + ((tokens + 31) >> 5));
         const bool whole = x == start && stop == start + length;
         x = stop;
 
@@ -608,14 +622,14 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             if (more) fetch(tile + step, na, nb, to_v, vt);
         }
         st.sum = half_sum(st.sum);
-        if (solo) {
+        const bool direct = whole && (p.P == 0 || p.pre_tiles);
+        const int slot = item + w;
+        uint8_t* blk = p.blocks + (p.joint_blocks + p.packed_blocks + slot) * block_bytes<D>();
+        if (team) {
             const int row = r0 + (tid >> 3);
-            merge<D>(p, st, lds, stats, tid, wave, lane, rows - r0, rq.q0 + row / p.G, h * p.G + row % p.G);
-        } else {
-            const bool direct = whole && (p.P == 0 || p.pre_tiles);
-            const int slot = item + w, row = lane & 31;
-            if (r0 + row < rows && (direct || slot < p.narrow_blocks))
-                leave<D>(p, st, direct, (int64_t)ti, h * p.G + g, p.blocks + (p.joint_blocks + p.packed_blocks + slot) * block_bytes<D>(), row, lane >> 5);
+            merge<D>(p, st, lds, stats, tid, wave, lane, direct || slot < p.narrow_blocks ? rows - r0 : 0, direct, rq.q0 + row / p.G, h * p.G + row % p.G, blk);
+        } else if (r0 + (lane & 31) < rows && (direct || slot < p.narrow_blocks)) {
+            leave<D>(p, st, direct, (int64_t)ti, h * p.G + g, blk, lane & 31, lane >> 5);
         }
     }
 }
@@ -765,7 +779,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
 
 struct AttnShared {
     Sums sums;
-    int part[4][8];
+    int part[4][9];
     float stats[256];
 };
 
@@ -777,8 +791,8 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     auto& part = sh.part;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int T = (int)p.T;
-    constexpr int NV = 7;  // narrow, pieces of the three lengths, items, rows, wide
-    int mine[NV] = {0, 0, 0, 0, 0, 0, 0}, v[NV], total[NV];
+    constexpr int NV = 8;  // narrow, pieces of the three lengths, items, rows, wide, teams' pieces
+    int mine[NV] = {0, 0, 0, 0, 0, 0, 0, 0}, v[NV], total[NV];
     bool wrong = false, few = true, many = true;  // no more than SOLO_FEW, SOLO_MANY tokens
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
     for (int b = b0; b < b1; ++b) {
@@ -787,8 +801,8 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
         if (wrong) break;
         const Extent e = extent(p, r, CUT);
         few &= p.P + r.L <= SOLO_FEW, many &= p.P + r.L <= SOLO_MANY;
-        const int n = narrow_length(p, r.L, CUT);
-        mine[0] += e.narrow, mine[4] += e.items, mine[5] += e.rows, mine[6] += e.wide;
+        const int n = narrow_units(p, r.L, TEAM) + p.pre_tiles;
+        mine[0] += e.narrow, mine[4] += e.items, mine[5] += e.rows, mine[6] += e.wide, mine[7] += e.items * ((n + TEAM - 1) / TEAM);
         mine[1] += e.items * ((n + PIECE1 - 1) / PIECE1), mine[2] += e.items * ((n + PIECE2 - 1) / PIECE2), mine[3] += e.items * ((n + PIECE3 - 1) / PIECE3);
     }
 #pragma unroll
@@ -819,10 +833,10 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
             total[k] += part[u][k];
         }
     }
-    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), uni(total[5]), uni(total[6]),
+    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[7]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), uni(total[5]), uni(total[6]),
                                    uni(part[0][NV] & part[1][NV] & part[2][NV] & part[3][NV]));
     if (plan.piece == SOLO) v[0] = v[4];
-    else if (plan.piece) v[0] = plan.piece * (plan.piece == PIECE1 ? v[1] : plan.piece == PIECE2 ? v[2] : v[3]);
+    else if (plan.piece) v[0] = plan.piece * (plan.piece == TEAM ? v[7] : plan.piece == PIECE1 ? v[1] : plan.piece == PIECE2 ? v[2] : v[3]);
     sums.narrow[tid] = v[0], sums.items[tid] = v[4], sums.rows[tid] = v[5], sums.wide[tid] = v[6];
     if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
         if (tid == 0) *p.plan = plan;
@@ -880,7 +894,7 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
     if (i < 0 || i >= rq.n) return;
     const int* rec = p.records + (int64_t)b * 4;
     const bool joint = is_long(p, rq.n);
-    const int cp = rounded(narrow_units(p, p.P), plan.piece), packed_item = packed_length(p, plan.super);
+    const int cp = rounded(narrow_units(p, p.P, plan.piece), plan.piece), packed_item = packed_length(p, plan.super);
     const int pre_pieces = packed_item == plan.wide_per ? 1 : plan.tiles ? (packed_item - 1) / plan.wide_per + 2 : 0;  // of a piece of the prefix, at most
 
     // this lane's row: `own` segments of its request's tile, the first at `first`; then up to `more` of the prefix
@@ -1051,7 +1065,7 @@ int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
     const int64_t rows = a.T * p.G, is_long = rows / (p.P ? LONG_PREFIX : LONG), tiles = rows / WROWS + 1, some = std::min<int64_t>(a.B, a.T);
     const int64_t wide = (int64_t)p.Hkv * (a.T / p.tpt + is_long) * (WIDE_EDGE + p.P + (int64_t)p.max_kv + a.T + WROWS) +
                          (int64_t)p.Hkv * tiles * 2 * (p.P + (WIDE_EDGE + 64) * MAX_SUPER);
-    const int64_t narrow = (int64_t)p.Hkv * (rows / 32 + some + 1) * (std::max<int64_t>(p.P, p.max_kv) / 32 + p.pre_tiles + NARROW_EDGE + PIECE3 + 1);
+    const int64_t narrow = (int64_t)p.Hkv * (rows / 32 + some + 1) * (std::max<int64_t>(p.P, p.max_kv) / 32 + p.pre_tiles + CUT_EDGE + PIECE3 + 1);
     for (p.ws = 0; wide >> p.ws > 1 << 30;) ++p.ws;
     for (p.ns = 0; narrow >> p.ns > 1 << 30;) ++p.ns;
     return a.D == 64 ? launch<64>(p, st) : launch<128>(p, st);
