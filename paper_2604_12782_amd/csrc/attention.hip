@@ -783,6 +783,17 @@ struct AttnShared {
     float stats[256];
 };
 
+// sums over the lanes below and this one, on the vector ALU: four steps inside rows of 16 lanes, then the rows' last lanes
+__device__ __forceinline__ int wave_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // from one lane below
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);   // two
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);   // four
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);   // eight
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 of a row to the next, in rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2 and 3
+    return v;
+}
+
 template <int D>
 __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(const AttnArgs p) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -808,12 +819,7 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
 #pragma unroll
     for (int k = 0; k < NV; ++k) v[k] = mine[k];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int u = __shfl_up(v[k], d);
-            if (lane >= d) v[k] += u;
-        }
+    for (int k = 0; k < NV; ++k) v[k] = wave_scan(v[k]);
     if (lane == 63)
 #pragma unroll
         for (int k = 0; k < NV; ++k) part[wave][k] = v[k];
