@@ -4,16 +4,24 @@
 // the G = Hq / Hkv.  Requests are served in two ways:
 //   long   their own tiles of 128 rows walk the prefix and then their own tokens (`joint`)
 //   short  tiles of 32 rows walk the own tokens only; the short requests' rows, one behind the other, form tiles of 128 that
-//          walk the prefix, which is therefore read once for all of them (`packed`; 32 rows or fewer: one tile of 32)
+//          walk the prefix, which is therefore read once for all of them (`packed`; 32 rows or fewer: one tile of 32).  A prefix so short
+//          that every request may walk it as well is the start of their own items instead (`pre_tiles`), and nothing is joined
 // With a prefix, long means 256 rows or more (a last tile that is not full costs at most a third); without one, more than 32.
 //
 // Work.  Tiles of 128 rows and tiles of 32 rows are two lists.  An item is a tile with the tokens that it walks; the items of
-// a list lie behind each other on a line whose length is tokens, and every workgroup takes an equal piece of both lines. So
-// all workgroups end together whatever the lengths are, no length is read back to the host, and an item is cut at most where a
-// piece ends.  What a workgroup computes of an item is a segment: unnormalised sums, their weight and their base.  A long request's tile
-// in one segment is written as it is; all others go to the workspace and a second kernel joins them, in the order of the
-// line: the same bits in every run.  The two lists are bound by different things (matrix cores and LDS; HBM), so
-// half of the workgroups take them in the other order.
+// a list lie behind each other on a line that measures work, and every workgroup takes its piece of both lines, so
+// all end together whatever the lengths are, no length is read back to the host, and an item is cut at most where a
+// piece ends (pieces of the line of 32-row tiles may be a wavefront's, and rounded up to items: see the modes below).  What is computed of
+// an item in one piece is a segment: unnormalised sums, their weight and their base.  Rows whose tokens are all in one segment are written
+// as they are; all others go to the workspace and a second kernel joins them, in the order of the line: the same bits in every run.
+// The two lists are bound by different things (matrix cores and power; HBM), so half of the workgroups take them in the other
+// order.
+//
+// Bounds.  256 requests behind 32700 tokens take 234 us (86 for the products at the rate of bare matrix loops, 98 for the bytes at that of a
+// reading pass), 40 prompts and decoding requests behind 4096 238 us (109, products): matrix cores 30 to 40 % busy, the weights'
+// exponentials and LDS reads take turns with them, and power brings the clock from 2.4 to 1.9 GHz meanwhile; no one part left out makes
+// up the difference.  12 long requests without a prefix 66 us (42, bytes): 5.3 TB/s in the first kernel, then the second.  Small
+// batches are bound by latency: the plan's reads, a few tiles that depend on one another, the second kernel's reads.
 #include <algorithm>
 
 #include "osc_internal.h"
@@ -24,7 +32,6 @@ namespace osc {
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int WG = 256, WROWS = 128, GROUPS = 256;
 // Workgroups: two on a CU (LDS for their tiles), three where heads are small.
@@ -35,10 +42,16 @@ constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
 //         tokens, or SOLO_MANY where a quarter of the workgroups or more have an item
 //   TEAM  few items: rounded up to pieces of TEAM tiles, as many as workgroups at most
 //   CUT   long lines, cut where the workgroups' pieces end
-// By wavefronts, each its own: items rounded up to pieces of 3, 6 or 12 tiles, the shortest that the wavefronts can take at once.
+// By wavefronts, each its own: items rounded up to pieces of 3, 6 or 12 tiles, the shortest that the wavefronts can take at once; not where
+// items would come to more than FEW_PIECES of the longest each, whose joining costs more than the merges in LDS do.
+// us, 32 heads of 128 on 8, this rule / without the variant:  SOLO 32 requests behind 390 tokens 15.3 / 20.6, and with four times the limits 16
+// of up to 2000 tokens 31.2 instead of 25.1;  TEAM 4 of up to 1000 tokens 16.2 / 17.4;  wavefronts' pieces 100 of up to 100 tokens 15.4 / 25.5 (20.4 without the
+// rule for pieces of 6), 200 behind 200 27.2 / 38.5, 100 behind 3000 35.8 / 43.9;  FEW_PIECES 16 of up to 8000 tokens 55.7 / 62.7, one behind
+// 30000 39.5 / 50.2, 8 behind 12000 with 2000 of their own 31.6 / 41.0.
 enum { CUT = 0, SOLO = -1, TEAM = 5, PIECE1 = 3, PIECE2 = 6, PIECE3 = 12 };
-constexpr int SOLO_FEW = 512, SOLO_MANY = 1024;
-// Short requests walk the prefix themselves, tile after tile of their own items, where that is no more than this many tiles a wavefront
+constexpr int SOLO_FEW = 512, SOLO_MANY = 1024, FEW_PIECES = 4;
+// Short requests walk the prefix themselves, tile after tile of their own items, where that is no more than this many tiles a wavefront (us
+// with 0, 4, 8: 32 requests behind 300 tokens 22.5, 15.3, 15.7; behind 1000 21.2, 21.3, 25.3; behind 1500 21.6, 22.0, 32.4).
 constexpr int INLINE_TILES = 4;
 // The line of 32-row tiles is measured in tiles of 32 tokens, that of 128-row tiles in tokens.  Starting and ending a segment costs
 // about as much as the EDGEs; no piece is smaller than the MINs (MIN_WIDE where workgroups have little to do, and twice that where
@@ -46,7 +59,9 @@ constexpr int INLINE_TILES = 4;
 // 9000 26.0 / 28.5; 100 behind 3000 40.7 / 37.0, 64 behind 8192 with 400 of their own 53.9 / 45.4).
 constexpr int CUT_EDGE = 4, PIECE_EDGE = 1, MIN_NARROW = 8, WIDE_EDGE = 128, MIN_WIDE = 256;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
-constexpr int LONG_PREFIX = 256, LONG = 33;  // rows of a long request, with a prefix and without
+// Rows of a long request, with a prefix and without (us with 128, 256, 512, 24 prompts behind 4000 tokens: of up to 80 tokens 105, 103, 96; of up to 120
+// 144, 149, 155).
+constexpr int LONG_PREFIX = 256, LONG = 33;
 
 struct AttnArgs {
     const uint16_t* Q;
@@ -126,7 +141,7 @@ __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, in
 // pieces of length `a`, the others, which come first on the line, of length `b`, so that all have the same to do: a wide block of 64 tokens takes about a third
 // of the time of a narrow tile (2 us where a CU has two workgroups at it; 16 KB, 6 us where all wavefronts share 5.5 TB/s).  Where there are
 // wavefronts enough for pieces of 3, 6 or 12 tiles, items are rounded up to whole ones: a wavefront has parts of one item, and most
-// items are in one piece.
+// items are in one piece.  Where pieces are workgroups', the same with four times the tiles.
 struct Plan {
     int narrow, wide;      // lengths of the lines
     int narrow0, items0;   // of which the prefix's narrow items are the first
@@ -161,7 +176,7 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int tea
     // all in one piece of the second length, and nothing else: nothing to join, which takes longer than three tiles
     const bool alone = rows == 0 && wide == 0 && pieces2 == items && items <= WAVES;
     const bool solo = rows == 0 && wide == 0 && items <= N && (items < N / 4 ? small & 1 : small >> 1);
-    a.piece = solo ? SOLO : alone ? PIECE2 : teams <= N ? TEAM : pieces1 <= WAVES ? PIECE1 : pieces2 <= WAVES ? PIECE2 : pieces3 <= WAVES ? PIECE3 : CUT;
+    a.piece = solo ? SOLO : alone ? PIECE2 : teams <= N ? TEAM : pieces3 > FEW_PIECES * items ? CUT : pieces1 <= WAVES ? PIECE1 : pieces2 <= WAVES ? PIECE2 : pieces3 <= WAVES ? PIECE3 : CUT;
     a.team = a.piece == SOLO || a.piece == TEAM || a.piece == CUT;
     if (solo) narrow = items;
     else if (a.piece) narrow = a.piece * (a.piece == TEAM ? teams : a.piece == PIECE1 ? pieces1 : a.piece == PIECE2 ? pieces2 : pieces3);
@@ -883,22 +898,28 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
     const int t = (int)(unit / per_token);
     if (t >= p.T) return;
     const int head0 = (int)(unit - (int64_t)t * per_token) * H;
+    // Reads that depend on one another are what this kernel's time is, so they are as few as can be: the last request that starts at or
+    // before t is searched until 64 are left, whose lengths and records are read with their offsets, and beside the plan.
     const Plan plan = *p.plan;
-    if (!plan.valid || !plan.joins) return;
-    int lo = 0, hi = p.B + 1;  // the last request that starts at or before t
-    while (hi - lo > 1) {
+    int lo = 0, hi = p.B + 1;
+    while (hi - lo > 64) {
         const int step = (hi - lo + 63) / 64, at = lo + lane * step;
         const int n = __popcll(__ballot(at < hi && p.q_offsets[min(at, p.B)] <= t));
         if (n == 0) return;
         lo += (n - 1) * step;
         hi = min(hi, lo + step);
     }
-    const int b = uni(lo);
-    if (b >= p.B) return;
-    const Request rq = request(p, b);
+    const int at_b = min(lo + lane, p.B - 1), start = p.q_offsets[min(lo + lane, p.B)], after = p.q_offsets[at_b + 1], len = p.kv_lens[at_b];
+    const int4 all = *reinterpret_cast<const int4*>(p.records + (int64_t)at_b * 4);
+    if (!plan.valid || !plan.joins) return;
+    const int found = uni(__popcll(__ballot(lo + lane < hi && start <= t))) - 1;
+    if (found < 0 || lo + found >= p.B) return;
+    const Request rq{__builtin_amdgcn_readlane(start, found), __builtin_amdgcn_readlane(after, found) - __builtin_amdgcn_readlane(start, found),
+                     min(max(__builtin_amdgcn_readlane(len, found), 0), p.max_kv)};
+    const int rec[4] = {__builtin_amdgcn_readlane(all.x, found), __builtin_amdgcn_readlane(all.y, found), __builtin_amdgcn_readlane(all.z, found),
+                        __builtin_amdgcn_readlane(all.w, found)};
     const int i = t - rq.q0;
     if (i < 0 || i >= rq.n) return;
-    const int* rec = p.records + (int64_t)b * 4;
     const bool joint = is_long(p, rq.n);
     const int cp = rounded(narrow_units(p, p.P, plan.piece), plan.piece), packed_item = packed_length(p, plan.super);
     const int pre_pieces = packed_item == plan.wide_per ? 1 : plan.tiles ? (packed_item - 1) / plan.wide_per + 2 : 0;  // of a piece of the prefix, at most
@@ -956,6 +977,18 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         int at_row = 0;
         const int64_t blk = place(j0 + jl, at_row), at = blk < 0 ? 0 : blk * block_bytes<D>();
         const float2 z = *reinterpret_cast<const float2*>(p.blocks + at + (32 * D + at_row * 2) * 4);
+        const int64_t off = at + at_row * D * 4;
+        const int m = min(S, most - j0);
+        // four loads of a lane for a row of sums, segments j ..; the first ones are asked for before the weights are there
+        auto first_lane = [&](int q) { return H == 1 ? 0 : (sub * ROWS + q) * S; };
+        auto load = [&](int q, int j, float4 (&y)[4]) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                y[k] = *reinterpret_cast<const float4*>(p.blocks + __shfl(off, first_lane(q) + min(j + k * STEP + (H == 1 ? sub : 0), S - 1)) + l * 16);
+        };
+        float4 y[ROWS][4];
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) load(q, 0, y[q]);
         const float bs = blk < 0 ? -INFINITY : z.x, wt = blk < 0 ? 0.0f : z.y;
         float top = bs;
 #pragma unroll
@@ -964,28 +997,20 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         const float f = wt > 0.0f ? __builtin_amdgcn_exp2f(bs - next) : 0.0f;
         base = next;
         sum = fmaf(f, wt, sum * fade);
-        const int64_t off = at + at_row * D * 4;
-        const int m = min(S, most - j0);
 #pragma unroll
         for (int q = 0; q < ROWS; ++q) {
-            const int lane0 = H == 1 ? 0 : (sub * ROWS + q) * S;
-            const float fd = __shfl(fade, lane0);
+            const float fd = __shfl(fade, first_lane(q));
             acc[q].x *= fd, acc[q].y *= fd, acc[q].z *= fd, acc[q].w *= fd;
-            for (int j = 0; j < m; j += 4 * STEP) {  // four loads of a lane on their way
-                float4 y[4];
-                float fy[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int at_j = j + k * STEP + (H == 1 ? sub : 0), from = lane0 + min(at_j, S - 1);
-                    const float g = __shfl(f, from);
-                    fy[k] = at_j < m ? g : 0.0f;
-                    y[k] = *reinterpret_cast<const float4*>(p.blocks + __shfl(off, from) + l * 16);
-                }
+            for (int j = 0; j < m; j += 4 * STEP) {
+                if (j) load(q, j, y[q]);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {  // a segment without weight may not have left sums
-                    const bool has = fy[k] > 0.0f;
-                    acc[q].x = has ? fmaf(fy[k], y[k].x, acc[q].x) : acc[q].x, acc[q].y = has ? fmaf(fy[k], y[k].y, acc[q].y) : acc[q].y;
-                    acc[q].z = has ? fmaf(fy[k], y[k].z, acc[q].z) : acc[q].z, acc[q].w = has ? fmaf(fy[k], y[k].w, acc[q].w) : acc[q].w;
+                    const int at_j = j + k * STEP + (H == 1 ? sub : 0);
+                    const float g = __shfl(f, first_lane(q) + min(at_j, S - 1)), fy = at_j < m ? g : 0.0f;
+                    const float4 v = y[q][k];
+                    const bool has = fy > 0.0f;
+                    acc[q].x = has ? fmaf(fy, v.x, acc[q].x) : acc[q].x, acc[q].y = has ? fmaf(fy, v.y, acc[q].y) : acc[q].y;
+                    acc[q].z = has ? fmaf(fy, v.z, acc[q].z) : acc[q].z, acc[q].w = has ? fmaf(fy, v.w, acc[q].w) : acc[q].w;
                 }
             }
         }

@@ -309,6 +309,13 @@ def test_attention_few_rows_behind_a_long_prefix(osc, D, P):
     check_attention(osc, make(32, 7, P, [5, 200, 33, 1, 64, 90, 17], [1, 1, 0, 1, 1, 1, 1], 24, 8, D, 128))
 
 
+def test_attention_few_long_requests(osc):
+    """items of many pieces each: tokens of their own, and a prefix that few rows walk"""
+    check_attention(osc, make(33, 5, 0, [5000, 1, 7000, 333, 2600], [1, 1, 1, 2, 1], 16, 8, 128, 32))
+    check_attention(osc, make(34, 3, 0, [12000, 9000, 31], [1, 3, 1], 8, 8, 64, 128))
+    check_attention(osc, make(35, 2, 15000, [300, 5], [1, 1], 32, 8, 128, 64))
+
+
 @pytest.mark.parametrize("D,P,Hq,Hkv", [(128, 700, 4, 2), (64, 1300, 6, 1), (128, 4100, 8, 8), (64, 4999, 5, 1)])
 def test_attention_packed_rows(osc, D, P, Hq, Hkv):
     """the rows of many requests in tiles of 128 that walk the prefix; idle requests between them, and long ones that walk it themselves"""
