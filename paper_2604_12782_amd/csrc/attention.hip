@@ -117,17 +117,19 @@ __device__ __forceinline__ int narrow_units(const AttnArgs& p, int L, int piece)
 __device__ __forceinline__ int rounded(int n, int piece) { return piece ? (n + piece - 1) / piece * piece : n; }
 __device__ __forceinline__ int narrow_length(const AttnArgs& p, int L, int piece) { return piece == SOLO ? 1 : rounded(narrow_units(p, L, piece) + p.pre_tiles, piece); }
 __device__ __forceinline__ int narrow_tile(const AttnArgs& p, int y, int piece) { return max(0, (y << p.ns) - narrow_edge(piece)); }  // the first tile at place y of an item
-// the first k tiles of a long request on their line: each sees `seen` and a tile's tokens more than the one before it
-__device__ __forceinline__ int wide_sum(const AttnArgs& p, int seen, int k) { return k * seen + (p.tpt >> p.ws) * (k * (k + 1) / 2); }
-__device__ __forceinline__ int wide_seen(const AttnArgs& p, const Request& r) { return ((WIDE_EDGE + p.P + max(r.L - r.n, 0)) >> p.ws) + 1; }
-__device__ __forceinline__ int wide_length(const AttnArgs& p, int seen, int tile) { return seen + (tile + 1) * (p.tpt >> p.ws); }
+// Tiles of a long request on their line: each sees `step` more tokens than the one before it, the first `seen` and that; dealt out whole
+// (SOLO), each is 1 long.
+__device__ __forceinline__ int wide_step(const AttnArgs& p, int piece) { return piece == SOLO ? 0 : p.tpt >> p.ws; }
+__device__ __forceinline__ int wide_seen(const AttnArgs& p, const Request& r, int piece) { return piece == SOLO ? 1 : ((WIDE_EDGE + p.P + max(r.L - r.n, 0)) >> p.ws) + 1; }
+__device__ __forceinline__ int wide_sum(int step, int seen, int k) { return k * seen + step * (k * (k + 1) / 2); }  // the first k
+__device__ __forceinline__ int wide_length(int step, int seen, int tile) { return seen + (tile + 1) * step; }
 __device__ __forceinline__ int wide_tiles(const AttnArgs& p, int n) { return (n + p.tpt - 1) / p.tpt; }
 __device__ __forceinline__ int packed_length(const AttnArgs& p, int blocks) { return ((blocks * 64 + WIDE_EDGE) >> p.ws) + 1; }
 __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, int piece) {
     Extent e{0, 0, 0, 0};
     if (r.n == 0) return e;
     if (is_long(p, r.n)) {
-        e.wide = p.Hkv * wide_sum(p, wide_seen(p, r), wide_tiles(p, r.n));
+        e.wide = p.Hkv * wide_sum(wide_step(p, piece), wide_seen(p, r, piece), wide_tiles(p, r.n));
     } else {
         e.items = narrow_tiles(p, r.n) * p.Hkv;
         e.narrow = e.items * narrow_length(p, r.L, piece);
@@ -146,7 +148,7 @@ struct Plan {
     int narrow, wide;      // lengths of the lines
     int narrow0, items0;   // of which the prefix's narrow items are the first
     int wide0, head;       // of which the packed tiles are the first, `head` for every key/value head
-    int wide_per, a, b, cut;
+    int wide_per, wide_piece, a, b, cut;
     int with_wide, others, piece, team;
     int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; pieces of the prefix, blocks of 64 tokens in one, in the prefix
     int valid;  // offsets are in order
@@ -158,7 +160,7 @@ __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
     return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
 }
 template <int D>
-__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int teams, int pieces1, int pieces2, int pieces3, int items, int rows, int wide, int small) {
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int teams, int pieces1, int pieces2, int pieces3, int items, int rows, int wide, int wide_items, int small) {
     constexpr int N = attn_wgs<D>(), WAVES = 4 * N;
     Plan a;
     a.valid = 1;
@@ -196,10 +198,13 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int tea
     }
     a.narrow = narrow;
     a.wide = a.wide0 + wide;
-    if (!a.wide_per) a.wide_per = max((a.wide + N - 1) / N, max(2 * MIN_WIDE >> p.ws, 1));
+    a.wide_piece = rows <= 32 && wide_items <= N && (wide_items < N / 4 ? small & 1 : small >> 1) ? SOLO : CUT;
+    int busy = a.wide_per;  // what a workgroup has of the wide line
+    if (!busy) busy = a.wide_per = max((a.wide + N - 1) / N, max((a.wide0 ? 2 * MIN_WIDE : MIN_WIDE) >> p.ws, 1));
+    if (a.wide_piece == SOLO) busy = wide / max(wide_items, 1), a.wide = wide_items, a.wide_per = 1;
     a.with_wide = ((a.wide + a.wide_per - 1) / a.wide_per + 7) / 8 * 8;  // as many on every XCD
     const int all = a.team ? N : WAVES, with = all / N * a.with_wide, others = all - with;
-    const int cost = (int)min((((int64_t)a.wide_per << p.ws) * 5 / (64 * 4) * N / all) >> p.ns, (int64_t)1 << 18);
+    const int cost = (int)min((((int64_t)busy << p.ws) * 5 / (64 * 4) * N / all) >> p.ns, (int64_t)1 << 18);
     a.b = (narrow + all - 1) / all + (with * cost + all - 1) / all;
     a.a = a.b - cost;
     if (a.piece == SOLO) a.a = a.b = 1;
@@ -208,7 +213,7 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int tea
     else if (a.a < MIN_NARROW) a.a = MIN_NARROW, a.b = max((narrow + others - 1) / others, MIN_NARROW);
     a.others = others;
     a.cut = a.b * others;
-    a.joins = a.wide > 0 || a.items0 > 0 || (a.piece != SOLO && (!a.piece || narrow > items * a.piece));
+    a.joins = (a.wide > 0 && a.wide_piece != SOLO) || a.items0 > 0 || (a.piece != SOLO && (!a.piece || narrow > items * a.piece));
     return a;
 }
 // the workgroup or wavefront, in the order of the pieces, that has place x of the narrow line: those without a wide piece come first
@@ -680,19 +685,19 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             slot = p.joint_blocks + ((int64_t)(h * plan.supers + s) * plan.tiles + tile + w) * 4;
         } else {
             Extent before;
-            b = find_request<true>(p, sums, CUT, x - plan.wide0, lane, before);
+            b = find_request<true>(p, sums, plan.wide_piece, x - plan.wide0, lane, before);
             rq = request(p, b);
             const int nt = wide_tiles(p, rq.n);
-            const int seen = wide_seen(p, rq), head = wide_sum(p, seen, nt), y = x - plan.wide0 - before.wide;
+            const int step = wide_step(p, plan.wide_piece), seen = wide_seen(p, rq, plan.wide_piece), head = wide_sum(step, seen, nt), y = x - plan.wide0 - before.wide;
             h = y / head;
             int lo = 0, hi = nt;  // the last tile that starts at or before y
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (wide_sum(p, seen, mid) <= y - h * head) lo = mid;
+                if (wide_sum(step, seen, mid) <= y - h * head) lo = mid;
                 else hi = mid;
             }
-            start = plan.wide0 + before.wide + h * head + wide_sum(p, seen, lo);
-            length = wide_length(p, seen, lo);
+            start = plan.wide0 + before.wide + h * head + wide_sum(step, seen, lo);
+            length = wide_length(step, seen, lo);
             t_base = lo * p.tpt;
             const int tokens = min(p.tpt, rq.n - t_base);
             rows = tokens * p.G;
@@ -794,7 +799,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
 
 struct AttnShared {
     Sums sums;
-    int part[4][9];
+    int part[4][10];
     float stats[256];
 };
 
@@ -817,8 +822,8 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     auto& part = sh.part;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int T = (int)p.T;
-    constexpr int NV = 8;  // narrow, pieces of the three lengths, items, rows, wide, teams' pieces
-    int mine[NV] = {0, 0, 0, 0, 0, 0, 0, 0}, v[NV], total[NV];
+    constexpr int NV = 9;  // narrow, pieces of the three lengths, items, rows, wide, teams' pieces, wide tiles
+    int mine[NV] = {0, 0, 0, 0, 0, 0, 0, 0, 0}, v[NV], total[NV];
     bool wrong = false, few = true, many = true;  // no more than SOLO_FEW, SOLO_MANY tokens
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
     for (int b = b0; b < b1; ++b) {
@@ -828,6 +833,7 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
         const Extent e = extent(p, r, CUT);
         few &= p.P + r.L <= SOLO_FEW, many &= p.P + r.L <= SOLO_MANY;
         const int n = narrow_units(p, r.L, TEAM) + p.pre_tiles;
+        if (e.wide > 0) mine[8] += p.Hkv * wide_tiles(p, r.n);
         mine[0] += e.narrow, mine[4] += e.items, mine[5] += e.rows, mine[6] += e.wide, mine[7] += e.items * ((n + TEAM - 1) / TEAM);
         mine[1] += e.items * ((n + PIECE1 - 1) / PIECE1), mine[2] += e.items * ((n + PIECE2 - 1) / PIECE2), mine[3] += e.items * ((n + PIECE3 - 1) / PIECE3);
     }
@@ -854,10 +860,11 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
             total[k] += part[u][k];
         }
     }
-    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[7]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), uni(total[5]), uni(total[6]),
+    const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[7]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), uni(total[5]), uni(total[6]), uni(total[8]),
                                    uni(part[0][NV] & part[1][NV] & part[2][NV] & part[3][NV]));
     if (plan.piece == SOLO) v[0] = v[4];
     else if (plan.piece) v[0] = plan.piece * (plan.piece == TEAM ? v[7] : plan.piece == PIECE1 ? v[1] : plan.piece == PIECE2 ? v[2] : v[3]);
+    if (plan.wide_piece == SOLO) v[6] = v[8];
     sums.narrow[tid] = v[0], sums.items[tid] = v[4], sums.rows[tid] = v[5], sums.wide[tid] = v[6];
     if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
         if (tid == 0) *p.plan = plan;
@@ -865,7 +872,7 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
             const Extent e = extent(p, request(p, b), plan.piece);
             int* r = p.records + (int64_t)b * 4;
             r[0] = v[0], r[1] = v[4], r[2] = v[5], r[3] = v[6];
-            v[0] += e.narrow, v[4] += e.items, v[5] += e.rows, v[6] += e.wide;
+            v[0] += e.narrow, v[4] += e.items, v[5] += e.rows, v[6] += plan.wide_piece == plan.piece ? e.wide : extent(p, request(p, b), plan.wide_piece).wide;
         }
     }
     __syncthreads();
@@ -929,10 +936,10 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
     const int packed = rec[2] + r;
     int own, more = 0, row, first;
     if (joint) {
-        const int seen = wide_seen(p, rq), tile = i / p.tpt;
-        const int s0 = plan.wide0 + rec[3] + h * wide_sum(p, seen, wide_tiles(p, rq.n)) + wide_sum(p, seen, tile);
+        const int step = wide_step(p, plan.wide_piece), seen = wide_seen(p, rq, plan.wide_piece), tile = i / p.tpt;
+        const int s0 = plan.wide0 + rec[3] + h * wide_sum(step, seen, wide_tiles(p, rq.n)) + wide_sum(step, seen, tile);
         first = s0 / plan.wide_per;
-        own = (s0 + wide_length(p, seen, tile) - 1) / plan.wide_per - first + 1;
+        own = (s0 + wide_length(step, seen, tile) - 1) / plan.wide_per - first + 1;
         row = r - tile * p.tpt * p.G;
     } else {
         const int length = narrow_length(p, rq.L, plan.piece);
