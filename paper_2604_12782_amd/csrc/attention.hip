@@ -54,10 +54,15 @@ constexpr int SOLO_FEW = 512, SOLO_MANY = 1024, FEW_PIECES = 4;
 // with 0, 4, 8: 32 requests behind 300 tokens 22.5, 15.3, 15.7; behind 1000 21.2, 21.3, 25.3; behind 1500 21.6, 22.0, 32.4).
 constexpr int INLINE_TILES = 4;
 // The line of 32-row tiles is measured in tiles of 32 tokens, that of 128-row tiles in tokens.  Starting and ending a segment costs
-// about as much as the EDGEs; no piece is smaller than the MINs (MIN_WIDE where workgroups have little to do, and twice that where
-// they have more than 16 narrow tiles each: us with 256 against 512, 32 heads on 8, 32 requests behind 1000 tokens 21.0 / 25.4, 20 behind
-// 9000 26.0 / 28.5; 100 behind 3000 40.7 / 37.0, 64 behind 8192 with 400 of their own 53.9 / 45.4).
+// about as much as the EDGEs; no piece is smaller than the MINs.  MIN_WIDE: pieces of packed rows where workgroups have no more than 16 narrow tiles
+// each (us with 256 against 512, 32 heads on 8, 32 requests behind 1000 tokens 21.0 / 25.4, 20 behind 9000 26.0 / 28.5), and prompts' where nothing is packed (66 rows behind 1000 tokens
+// of their own 22.7 / 26.2, with 192 22.0, but a prompt of 2000 then 32.8 / 29.0); twice that otherwise (100 behind 3000 40.7 / 37.0, 64 behind 8192 with 400 of
+// their own 53.9 / 45.4, 38 mixed of up to 107 rows behind 1112 41.5 / 39.4).
 constexpr int CUT_EDGE = 4, PIECE_EDGE = 1, MIN_NARROW = 8, WIDE_EDGE = 128, MIN_WIDE = 256;
+// Wide tiles are dealt out whole, as many to every workgroup, and not joined, where the longest ones take no more than cut pieces and their joining:
+// JOIN_COST tokens, and one for 2^JOIN_ROWS rows.  us, 32 heads on 8, whole / cut: a prompt of 512 tokens 17 / 28, of 6000 61 / 78, 16 of up to 1000
+// 89 / 118;  12 of up to 20 behind up to 830 tokens of their own 30 / 24, 6 of up to 80 behind 900 36 / 27.
+constexpr int JOIN_COST = 512, JOIN_ROWS = 6;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
 // Rows of a long request, with a prefix and without (us with 128, 256, 512, 24 prompts behind 4000 tokens: of up to 80 tokens 105, 103, 96; of up to 120
 // 144, 149, 155).
@@ -139,7 +144,7 @@ __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, in
 }
 
 // What follows from the totals: the prefix's items, which come first on their line, and the pieces.
-// Wide pieces are equal; the first `with_wide` workgroups have one.  A narrow piece is a wavefront's: those of these workgroups take
+// Wide pieces are equal, in tokens or whole tiles; the first `with_wide` workgroups have one.  A narrow piece is a wavefront's: those of these workgroups take
 // pieces of length `a`, the others, which come first on the line, of length `b`, so that all have the same to do: a wide block of 64 tokens takes about a third
 // of the time of a narrow tile (2 us where a CU has two workgroups at it; 16 KB, 6 us where all wavefronts share 5.5 TB/s).  Where there are
 // wavefronts enough for pieces of 3, 6 or 12 tiles, items are rounded up to whole ones: a wavefront has parts of one item, and most
@@ -160,7 +165,7 @@ __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
     return tiles > 1 ? (int)(n < 1 ? 1 : n > MAX_SUPER ? MAX_SUPER : n) : 1;
 }
 template <int D>
-__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int teams, int pieces1, int pieces2, int pieces3, int items, int rows, int wide, int wide_items, int small) {
+__device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int teams, int pieces1, int pieces2, int pieces3, int items, int rows, int wide, int wide_items, int longest, int small) {
     constexpr int N = attn_wgs<D>(), WAVES = 4 * N;
     Plan a;
     a.valid = 1;
@@ -198,10 +203,14 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int tea
     }
     a.narrow = narrow;
     a.wide = a.wide0 + wide;
-    a.wide_piece = rows <= 32 && wide_items <= N && (wide_items < N / 4 ? small & 1 : small >> 1) ? SOLO : CUT;
+    a.wide_piece = CUT;
     int busy = a.wide_per;  // what a workgroup has of the wide line
-    if (!busy) busy = a.wide_per = max((a.wide + N - 1) / N, max((a.wide0 ? 2 * MIN_WIDE : MIN_WIDE) >> p.ws, 1));
-    if (a.wide_piece == SOLO) busy = wide / max(wide_items, 1), a.wide = wide_items, a.wide_per = 1;
+    if (!busy) {
+        busy = a.wide_per = max((a.wide + N - 1) / N, max((a.wide0 ? 2 * MIN_WIDE : MIN_WIDE) >> p.ws, 1));
+        const int each = (wide_items + N - 1) / N;
+        if (rows <= 32 && (int64_t)each * longest <= busy + ((JOIN_COST + (p.T * p.Hq >> JOIN_ROWS)) >> p.ws))
+            a.wide_piece = SOLO, a.wide = wide_items, a.wide_per = max(each, 1), busy = each * (wide / max(wide_items, 1));
+    }
     a.with_wide = ((a.wide + a.wide_per - 1) / a.wide_per + 7) / 8 * 8;  // as many on every XCD
     const int all = a.team ? N : WAVES, with = all / N * a.with_wide, others = all - with;
     const int cost = (int)min((((int64_t)busy << p.ws) * 5 / (64 * 4) * N / all) >> p.ns, (int64_t)1 << 18);
@@ -799,18 +808,19 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
 
 struct AttnShared {
     Sums sums;
-    int part[4][10];
+    int part[4][11];
     float stats[256];
 };
 
-// sums over the lanes below and this one, on the vector ALU: four steps inside rows of 16 lanes, then the rows' last lanes
-__device__ __forceinline__ int wave_scan(int v) {
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // from one lane below
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);   // two
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);   // four
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);   // eight
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 of a row to the next, in rows 1 and 3
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2 and 3
+// of the lanes below and this one, on the vector ALU: four steps inside rows of 16 lanes, then the rows' last lanes; op(x, 0) is x
+template <class Op>
+__device__ __forceinline__ int wave_scan(int v, Op op) {
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true));   // from one lane below
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true));   // two
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true));   // four
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true));   // eight
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));  // lane 15 of a row to the next, in rows 1 and 3
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));  // lane 31 to rows 2 and 3
     return v;
 }
 
@@ -825,6 +835,7 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     constexpr int NV = 9;  // narrow, pieces of the three lengths, items, rows, wide, teams' pieces, wide tiles
     int mine[NV] = {0, 0, 0, 0, 0, 0, 0, 0, 0}, v[NV], total[NV];
     bool wrong = false, few = true, many = true;  // no more than SOLO_FEW, SOLO_MANY tokens
+    int longest = 0;  // the wide tile that sees most
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
     for (int b = b0; b < b1; ++b) {
         const Request r = request(p, b);
@@ -833,19 +844,23 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
         const Extent e = extent(p, r, CUT);
         few &= p.P + r.L <= SOLO_FEW, many &= p.P + r.L <= SOLO_MANY;
         const int n = narrow_units(p, r.L, TEAM) + p.pre_tiles;
-        if (e.wide > 0) mine[8] += p.Hkv * wide_tiles(p, r.n);
+        if (e.wide > 0) {
+            const int nt = wide_tiles(p, r.n);
+            mine[8] += p.Hkv * nt, longest = max(longest, wide_length(wide_step(p, CUT), wide_seen(p, r, CUT), nt - 1));
+        }
         mine[0] += e.narrow, mine[4] += e.items, mine[5] += e.rows, mine[6] += e.wide, mine[7] += e.items * ((n + TEAM - 1) / TEAM);
         mine[1] += e.items * ((n + PIECE1 - 1) / PIECE1), mine[2] += e.items * ((n + PIECE2 - 1) / PIECE2), mine[3] += e.items * ((n + PIECE3 - 1) / PIECE3);
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) v[k] = mine[k];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) v[k] = wave_scan(v[k]);
+    for (int k = 0; k < NV; ++k) v[k] = wave_scan(v[k], [](int a, int b) { return a + b; });
     if (lane == 63)
 #pragma unroll
         for (int k = 0; k < NV; ++k) part[wave][k] = v[k];
     const int small = (__ballot(!few) == 0) + 2 * (__ballot(!many) == 0);
-    if (lane == 0) part[wave][NV] = small;
+    longest = wave_scan(longest, [](int a, int b) { return max(a, b); });
+    if (lane == 63) part[wave][NV] = small, part[wave][NV + 1] = longest;
     if (__syncthreads_or(wrong)) {  // offsets that fall or name rows that are not there: nothing is read or written
         if (blockIdx.x == 0 && tid == 0) p.plan->valid = 0;
         return;
@@ -861,6 +876,7 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
         }
     }
     const Plan plan = make_plan<D>(p, uni(total[0]), uni(total[7]), uni(total[1]), uni(total[2]), uni(total[3]), uni(total[4]), uni(total[5]), uni(total[6]), uni(total[8]),
+                                   uni(max(max(part[0][NV + 1], part[1][NV + 1]), max(part[2][NV + 1], part[3][NV + 1]))),
                                    uni(part[0][NV] & part[1][NV] & part[2][NV] & part[3][NV]));
     if (plan.piece == SOLO) v[0] = v[4];
     else if (plan.piece) v[0] = plan.piece * (plan.piece == TEAM ? v[7] : plan.piece == PIECE1 ? v[1] : plan.piece == PIECE2 ? v[2] : v[3]);

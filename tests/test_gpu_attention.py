@@ -316,6 +316,13 @@ def test_attention_few_long_requests(osc):
     check_attention(osc, make(35, 2, 15000, [300, 5], [1, 1], 32, 8, 128, 64))
 
 
+@pytest.mark.parametrize("P", [0, 100])
+def test_attention_prompts_in_whole_tiles(osc, P):
+    """more tiles than workgroups, short enough that none is cut; single tokens beside them"""
+    check_attention(osc, make(36 + P, 16, P, [150] * 16, [150] * 16, 32, 8, 128, 64))
+    check_attention(osc, make(37 + P, 18, P, [150, 64, 90] * 6, [150, 1, 83] * 6, 24, 8, 64, 32))
+
+
 @pytest.mark.parametrize("D,P,Hq,Hkv", [(128, 700, 4, 2), (64, 1300, 6, 1), (128, 4100, 8, 8), (64, 4999, 5, 1)])
 def test_attention_packed_rows(osc, D, P, Hq, Hkv):
     """the rows of many requests in tiles of 128 that walk the prefix; idle requests between them, and long ones that walk it themselves"""
