@@ -17,8 +17,8 @@
 // The two lists are bound by different things (matrix cores and power; HBM), so half of the workgroups take them in the other
 // order.
 //
-// Bounds.  256 requests behind 32700 tokens take 234 us (86 for the products at the rate of bare matrix loops, 98 for the bytes at that of a
-// reading pass), 40 prompts and decoding requests behind 4096 238 us (109, products): matrix cores 30 to 40 % busy, the weights'
+// Bounds.  256 requests behind 32700 tokens take 233 to 238 us (86 for the products at the rate of bare matrix loops, 98 for the bytes at that of a
+// reading pass), 40 prompts and decoding requests behind 4096 238 to 244 (109, products): matrix cores 30 to 40 % busy, the weights'
 // exponentials and LDS reads take turns with them, and power brings the clock from 2.4 to 1.9 GHz meanwhile; no one part left out makes
 // up the difference.  12 long requests without a prefix 66 us (42, bytes): 5.3 TB/s in the first kernel, then the second.  Small
 // batches are bound by latency: the plan's reads, a few tiles that depend on one another, the second kernel's reads.
@@ -207,9 +207,11 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int tea
     int busy = a.wide_per;  // what a workgroup has of the wide line
     if (!busy) {
         busy = a.wide_per = max((a.wide + N - 1) / N, max((a.wide0 ? 2 * MIN_WIDE : MIN_WIDE) >> p.ws, 1));
-        const int each = (wide_items + N - 1) / N;
-        if (rows <= 32 && (int64_t)each * longest <= busy + ((JOIN_COST + (p.T * p.Hq >> JOIN_ROWS)) >> p.ws))
-            a.wide_piece = SOLO, a.wide = wide_items, a.wide_per = max(each, 1), busy = each * (wide / max(wide_items, 1));
+        if (wide_items > 0 && rows <= 32) {
+            const int each = (wide_items + N - 1) / N;
+            if ((int64_t)each * longest <= busy + ((JOIN_COST + (p.T * p.Hq >> JOIN_ROWS)) >> p.ws))
+                a.wide_piece = SOLO, a.wide = wide_items, a.wide_per = each, busy = each * (wide / wide_items);
+        }
     }
     a.with_wide = ((a.wide + a.wide_per - 1) / a.wide_per + 7) / 8 * 8;  // as many on every XCD
     const int all = a.team ? N : WAVES, with = all / N * a.with_wide, others = all - with;
