@@ -399,7 +399,9 @@ int osc_dual_gemm_g16(const uint8_t *Xq, const uint8_t *Xs16, float x_tensor_sca
  *            the sum get -1 in both (a launch padded to a fixed size)
  *   info         int32 [4]: pages left, pages taken, requests refused, tokens.  info[0] is the next step's n_free
  *            (n_free must not point into the info that this call writes)
- * B <= 8192.  Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
+ * B <= 8192.  B = 0 is a step without requests: all T rows are padding, q_offsets[0] = 0, no page is taken.  kv_lens and q_lens are
+ * not read then, but are null only where there is no step at all: with B = 0 and both null nothing is written.
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
  */
 int osc_page_slots(const int32_t *kv_lens, const int32_t *q_lens, int32_t B, int32_t page_size, const int32_t *free_pages,
                    int64_t n_pool, const int32_t *n_free, int32_t *block_table, int64_t ldt, int32_t pos_base,

@@ -702,9 +702,9 @@ int osc_page_slots(const int32_t* kv_lens, const int32_t* q_lens, int32_t B, int
             (long long)T, (long long)ldt, (long long)n_pool, pos_base);
     REQUIRE(B <= PAGED_MAX_REQUESTS, OSC_ERR_UNSUPPORTED, "osc_page_slots: %d requests (at most %d)", B, PAGED_MAX_REQUESTS);
     REQUIRE(T <= 0x7fffffff && n_pool <= 0x7fffffff && ldt <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "osc_page_slots: an extent above 2^31-1");
-    if (B == 0) return OSC_OK;
-    REQUIRE(kv_lens && q_lens && n_free && kv_lens_out && q_offsets && info, OSC_ERR_NULL, "osc_page_slots: null pointer");
-    REQUIRE((free_pages || n_pool == 0) && (block_table || ldt == 0) && ((positions && slots) || T == 0), OSC_ERR_NULL,
+    if (B == 0 && !kv_lens && !q_lens) return OSC_OK;  // no step at all
+    REQUIRE(kv_lens && q_lens && n_free && (kv_lens_out || B == 0) && q_offsets && info, OSC_ERR_NULL, "osc_page_slots: null pointer");
+    REQUIRE((free_pages || n_pool == 0) && (block_table || ldt == 0 || B == 0) && ((positions && slots) || T == 0), OSC_ERR_NULL,
             "osc_page_slots: null pointer to an array that is not empty");
     REQUIRE(kv_lens_out + B <= kv_lens || kv_lens + B <= kv_lens_out, OSC_ERR_UNSUPPORTED,
             "osc_page_slots: the new lengths need an array of their own (every workgroup reads the old ones)");

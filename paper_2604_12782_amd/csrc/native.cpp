@@ -441,6 +441,7 @@ PyObject* page_slots(PyObject* const* a) {
             *o2 = ints(pos.o, T, kv, "positions: int32 [T]"), *o3 = ints(slots.o, T, kv, "slots: int32 [T]"), *o4 = ints(info.o, 4, kv, "info: int32 [4]");
     int32_t* pt = table.data_ptr<int32_t>();
     if (B > 0x7fffffff) reject("too many requests");
+    if (B == 0) pk = pq = pn;  // empty tensors have no address; the step's rows and counts are written all the same, and no length is read
     enqueue([&](void* st) { return osc_page_slots(pk, pq, (int32_t)B, ps, pf, pool, pn, pt, width, base, T, o0, o1, o2, o3, o4, st); });
     return tuple({&lens, &offs, &pos, &slots, &info});
 }

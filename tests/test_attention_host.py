@@ -139,3 +139,10 @@ def test_plain_attention_against_torch():
     s[0, :, 36:] = -torch.inf
     s[1, :, 37:] = -torch.inf
     assert np.allclose(o, (torch.softmax(s, -1) @ flat(V)).numpy()) and np.allclose(lse, torch.logsumexp(s, -1).numpy())
+
+
+@pytest.mark.parametrize("code,change", [(NULL, dict(kv=None)), (NULL, dict(q=None)), (NULL, dict(n_free=None)), (NULL, dict(offs=None)), (NULL, dict(info=None)),
+                                         (NULL, dict(pos=None)), (NULL, dict(slots=None)), (NULL, dict(free=None)), (UNSUPPORTED, dict(n_free=10 * P))])
+def test_slots_refusals_without_requests(code, change):
+    """a step of no requests writes its padding, offset and counts, so it needs where to"""
+    assert rc(SLOTS, **dict(dict(B=0, kv_out=None, table=None), **change)) == code

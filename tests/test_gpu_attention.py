@@ -99,6 +99,18 @@ def test_slots_step_by_step(osc):
         w_lens, w_table, w_free = want[0], want[5], want[4][0]
 
 
+@pytest.mark.parametrize("T", [0, 1, 300])
+def test_slots_no_requests(osc, T):
+    """an idle step of a launch padded to T rows: every row is padding, nothing is taken"""
+    none, table = i32([]), torch.empty((0, 4), dtype=torch.int32, device=DEV)
+    for n_pool, n_free, left in ((9, 7, 7), (9, 12, 9), (9, -3, 0), (0, 5, 0)):
+        outs = [torch.full((n,), 77, dtype=torch.int32, device=DEV) for n in (0, 1, T, T, 4)]
+        for out in (tuple(outs), None):
+            lens, offs, pos, slots, info = osc.osc_page_slots(none, none, i32(np.arange(n_pool)), i32([n_free]), table, 16, T, 5, out=out)
+            assert lens.numel() == 0 and offs.tolist() == [0] and info.tolist() == [left, 0, 0, 0]
+            assert pos.tolist() == slots.tolist() == [-1] * T
+
+
 # ---- norms, rotation, cache ------------------------------------------------------------------------------------------
 
 
