@@ -395,8 +395,8 @@ int osc_dual_gemm_g16(const uint8_t *Xq, const uint8_t *Xs16, float x_tensor_sca
  *   block_table  int32 [B, ldt], in and out: entries of the pages a request has are read, new ones written
  *   kv_lens_out  int32 [B]: the lengths after the step (not the array kv_lens: keep two and swap them)
  *   q_offsets    int32 [B + 1]: running sum of q_lens, refused requests included
- *   positions, slots  int32 [T]; T at least the sum of q_lens (tokens past T get neither slot nor page); rows past
- *            the sum get -1 in both (a launch padded to a fixed size)
+ *   positions, slots  int32 [T]; T at least the sum of q_lens: rows past the sum get -1 in both (a launch padded to a fixed
+ *            size), tokens past T get no row, though their requests' lengths and pages are counted and entered with them
  *   info         int32 [4]: pages left, pages taken, requests refused, tokens.  info[0] is the next step's n_free
  *            (n_free must not point into the info that this call writes)
  * B <= 8192.  B = 0 is a step without requests: all T rows are padding, q_offsets[0] = 0, no page is taken.  kv_lens and q_lens are

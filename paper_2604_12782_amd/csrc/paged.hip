@@ -11,7 +11,8 @@ namespace osc {
 // Two running sums over the requests place everything: q_off[b] = sum of the new tokens before b, need_off[b] = sum of the new
 // pages before b.  A workgroup computes both for all requests in LDS (a request costs it 8 bytes from L2) and then serves its
 // share of the tokens: a binary search in q_off finds the request, need_off the page.  So the step is one launch with
-// no word passed between workgroups; the first token of a new page writes that page's table entry.  Sums stop at 2^32 - 1,
+// no word passed between workgroups; the first token of a new page writes that page's table entry, and where T leaves that token
+// without a row, the first workgroup's lane of the request does.  Sums stop at 2^32 - 1,
 // which keeps them in order: what lies past 2^31 - 1 tokens or past the free pages needs no exact number.
 // Bound by latency: the lengths' read, the two sums, the table's read and the store depend on one another.
 template <int NT, int PER>
@@ -80,6 +81,10 @@ __global__ __launch_bounds__(NT) void page_slots_kernel(const int32_t* __restric
                 kv_out[b] = (int32_t)(ok ? kv[k] + q[k] : kv[k]);
                 if (ok) taken += (int)need[k];
                 else ++refused;
+                if (ok && need[k] && (int64_t)sq + q[k] > T) {  // pages whose first token has no row are entered all the same: they are the request's
+                    const int64_t have = ((int64_t)kv[k] + ps1) >> lg, from = ((int64_t)kv[k] + max(T - (int64_t)sq, (int64_t)0) + ps1) >> lg;
+                    for (int64_t i = max(have, from); i < have + need[k]; ++i) table[(int64_t)b * ldt + i] = free_pages[n_free - 1 - (sn + (i - have))];
+                }
             }
         }
         sq = __builtin_elementwise_add_sat(sq, q[k]);

@@ -111,6 +111,19 @@ def test_slots_no_requests(osc, T):
             assert pos.tolist() == slots.tolist() == [-1] * T
 
 
+@pytest.mark.parametrize("B", [1, 5, 300, 1500, 2500])
+def test_slots_fewer_rows_than_tokens(osc, B):
+    """tokens past T have no row; their requests' pages are dealt and entered all the same, so the next step finds them"""
+    gen = np.random.default_rng(B)
+    kv, q = gen.integers(0, 70, B), gen.integers(0, 60, B)
+    kv[gen.random(B) < 0.3] = 32
+    q[0] = 45  # three pages in one request
+    pages = sum(-(-(a + b) // 16) - -(-a // 16) for a, b in zip(kv.tolist(), q.tolist()))
+    for T in (0, 1, 16, int(q.sum()) // 2, int(q.sum()) - 1):
+        check_slots(osc, kv, q, 16, pages + 3, pages + 3, 9, T, 7, seed=T)
+        check_slots(osc, kv, q, 16, pages + 3, pages // 2, 6, T, 7, seed=T)  # some are refused, for want of pages or of room in the table
+
+
 # ---- norms, rotation, cache ------------------------------------------------------------------------------------------
 
 
