@@ -393,7 +393,8 @@ int osc_dual_gemm_g16(const uint8_t *Xq, const uint8_t *Xs16, float x_tensor_sca
  *   token i of request b is row q_offsets[b] + i: position pos_base + kv + i, slot as above.
  *   free_pages   int32 [n_pool];  n_free int32 [1]: how many of them, from the start, are free (limited to n_pool)
  *   block_table  int32 [B, ldt], in and out: entries of the pages a request has are read, new ones written
- *   kv_lens_out  int32 [B]: the lengths after the step (not the array kv_lens: keep two and swap them)
+ *   kv_lens_out  int32 [B]: the lengths after the step (not the array kv_lens: keep two and swap them).  No array that is written
+ *            may overlap another one
  *   q_offsets    int32 [B + 1]: running sum of q_lens, refused requests included
  *   positions, slots  int32 [T]; T at least the sum of q_lens: rows past the sum get -1 in both (a launch padded to a fixed
  *            size), tokens past T get no row, though their requests' lengths and pages are counted and entered with them

@@ -706,9 +706,19 @@ int osc_page_slots(const int32_t* kv_lens, const int32_t* q_lens, int32_t B, int
     REQUIRE(kv_lens && q_lens && n_free && (kv_lens_out || B == 0) && q_offsets && info, OSC_ERR_NULL, "osc_page_slots: null pointer");
     REQUIRE((free_pages || n_pool == 0) && (block_table || ldt == 0 || B == 0) && ((positions && slots) || T == 0), OSC_ERR_NULL,
             "osc_page_slots: null pointer to an array that is not empty");
-    REQUIRE(kv_lens_out + B <= kv_lens || kv_lens + B <= kv_lens_out, OSC_ERR_UNSUPPORTED,
-            "osc_page_slots: the new lengths need an array of their own (every workgroup reads the old ones)");
-    REQUIRE(n_free < info || n_free >= info + 4, OSC_ERR_UNSUPPORTED, "osc_page_slots: n_free lies inside info, which this call writes");
+    // every workgroup reads the inputs while others write, so what is written has memory of its own
+    const struct {
+        const char* name;
+        const int32_t* at;
+        int64_t n;
+    } arrays[] = {{"kv_lens_out", kv_lens_out, B}, {"q_offsets", q_offsets, (int64_t)B + 1}, {"positions", positions, T}, {"slots", slots, T}, {"info", info, 4},
+                  {"block_table", block_table, B * ldt}, {"kv_lens", kv_lens, B}, {"q_lens", q_lens, B}, {"free_pages", free_pages, n_pool}, {"n_free", n_free, 1}};
+    for (int i = 0; i < 6; ++i)
+        for (int j = i + 1; j < 10; ++j) {
+            const uintptr_t a = (uintptr_t)arrays[i].at, b = (uintptr_t)arrays[j].at;
+            REQUIRE(arrays[i].n == 0 || arrays[j].n == 0 || a + arrays[i].n * 4 <= b || b + arrays[j].n * 4 <= a, OSC_ERR_UNSUPPORTED,
+                    "osc_page_slots: %s, which is written, overlaps %s", arrays[i].name, arrays[j].name);
+        }
     return launch_page_slots(kv_lens, q_lens, B, lg, free_pages, n_pool, n_free, block_table, ldt, pos_base, T, kv_lens_out, q_offsets,
                              positions, slots, info, as_stream(stream));
 }

@@ -146,3 +146,12 @@ def test_plain_attention_against_torch():
 def test_slots_refusals_without_requests(code, change):
     """a step of no requests writes its padding, offset and counts, so it needs where to"""
     assert rc(SLOTS, **dict(dict(B=0, kv_out=None, table=None), **change)) == code
+
+
+@pytest.mark.parametrize("change", [dict(kv_out=2 * P), dict(kv_out=2 * P - 12), dict(offs=P), dict(offs=2 * P + 12), dict(offs=4 * P), dict(pos=P), dict(pos=8 * P, slots=8 * P + 28),
+                                    dict(slots=2 * P - 4), dict(info=3 * P), dict(info=5 * P + 92), dict(table=P - 92), dict(table=3 * P + 32), dict(table=7 * P), dict(offs=9 * P),
+                                    dict(kv_out=10 * P), dict(n_free=7 * P + 16), dict(n_free=8 * P), dict(n_free=6 * P), dict(n_free=5 * P + 4)])
+def test_slots_refuses_arrays_that_share_memory(change):
+    """what the call writes lies apart from all that it reads, and from all else that it writes"""
+    assert rc(SLOTS, **change) == UNSUPPORTED
+    assert b"overlaps" in osc.lib().osc_last_error()
