@@ -27,7 +27,8 @@ def page_slots(kv_lens, q_lens, page_size, free_pages, n_free, table, T, pos_bas
         offs.append(offs[-1] + q)
         for p in range(kv, kv + q):
             pos.append(pos_base + p)
-            slots.append(table[b, p // page_size] * page_size + p % page_size if ok else -1)
+            page = table[b, p // page_size] if ok else -1
+            slots.append(page * page_size + p % page_size if 0 <= page < 2 ** 31 // page_size else -1)  # -1 too for a page that no cache can have
     pad = max(0, T - len(pos))
     return (np.array(after), np.array(offs), np.array(pos + [-1] * pad)[:T], np.array(slots + [-1] * pad)[:T],
             np.array([n_free - taken, taken, refused, offs[-1]]), table)

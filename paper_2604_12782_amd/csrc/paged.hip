@@ -123,7 +123,7 @@ __global__ __launch_bounds__(NT) void page_slots_kernel(const int32_t* __restric
                     page = free_pages[n_free - 1 - (need_off[lo] + (i - have))];
                     if ((p & ps1) == 0) *entry = page;
                 }
-                slot = (int)(((int64_t)page << lg) + (p & ps1));
+                if ((uint32_t)page <= 0x7fffffffu >> lg) slot = (int)(((int64_t)page << lg) + (p & ps1));  // otherwise no cache has it, and 32 bits would name another
             }
         }
         positions[t] = pos;

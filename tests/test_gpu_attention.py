@@ -124,6 +124,26 @@ def test_slots_fewer_rows_than_tokens(osc, B):
         check_slots(osc, kv, q, 16, pages + 3, pages // 2, 6, T, 7, seed=T)  # some are refused, for want of pages or of room in the table
 
 
+def test_slots_of_pages_that_no_cache_has(osc):
+    """a page number that is negative, or whose slots 31 bits cannot hold, gives slot -1, not another page's slot"""
+    for ps in (16, 256):
+        lim = 2 ** 31 // ps
+        bad = [lim, -lim, -1, 2 ** 31 - 1, -2 ** 31, lim + 1, 2 * lim % 2 ** 31]
+        kv, q = [3] * len(bad), [2] * len(bad)
+        _, _, pos, slots, _ = osc.osc_page_slots(i32(kv), i32(q), i32([]), i32([0]), i32([[b] for b in bad]), ps, 2 * len(bad))
+        assert pos.tolist() == [3, 4] * len(bad)
+        want = [b * ps + r if 0 <= b < lim else -1 for b in bad for r in (3, 4)]
+        assert slots.tolist() == want
+        fresh = osc.osc_page_slots(i32([0] * len(bad)), i32(q), i32(bad[::-1]), i32([len(bad)]), i32([[5]] * len(bad)), ps, 2 * len(bad))
+        assert fresh[3].tolist() == [b * ps + r if 0 <= b < lim else -1 for b in bad for r in (0, 1)]
+        assert osc.osc_page_slots(i32([3]), i32([1]), i32([]), i32([0]), i32([[lim - 1]]), ps, 1)[3].tolist() == [(lim - 1) * ps + 3]
+    gen = np.random.default_rng(9)
+    table = gen.integers(-2 ** 31, 2 ** 31, (40, 3))
+    kv, q = gen.integers(1, 17, 40), gen.integers(0, 15, 40)
+    want = ref.page_slots(kv, q, 16, np.arange(40), 40, table, int(q.sum()))
+    assert np.array_equal(osc.osc_page_slots(i32(kv), i32(q), i32(np.arange(40)), i32([40]), i32(table), 16, int(q.sum()))[3].cpu().numpy(), want[3])
+
+
 # ---- norms, rotation, cache ------------------------------------------------------------------------------------------
 
 
