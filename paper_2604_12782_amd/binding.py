@@ -434,6 +434,7 @@ def osc_rope_table(base, rot, n_pos, device="cuda", out=None):
     if out is None:
         out = torch.empty((n_pos, rot), dtype=torch.float32, device=device)
     assert out.dtype == torch.float32 and out.is_contiguous() and tuple(out.shape) == (n_pos, rot), "need a float32 [n_pos, rot] table"
+    assert out.is_cuda, "need a table on the GPU"
     _check(lib().osc_rope_table(base, rot, n_pos, _ptr(out), _stream()))
     return out
 

@@ -382,6 +382,10 @@ int32_t* ints(PyObject* o, int64_t n, const at::Tensor& like, const char* what) 
     if (t.scalar_type() != at::kInt || !t.is_contiguous() || t.numel() < n || t.device() != like.device()) reject(what);
     return t.data_ptr<int32_t>();
 }
+// the device that all of a call's tensors are on, once they are seen to agree: a kernel that is given host addresses faults
+void on_gpu(const at::Tensor& t) {
+    if (!t.is_cuda()) reject("need tensors on the GPU");
+}
 int64_t rows_pitch(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
 // rows16 of at least `width` columns, on `like`'s device
 const at::Tensor& rows16_of(PyObject* o, int64_t n, int64_t width, const at::Tensor& like, const char* what) {
@@ -442,6 +446,7 @@ PyObject* page_slots(PyObject* const* a) {
     int32_t* pt = table.data_ptr<int32_t>();
     if (B > 0x7fffffff) reject("too many requests");
     if (B == 0) pk = pq = pn;  // empty tensors have no address; the step's rows and counts are written all the same, and no length is read
+    on_gpu(kv);
     enqueue([&](void* st) { return osc_page_slots(pk, pq, (int32_t)B, ps, pf, pool, pn, pt, width, base, T, o0, o1, o2, o3, o4, st); });
     return tuple({&lens, &offs, &pos, &slots, &info});
 }
@@ -486,6 +491,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {
     const at::Tensor& Y = rows16_of(y.o, T, Hq * D, X, "out: bf16 [T, Hq D]");
     void *x = X.data_ptr(), *py = Y.data_ptr();
     const int64_t ldx = rows_pitch(X), ldy = rows_pitch(Y);
+    on_gpu(X);
     enqueue([&](void* st) {
         return osc_qk_norm_rope(x, T, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, ldx, g[0], g[1], eps, cs.data_ptr<float>(), cs.size(0), (int32_t)rot, style,
                                 pos.data_ptr<int32_t>(), T, axes > 1 ? sec : nullptr, (int32_t)axes, ps, py, ldy, K.data, V.data, K.pages,
@@ -532,6 +538,7 @@ PyObject* prefix_attention(PyObject* const* a) {
     void *q = Q.data_ptr(), *po = O.data_ptr(), *pl = ptr(lse.o), *pw = W.data_ptr();
     const int64_t ldq = rows_pitch(Q), ldo = rows_pitch(O), ldt = table.size(1);
     const int32_t* pt = table.data_ptr<int32_t>();
+    on_gpu(Q);
     enqueue([&](void* st) {
         return osc_prefix_attention(q, T, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, ldq, K.data, V.data, K.pages, K.page_size, pp, P, pt, ldt, kl, qo,
                                     (int32_t)B, scale, po, ldo, (float*)pl, pw, W.nbytes(), st);

@@ -155,3 +155,18 @@ def test_slots_refuses_arrays_that_share_memory(change):
     """what the call writes lies apart from all that it reads, and from all else that it writes"""
     assert rc(SLOTS, **change) == UNSUPPORTED
     assert b"overlaps" in osc.lib().osc_last_error()
+
+
+def test_binding_refuses_tensors_in_host_memory():
+    """a kernel given host addresses faults: calls whose tensors fit each other but lie on the CPU are refused"""
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    h = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    slots = dict(kv_lens=i(3), q_lens=i(3), free_pages=i(9), n_free=i(1), block_table=i(3, 4), page_size=16, T=8)
+    rope = dict(QKV=h(5, 768), Hq=4, Hkv=1, D=128, cos_sin=torch.zeros(9, 128), positions=i(5), slots=i(5), Kc=h(2, 1, 16, 128), Vc=h(2, 1, 16, 128))
+    attn = dict(Q=h(5, 512), Hq=4, Hkv=1, D=128, Kc=h(4, 1, 16, 128), Vc=h(4, 1, 16, 128), prefix_pages=i(2), prefix_len=20, block_table=i(3, 4), kv_lens=i(3), q_offsets=i(4))
+    for call in (lambda: osc.osc_page_slots(**slots), lambda: osc.osc_page_slots(**slots, out=(i(3), i(4), i(8), i(8), i(4))), lambda: osc.osc_qk_norm_rope(**rope),
+                 lambda: osc.osc_qk_norm_rope(**rope, out=h(5, 512)), lambda: osc.osc_prefix_attention(**attn),
+                 lambda: osc.osc_prefix_attention(**attn, workspace=torch.zeros(1 << 20, dtype=torch.uint8), out=(h(5, 512), None)),
+                 lambda: osc.osc_rope_table(1e4, 64, 8, device="cpu"), lambda: osc.osc_rope_table(1e4, 64, 8, out=torch.zeros(8, 64))):
+        with pytest.raises(AssertionError, match="GPU"):
+            call()
