@@ -382,14 +382,21 @@ int32_t* ints(PyObject* o, int64_t n, const at::Tensor& like, const char* what) 
     if (t.scalar_type() != at::kInt || !t.is_contiguous() || t.numel() < n || t.device() != like.device()) reject(what);
     return t.data_ptr<int32_t>();
 }
+// bf16, or its bits in integers; fp16 is another type of as many bits
+bool is_bf16(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kUInt16 || t.scalar_type() == at::kShort; }
+const at::Tensor& rows_bf16(PyObject* o) {
+    const at::Tensor& t = rows16(o);
+    if (!is_bf16(t)) reject("need a 2-D bf16 tensor");
+    return t;
+}
 // the device that all of a call's tensors are on, once they are seen to agree: a kernel that is given host addresses faults
 void on_gpu(const at::Tensor& t) {
     if (!t.is_cuda()) reject("need tensors on the GPU");
 }
 int64_t rows_pitch(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
-// rows16 of at least `width` columns, on `like`'s device
-const at::Tensor& rows16_of(PyObject* o, int64_t n, int64_t width, const at::Tensor& like, const char* what) {
-    const at::Tensor& t = rows16(o);
+// rows of bf16, at least `width` columns, on `like`'s device
+const at::Tensor& rows_bf16_of(PyObject* o, int64_t n, int64_t width, const at::Tensor& like, const char* what) {
+    const at::Tensor& t = rows_bf16(o);
     if (t.size(0) < n || t.size(1) < width || t.device() != like.device()) reject(what);
     return t;
 }
@@ -400,7 +407,7 @@ struct Cache {
     Cache(PyObject* o, int64_t Hkv, int64_t D, const at::Tensor& like) {
         if (none(o)) return;
         const at::Tensor& t = tensor(o);
-        if (!(t.dim() == 4 && t.is_contiguous() && t.element_size() == 2 && t.size(1) == Hkv && t.size(3) == D && t.device() == like.device()))
+        if (!(t.dim() == 4 && t.is_contiguous() && is_bf16(t) && t.size(1) == Hkv && t.size(3) == D && t.device() == like.device()))
             reject("need a contiguous bf16 cache [pages, Hkv, page_size, D]");
         data = t.data_ptr(), pages = t.size(0), page_size = (int32_t)t.size(2);
     }
@@ -453,7 +460,7 @@ PyObject* page_slots(PyObject* const* a) {
 
 // QKV, Hq, Hkv, D, cos_sin, positions, slots, Kc, Vc, gamma_q, gamma_k, eps, rot, style, sections, out
 PyObject* qk_norm_rope(PyObject* const* a) {
-    const at::Tensor& X = rows16(a[0]);
+    const at::Tensor& X = rows_bf16(a[0]);
     const int64_t T = X.size(0), Hq = num(a[1]), Hkv = num(a[2]), D = num(a[3]);
     if (Hq < 0 || Hkv < 0 || D < 0 || Hq > 65536 || Hkv > 65536 || D > 65536 || X.size(1) < (Hq + 2 * Hkv) * D) reject("QKV: bf16 [T, (Hq + 2 Hkv) D]");
     const at::Tensor& cs = tensor(a[4]);
@@ -479,7 +486,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {
     for (int i = 0; i < 2; ++i) {
         if (!none(a[9 + i])) {
             const at::Tensor& t = tensor(a[9 + i]);
-            if (t.element_size() != 2 || t.numel() != D || !t.is_contiguous() || t.device() != X.device()) reject("gamma: bf16 [D]");
+            if (!is_bf16(t) || t.numel() != D || !t.is_contiguous() || t.device() != X.device()) reject("gamma: bf16 [D]");
         }
         g[i] = ptr(a[9 + i]);
     }
@@ -488,7 +495,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {
     Ref y;
     if (!none(a[15])) y.share(a[15]);
     else y.own(fresh(X, {T, Hq * D}, at::kBFloat16));
-    const at::Tensor& Y = rows16_of(y.o, T, Hq * D, X, "out: bf16 [T, Hq D]");
+    const at::Tensor& Y = rows_bf16_of(y.o, T, Hq * D, X, "out: bf16 [T, Hq D]");
     void *x = X.data_ptr(), *py = Y.data_ptr();
     const int64_t ldx = rows_pitch(X), ldy = rows_pitch(Y);
     on_gpu(X);
@@ -502,7 +509,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {
 
 // Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets, scale, want_lse, workspace, out
 PyObject* prefix_attention(PyObject* const* a) {
-    const at::Tensor& Q = rows16(a[0]);
+    const at::Tensor& Q = rows_bf16(a[0]);
     const int64_t T = Q.size(0), Hq = num(a[1]), Hkv = num(a[2]), D = num(a[3]), P = num(a[7]);
     if (Hq <= 0 || Hkv <= 0 || D <= 0 || Hq > 65536 || Hkv > 65536 || D > 65536 || Q.size(1) < Hq * D) reject("Q: bf16 [T, Hq D]");
     const Cache K(a[4], Hkv, D, Q), V(a[5], Hkv, D, Q);
@@ -524,7 +531,7 @@ PyObject* prefix_attention(PyObject* const* a) {
         if (truth(a[12])) lse.own(fresh(Q, {T, Hq}, at::kFloat));
         else lse.share(Py_None);
     }
-    const at::Tensor& O = rows16_of(o.o, T, Hq * D, Q, "out: bf16 [T, Hq D]");
+    const at::Tensor& O = rows_bf16_of(o.o, T, Hq * D, Q, "out: bf16 [T, Hq D]");
     if (!none(lse.o)) {
         const at::Tensor& t = tensor(lse.o);
         if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() < T * Hq || t.device() != Q.device()) reject("lse: float32 [T, Hq]");

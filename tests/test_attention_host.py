@@ -170,3 +170,21 @@ def test_binding_refuses_tensors_in_host_memory():
                  lambda: osc.osc_rope_table(1e4, 64, 8, device="cpu"), lambda: osc.osc_rope_table(1e4, 64, 8, out=torch.zeros(8, 64))):
         with pytest.raises(AssertionError, match="GPU"):
             call()
+
+
+def test_binding_refuses_other_types_of_16_bits():
+    """fp16 is not read as if its bits were bf16; bits of bf16 in integers are (they go as far as the check that they are on the GPU)"""
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    h = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    rope = dict(QKV=h(5, 768), Hq=4, Hkv=1, D=128, cos_sin=torch.zeros(9, 128), positions=i(5), slots=i(5), Kc=h(2, 1, 16, 128), Vc=h(2, 1, 16, 128), gamma_q=h(128),
+                gamma_k=h(128), out=h(5, 512))
+    attn = dict(Q=h(5, 512), Hq=4, Hkv=1, D=128, Kc=h(4, 1, 16, 128), Vc=h(4, 1, 16, 128), prefix_pages=i(2), prefix_len=20, block_table=i(3, 4), kv_lens=i(3), q_offsets=i(4))
+    for call, good, names in ((osc.osc_qk_norm_rope, rope, ("QKV", "Kc", "Vc", "gamma_q", "gamma_k", "out")), (osc.osc_prefix_attention, attn, ("Q", "Kc", "Vc"))):
+        for name in names:
+            with pytest.raises(AssertionError, match="bf16"):
+                call(**dict(good, **{name: good[name].half()}))
+            for bits in (torch.uint16, torch.int16):
+                with pytest.raises(AssertionError, match="GPU"):
+                    call(**dict(good, **{name: good[name].view(bits)}))
+    with pytest.raises(AssertionError, match="bf16"):
+        osc.osc_prefix_attention(**attn, out=(h(5, 512).half(), None))
