@@ -375,6 +375,11 @@ PyObject* quantize_act_dynamic(PyObject* const* a) {
     PyErr_SetString(PyExc_AssertionError, what);
     throw PyFailed();
 }
+int32_t num32(PyObject* o) {
+    const int64_t v = num(o);
+    if (v != (int32_t)v) reject("need a number of 32 bits");
+    return (int32_t)v;
+}
 // a contiguous int32 tensor of at least n elements on `like`'s device (null for None)
 int32_t* ints(PyObject* o, int64_t n, const at::Tensor& like, const char* what) {
     if (none(o)) return nullptr;
@@ -407,7 +412,8 @@ struct Cache {
     Cache(PyObject* o, int64_t Hkv, int64_t D, const at::Tensor& like) {
         if (none(o)) return;
         const at::Tensor& t = tensor(o);
-        if (!(t.dim() == 4 && t.is_contiguous() && is_bf16(t) && t.size(1) == Hkv && t.size(3) == D && t.device() == like.device()))
+        if (!(t.dim() == 4 && t.is_contiguous() && is_bf16(t) && t.size(1) == Hkv && t.size(2) > 0 && t.size(2) <= 0x7fffffff && t.size(3) == D &&
+              t.device() == like.device()))
             reject("need a contiguous bf16 cache [pages, Hkv, page_size, D]");
         data = t.data_ptr(), pages = t.size(0), page_size = (int32_t)t.size(2);
     }
@@ -417,10 +423,10 @@ struct Cache {
 PyObject* page_slots(PyObject* const* a) {
     const at::Tensor& kv = tensor(a[0]);
     const int64_t B = kv.numel(), T = num(a[6]);
-    const int32_t ps = (int32_t)num(a[5]), base = (int32_t)num(a[7]);
+    const int32_t ps = num32(a[5]), base = num32(a[7]);
     const int32_t *pk = ints(a[0], B, kv, "kv_lens: int32 [B]"), *pq = ints(a[1], B, kv, "q_lens: int32 [B]");
     const int32_t* pf = ints(a[2], 0, kv, "free_pages: int32 [pool]");
-    const int64_t pool = count(a[2]);
+    const int64_t pool = none(a[2]) ? 0 : tensor(a[2]).numel();
     const int32_t* pn = ints(a[3], 1, kv, "n_free: int32 [1]");
     const at::Tensor& table = tensor(a[4]);
     if (!(table.dim() == 2 && table.scalar_type() == at::kInt && table.size(0) == B && table.is_contiguous() && table.device() == kv.device()))
@@ -466,7 +472,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {
     const at::Tensor& cs = tensor(a[4]);
     if (!(cs.dim() == 2 && cs.scalar_type() == at::kFloat && cs.is_contiguous() && cs.device() == X.device())) reject("cos_sin: float32 [n_pos, rot]");
     const int64_t rot = none(a[12]) ? cs.size(1) : num(a[12]);
-    if (cs.size(1) != rot) reject("cos_sin: float32 [n_pos, rot]");
+    if (cs.size(1) != rot || rot > 65536) reject("cos_sin: float32 [n_pos, rot]");
     const at::Tensor& pos = tensor(a[5]);
     const int64_t axes = pos.dim() == 2 ? pos.size(0) : 1;
     if (!(pos.dim() >= 1 && pos.dim() <= 2 && pos.scalar_type() == at::kInt && pos.is_contiguous() && pos.size(-1) == T && pos.device() == X.device()))
@@ -477,7 +483,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {
         seq.own(PySequence_Fast(a[14], "`sections` is a sequence of numbers"));
         if (!seq.o) throw PyFailed();
         if (PySequence_Fast_GET_SIZE(seq.o) != axes) reject("sections: one number an axis");
-        for (int64_t i = 0; i < axes; ++i) sec[i] = (int32_t)num(PySequence_Fast_GET_ITEM(seq.o, i));
+        for (int64_t i = 0; i < axes; ++i) sec[i] = num32(PySequence_Fast_GET_ITEM(seq.o, i));
     }
     const Cache K(a[7], Hkv, D, X), V(a[8], Hkv, D, X);
     if (!none(a[7]) && !none(a[8]) && (K.pages != V.pages || K.page_size != V.page_size)) reject("the two caches differ in shape");
@@ -491,7 +497,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {
         g[i] = ptr(a[9 + i]);
     }
     const float eps = real(a[11]);
-    const int style = (int)num(a[13]);
+    const int style = num32(a[13]);
     Ref y;
     if (!none(a[15])) y.share(a[15]);
     else y.own(fresh(X, {T, Hq * D}, at::kBFloat16));
@@ -514,7 +520,7 @@ PyObject* prefix_attention(PyObject* const* a) {
     if (Hq <= 0 || Hkv <= 0 || D <= 0 || Hq > 65536 || Hkv > 65536 || D > 65536 || Q.size(1) < Hq * D) reject("Q: bf16 [T, Hq D]");
     const Cache K(a[4], Hkv, D, Q), V(a[5], Hkv, D, Q);
     if (K.pages != V.pages || K.page_size != V.page_size) reject("the two caches differ in shape");
-    const int32_t* pp = ints(a[6], P > 0 ? (P + K.page_size - 1) / K.page_size : 0, Q, "prefix_pages: int32, one a page of the prefix");
+    const int32_t* pp = ints(a[6], P > 0 ? (P - 1) / K.page_size + 1 : 0, Q, "prefix_pages: int32, one a page of the prefix");
     const at::Tensor& table = tensor(a[8]);
     if (!(table.dim() == 2 && table.scalar_type() == at::kInt && table.is_contiguous() && table.device() == Q.device())) reject("block_table: int32 [B, pages]");
     const int64_t B = table.size(0);

@@ -188,3 +188,29 @@ def test_binding_refuses_other_types_of_16_bits():
                     call(**dict(good, **{name: good[name].view(bits)}))
     with pytest.raises(AssertionError, match="bf16"):
         osc.osc_prefix_attention(**attn, out=(h(5, 512).half(), None))
+
+
+def test_binding_refuses_numbers_that_do_not_fit():
+    """numbers past 32 bits are refused, not cut to some other number; a cache whose pages hold nothing is refused before anything is divided by its page size"""
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    h = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    wrap = 2 ** 32
+    slots = dict(kv_lens=i(3), q_lens=i(3), free_pages=i(9), n_free=i(1), block_table=i(3, 4), page_size=16, T=8)
+    for k, v in (("page_size", wrap + 16), ("page_size", -wrap + 16), ("pos_base", wrap), ("pos_base", 2 ** 31)):
+        with pytest.raises(AssertionError, match="32 bits"):
+            osc.osc_page_slots(**dict(slots, **{k: v}))
+    rope = dict(QKV=h(5, 768), Hq=4, Hkv=1, D=128, cos_sin=torch.zeros(9, 128), positions=i(2, 5), slots=i(5), Kc=h(2, 1, 16, 128), Vc=h(2, 1, 16, 128), sections=[32, 32])
+    for k, v in (("style", wrap + 1), ("sections", [wrap + 32, 32]), ("sections", [32, 32 - wrap])):
+        with pytest.raises(AssertionError, match="32 bits"):
+            osc.osc_qk_norm_rope(**dict(rope, **{k: v}))
+    with pytest.raises(AssertionError, match="cos_sin"):
+        osc.osc_qk_norm_rope(**dict(rope, cos_sin=torch.zeros(0, wrap + 128)))
+    attn = dict(Q=h(5, 512), Hq=4, Hkv=1, D=128, Kc=h(4, 1, 16, 128), Vc=h(4, 1, 16, 128), prefix_pages=i(2), prefix_len=20, block_table=i(3, 4), kv_lens=i(3), q_offsets=i(4))
+    for bad in (h(4, 1, 0, 128), h(0, 1, wrap + 16, 128)):
+        with pytest.raises(AssertionError, match="cache"):
+            osc.osc_prefix_attention(**dict(attn, Kc=bad, Vc=bad))
+        with pytest.raises(AssertionError, match="cache"):
+            osc.osc_qk_norm_rope(**dict(rope, Kc=bad, Vc=bad))
+    for n in (2 ** 63 - 1, 2 ** 32):
+        with pytest.raises(AssertionError, match="prefix_pages"):
+            osc.osc_prefix_attention(**dict(attn, prefix_len=n))
