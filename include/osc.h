@@ -453,14 +453,14 @@ int osc_qk_norm_rope(const void *QKV, int64_t T, int32_t Hq, int32_t Hkv, int32_
  *   Q          bf16 [T, ldq], Hq heads of D (64 or 128) channels;  O bf16 [T, ldo], 16-byte aligned rows
  *   lse        float [T, Hq] or NULL: log of the softmax's denominator, log sum_j exp(scale * q . k_j)
  *   prefix_pages int32 [ceil(prefix_len / page_size)];  block_table int32 [B, ldt];  kv_lens int32 [B] (limited to what a
- *              row of the table can hold);  q_offsets int32 [B + 1], non-decreasing, within [0, T] (otherwise nothing is
+ *              row of the table can hold, and to 2^30 - 1);  q_offsets int32 [B + 1], non-decreasing, within [0, T] (otherwise nothing is
  *              computed); rows outside [q_offsets[0], q_offsets[B]) are not written
  *              A page outside [0, n_pages) is read as page 0: nothing outside the cache is touched.
  *              What pages hold past a request's last token does not matter; cached tokens must be finite.
  *   scale      > 0
  *   workspace  osc_prefix_attention_workspace_bytes(...) bytes, 256-byte aligned; contents do not matter and are
  *              not kept; calls that may overlap need one each.  35 to 230 MB for up to 4000 rows, whatever the lengths
- * B <= 8192, T * Hq < 2^31.  Results are identical from run to run.
+ * B <= 8192, T * Hq < 2^31, prefix_len <= 2^30 - 256.  Results are identical from run to run.
  * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_WORKSPACE, OSC_ERR_HIP.
  */
 size_t osc_prefix_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len);

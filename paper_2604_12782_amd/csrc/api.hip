@@ -788,7 +788,7 @@ int osc_prefix_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int3
     if (rc) return rc;
     REQUIRE(B >= 0 && ldt >= 0 && prefix_len >= 0, OSC_ERR_SHAPE, "%s: B=%d ldt=%lld prefix_len=%lld", who, B, (long long)ldt, (long long)prefix_len);
     REQUIRE(B <= PAGED_MAX_REQUESTS, OSC_ERR_UNSUPPORTED, "%s: %d requests (at most %d)", who, B, PAGED_MAX_REQUESTS);
-    REQUIRE(prefix_len <= 0x3fffffff && ldt <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "%s: prefix_len=%lld ldt=%lld", who, (long long)prefix_len, (long long)ldt);
+    REQUIRE(prefix_len <= ATTN_MAX_PREFIX && ldt <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "%s: prefix_len=%lld ldt=%lld", who, (long long)prefix_len, (long long)ldt);
     REQUIRE(ldq >= (int64_t)Hq * D && ldo >= (int64_t)Hq * D, OSC_ERR_SHAPE, "%s: ldq=%lld ldo=%lld", who, (long long)ldq, (long long)ldo);
     REQUIRE(Hq / Hkv <= 128, OSC_ERR_UNSUPPORTED, "%s: %d query heads a key/value head (at most 128)", who, Hq / Hkv);
     REQUIRE(scale > 0.0f && scale <= 1e6f, OSC_ERR_SHAPE, "%s: scale %g (a positive number)", who, (double)scale);

@@ -1109,7 +1109,7 @@ int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
     p.tpt = WROWS / p.G;
     p.K = static_cast<const uint8_t*>(a.K), p.V = static_cast<const uint8_t*>(a.V), p.n_pages = (uint32_t)a.n_pages, p.lg = a.lg;
     p.prefix_pages = a.prefix_pages, p.P = (int)a.prefix_len, p.table = a.table, p.ldt = a.ldt;
-    p.max_kv = (int)std::min<int64_t>(a.ldt << a.lg, 0x3fffffff);
+    p.max_kv = (int)std::min<int64_t>(a.ldt << a.lg, ATTN_MAX_TOKENS);
     p.kv_lens = a.kv_lens, p.q_offsets = a.q_offsets, p.B = a.B, p.per = (a.B + GROUPS - 1) / GROUPS, p.c = a.scale * 1.44269504088896341f;
     p.O = static_cast<uint16_t*>(a.O), p.ldo = a.ldo, p.lse = a.lse;
     p.pre_tiles = inline_tiles(a.T, a.B, a.Hq, a.Hkv, a.D, a.prefix_len);

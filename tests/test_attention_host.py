@@ -214,3 +214,9 @@ def test_binding_refuses_numbers_that_do_not_fit():
     for n in (2 ** 63 - 1, 2 ** 32):
         with pytest.raises(AssertionError, match="prefix_pages"):
             osc.osc_prefix_attention(**dict(attn, prefix_len=n))
+
+
+@pytest.mark.parametrize("code,change", [(UNSUPPORTED, dict(P=2 ** 30 - 1)), (UNSUPPORTED, dict(P=2 ** 30 - 255)), (WORKSPACE, dict(P=2 ** 30 - 256))])
+def test_attention_longest_prefix(code, change):
+    """a prefix and 2^30 - 1 tokens of a request's own, with what the plan adds to them, are counted in 31 bits"""
+    assert rc(ATTN, **change) == code
