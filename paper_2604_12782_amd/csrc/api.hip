@@ -771,7 +771,9 @@ int osc_qk_norm_rope(const void* QKV, int64_t T, int32_t Hq, int32_t Hkv, int32_
 }
 
 size_t osc_prefix_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
+    // as osc_prefix_attention: no size for what it refuses
     if (T < 0 || B < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || prefix_len < 0 || Hq / Hkv > 128) return 0;
+    if (Hq > 65536 / D || T > 0x7fffffff / Hq || B > PAGED_MAX_REQUESTS || prefix_len > ATTN_MAX_PREFIX) return 0;
     return prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len);
 }
 

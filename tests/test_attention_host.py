@@ -220,3 +220,15 @@ def test_binding_refuses_numbers_that_do_not_fit():
 def test_attention_longest_prefix(code, change):
     """a prefix and 2^30 - 1 tokens of a request's own, with what the plan adds to them, are counted in 31 bits"""
     assert rc(ATTN, **change) == code
+
+
+def test_workspace_size_as_documented():
+    """the sizes that the header names, and none for a call that would be refused"""
+    size = osc.osc_prefix_attention_workspace_bytes
+    for mb, args in ((34, (1, 1, 32, 8, 128, 0)), (26, (1, 1, 24, 8, 64, 0)), (180, (64, 64, 32, 8, 128, 8192)), (103, (8192, 1, 32, 8, 128, 0)),
+                     (227, (4000, 40, 32, 8, 128, 4096)), (770, (4000, 256, 32, 8, 128, 32700)), (1193, (8192, 8192, 32, 8, 128, 0))):
+        assert round(size(*args) / 1e6) == mb, args
+    for T, B, Hq, Hkv, D, P in ((2 ** 31, 4, 1, 1, 64, 0), (2 ** 27, 4, 32, 8, 128, 0), (2 ** 62, 1, 32, 8, 128, 0), (4, 8193, 8, 2, 128, 0), (4, 4, 8, 2, 128, 2 ** 30 - 255),
+                                (4, 4, 8, 2, 128, 2 ** 62), (4, 4, 1024, 1024, 128, 0), (4, 4, 129, 1, 64, 0)):
+        assert size(T, B, Hq, Hkv, D, P) == 0
+        assert rc(ATTN, T=T, B=B, Hq=Hq, Hkv=Hkv, D=D, P=P, ldq=Hq * D, ldo=Hq * D) == UNSUPPORTED
