@@ -447,7 +447,8 @@ int osc_qk_norm_rope(const void *QKV, int64_t T, int32_t Hq, int32_t Hkv, int32_
  * whole prefix and the request's own tokens 0 .. L - n + i, L = kv_lens[b] (its new tokens are in the cache by now):
  *   O[t, h] = sum_j softmax_j(scale * Q[t, h] . K[j, h / (Hq/Hkv)]) V[j, h / (Hq/Hkv)]
  * Scores and sums are single precision; the weights are rounded to bf16 for the second product (their sum is
- * not), O is rounded once.  A row that sees nothing (no prefix, L - n + i < 0) gives zeros, and lse -infinity.
+ * not), O is rounded once.  A row that sees nothing (no prefix, L - n + i < 0) gives zeros, and lse -infinity.  A head of
+ * queries with NaN or infinity gives NaN in both (zeros and -infinity where all its scores are -infinity), and touches no other.
  * The prefix is read once for all rows of short requests, not once a request, but where it is so short that they
  * can all walk it at once (it then comes from the caches).
  *   Q          bf16 [T, ldq], Hq heads of D (64 or 128) channels;  O bf16 [T, ldo], 16-byte aligned rows

@@ -464,8 +464,11 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2bf));  // nearest even
 }
+// A row without weight has seen nothing: zeros, and -infinity.  A weight that is NaN (queries that are not finite) is not taken for
+// none: it makes the row NaN, whichever way its sums are finished.
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
 __device__ __forceinline__ float lse_of(float base, float sum) {
-    return sum > 0.0f ? (base + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+    return sum == 0.0f ? -INFINITY : (base + __log2f(sum)) * 0.69314718055994531f;
 }
 __device__ __forceinline__ void lds_order() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -484,7 +487,7 @@ __device__ __forceinline__ void lds_barrier() {
 template <int D>
 __device__ __forceinline__ void leave(const AttnArgs& p, const State<D>& st, bool direct, int64_t t, int head, uint8_t* blk, int row, int hi) {
     if (direct) {
-        const float inv = st.sum > 0.0f ? 1.0f / st.sum : 0.0f;
+        const float inv = inverse(st.sum);
         uint16_t* out = p.O + t * p.ldo + head * D + 4 * hi;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
@@ -529,7 +532,7 @@ __device__ __forceinline__ void merge(const AttnArgs& p, const State<D>& st, uin
             f[k] = base == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(stats[k * 32 + row] - base);
             sum += f[k] * stats[128 + k * 32 + row];
         }
-        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const float inv = inverse(sum);
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
             const int piece = k * 8 + part;
@@ -1019,7 +1022,7 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
 #pragma unroll
         for (int d = 1; d < S; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
         const float next = fmaxf(base, top), fade = next == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(base - next);
-        const float f = wt > 0.0f ? __builtin_amdgcn_exp2f(bs - next) : 0.0f;
+        const float f = wt == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(bs - next);
         base = next;
         sum = fmaf(f, wt, sum * fade);
 #pragma unroll
@@ -1052,7 +1055,7 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
         const int u = H == 1 ? 0 : sub * ROWS + q;
         const float total = __shfl(sum, u * S);
         const bool write = __shfl((int)done, u * S) == 0 && head0 + u < p.Hq && (H != 1 || sub == 0);
-        const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+        const float inv = inverse(total);
         if (write)
             *reinterpret_cast<uint2*>(p.O + (int64_t)t * p.ldo + (head0 + u) * D + l * 4) =
                 make_uint2(pack2(acc[q].x * inv, acc[q].y * inv), pack2(acc[q].z * inv, acc[q].w * inv));

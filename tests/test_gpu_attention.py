@@ -485,3 +485,40 @@ def test_step_in_a_graph_and_on_a_stream(osc):
                 a, b = (a[:m], b[:m]) if i >= 6 else (a, b)
                 assert torch.equal(a, b), (k, i)
             assert torch.equal(table, t2) and torch.equal(K, K2) and torch.equal(V, V2)
+
+
+# ways through the attention that differ in where a row's sums are finished
+WAYS = [("an item a workgroup", lambda D: make(41, 20, 300, list(range(3, 203, 10)), [1] * 18 + [40, 9], 8, 2, D, 16)),
+        ("workgroups' pieces, joined", lambda D: make(42, 6, 0, [900, 40, 1200, 7, 650, 33], [1, 2, 1, 1, 1, 3], 8, 2, D, 32)),
+        ("long lines, cut", lambda D: make(43, 5, 0, [5000, 1, 7000, 333, 2600], [1, 1, 1, 2, 1], 16, 8, D, 32)),
+        ("wavefronts' pieces, joined", lambda D: make(44, 110, 0, [20 + (37 * b) % 280 for b in range(110)], [1] * 110, 8, 8, D, 64)),
+        ("whole tiles of prompts", lambda D: make(45, 3, 0, [150, 1, 290], [150, 1, 190], 4, 1, D, 32)),
+        ("packed rows", lambda D: make(46, 120, 1300, [1 + (11 * b) % 60 for b in range(120)], [1] * 120, 8, 8, D, 32)),
+        ("packed rows and cut prompts, four rows joined a wavefront", lambda D: make(47, 61, 9000, [1 + (13 * b) % 60 for b in range(60)] + [150], [1] * 60 + [130], 24, 8, D, 64))]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("way", range(len(WAYS)), ids=[w for w, _ in WAYS])
+def test_attention_queries_that_are_not_finite(osc, way, D):
+    """NaN or infinity in a head of a row of queries: that head's result and lse are NaN whichever way it takes; the others are what they
+    were (both within the tolerance above, with the largest |v| for the weighted average, 2^-12 of it for the scores' errors, 2^-10 for those of lse)"""
+    s = WAYS[way][1](D)
+    T, Hq = s["Q"].shape[0], s["Hq"]
+    before, lse_before = call(osc, s)
+    offs, kv = s["offs"].cpu().numpy(), s["kv"].cpu().numpy()
+    b = np.searchsorted(offs, np.arange(T), side="right") - 1
+    sees = s["P"] + kv[b] - (offs[b + 1] - np.arange(T)) + 1
+    rows = [t for t in range(T) if sees[t] >= 30]  # keys of either sign, so that an infinite element makes infinite scores of either sign
+    bad = torch.zeros((T, Hq), dtype=torch.bool, device=DEV)
+    for k, t in enumerate(rows[::max(1, len(rows) // 9)]):
+        bad[t, 5 * k % Hq] = True
+        s["Q"].view(T, Hq, D)[t, 5 * k % Hq, 29 * k % D] = float("nan") if k % 2 else float("inf")
+    assert bad.sum() >= 3
+    o, lse = call(osc, s)
+    o, before = o.view(T, Hq, D), before.view(T, Hq, D)
+    assert torch.isnan(o[bad]).all() and torch.isnan(lse[bad]).all()
+    top = torch.nan_to_num(s["V"]).abs().max().double()
+    err = (o.double() - before.double()).abs()[~bad]
+    assert (err <= 2 * (2.0 ** -8 * before.double().abs()[~bad] + (2.0 ** -8 + 2.0 ** -12) * top)).all()
+    assert torch.equal(torch.isinf(lse)[~bad], torch.isinf(lse_before)[~bad])
+    assert (torch.nan_to_num(lse - lse_before, 0.0)[~bad].abs() <= 2.0 ** -9).all() and not torch.isnan(lse[~bad]).any()
