@@ -56,12 +56,14 @@ def head_rope(x, gamma, eps, cos_sin, positions, sections, rot, pairs):
     return y, size
 
 
-def prefix_attention(q, K, V, prefix_pages, prefix_len, table, kv_lens, q_offsets, scale):
-    """q [T, Hq, D]; K, V [pages, Hkv, ps, D] -> (o [T, Hq, D], lse [T, Hq], average of |v| under the weights, largest sum of |q k|)"""
+def prefix_attention(q, K, V, prefix_pages, prefix_len, table, kv_lens, q_offsets, scale, rows=None):
+    """q [T, Hq, D]; K, V [pages, Hkv, ps, D] -> (o [T, Hq, D], lse [T, Hq], average of |v| under the weights, largest sum of |q k|);
+    `rows`: only these, others are left at zeros and -infinity"""
     T, Hq, D = q.shape
     Hkv, ps = K.shape[1], K.shape[2]
     G = Hq // Hkv
     o, av, lse, big = np.zeros((T, Hq, D)), np.zeros((T, Hq, D)), np.full((T, Hq), -np.inf), np.zeros((T, Hq))
+    wanted = np.ones(T, bool) if rows is None else np.isin(np.arange(T), rows)
 
     def tokens(C, pages, n):
         j = np.arange(n)
@@ -69,11 +71,11 @@ def prefix_attention(q, K, V, prefix_pages, prefix_len, table, kv_lens, q_offset
     for b in range(len(kv_lens)):
         t0, t1 = int(q_offsets[b]), int(q_offsets[b + 1])
         L = max(int(kv_lens[b]), 0)
-        if t0 == t1:
+        if not wanted[t0:t1].any():
             continue
-        k = np.concatenate([tokens(C, pg, n) for C, pg, n in ((K, prefix_pages, prefix_len), (K, table[b], L)) if n] or [np.zeros((0, Hkv, D))])
-        v = np.concatenate([tokens(C, pg, n) for C, pg, n in ((V, prefix_pages, prefix_len), (V, table[b], L)) if n] or [np.zeros((0, Hkv, D))])
-        for t in range(t0, t1):
+        k, v = (np.concatenate([tokens(C, pg, n) for pg, n in ((prefix_pages, prefix_len), (table[b], L)) if n] or [np.zeros((0, Hkv, D))])
+                for C in (K, V))
+        for t in np.flatnonzero(wanted[t0:t1]) + t0:
             n = prefix_len + max(0, L - (t1 - t0) + (t - t0) + 1)
             if n == 0:
                 continue

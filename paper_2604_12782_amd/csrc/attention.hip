@@ -149,6 +149,7 @@ __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, in
 // of the time of a narrow tile (2 us where a CU has two workgroups at it; 16 KB, 6 us where all wavefronts share 5.5 TB/s).  Where there are
 // wavefronts enough for pieces of 3, 6 or 12 tiles, items are rounded up to whole ones: a wavefront has parts of one item, and most
 // items are in one piece.  Where pieces are workgroups', the same with four times the tiles.
+// (Tests read it at the workspace's start, by the places of its members.)
 struct Plan {
     int narrow, wide;      // lengths of the lines
     int narrow0, items0;   // of which the prefix's narrow items are the first

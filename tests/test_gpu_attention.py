@@ -522,3 +522,126 @@ def test_attention_queries_that_are_not_finite(osc, way, D):
     assert (err <= 2 * (2.0 ** -8 * before.double().abs()[~bad] + (2.0 ** -8 + 2.0 ** -12) * top)).all()
     assert torch.equal(torch.isinf(lse)[~bad], torch.isinf(lse_before)[~bad])
     assert (torch.nan_to_num(lse - lse_before, 0.0)[~bad].abs() <= 2.0 ** -9).all() and not torch.isnan(lse[~bad]).any()
+
+
+# ---- the attention's ways, each shown to be taken --------------------------------------------------------------------------
+
+# the plan that the first kernel leaves at the workspace's start
+PLAN = ("narrow", "wide", "narrow0", "items0", "wide0", "head", "wide_per", "wide_piece", "a", "b", "cut", "with_wide", "others", "piece", "team", "rows", "tiles", "supers",
+        "super", "nbp", "valid", "joins")
+SOLO, CUT, TEAM, PIECE1, PIECE2, PIECE3 = -1, 0, 5, 3, 6, 12
+
+
+def lens(seed, B, lo, hi):
+    return np.random.default_rng(seed).integers(lo, hi + 1, B).tolist()
+
+
+# name: for heads of D channels, (prefix, tokens a request has, rows of it, Hq, Hkv, page size); what the plan has to say; rows joined a wavefront
+BRANCHES = {
+    "an item a workgroup": (lambda D: (300, list(range(3, 203, 10)), [1] * 18 + [40, 9], 8, 2, 16), dict(piece=SOLO, joins=0, rows=0, wide=0), 1),
+    "a wavefront's piece an item, nothing joined": (lambda D: (0, lens(1, 110, 1, 160), [1] * 110, 8, 8, 32), dict(piece=PIECE2, joins=0, wide=0), 1),
+    "workgroups' pieces": (lambda D: (0, [900, 40, 1200, 7, 650, 33], [1, 2, 1, 1, 1, 3], 8, 2, 32), dict(piece=TEAM, joins=1, items0=0), 1),
+    "wavefronts' pieces of 3": (lambda D: (0, lens(2, 110, 20, 200 if D == 128 else 300), [1] * 110, 8, 8, 64), dict(piece=PIECE1, joins=1, items0=0), 1),
+    "wavefronts' pieces of 6": (lambda D: (0, lens(3, 110, 250, 400), [1] * 110, 8, 8, 16), dict(piece=PIECE2, joins=1, items0=0), 1),
+    "wavefronts' pieces of 12": (lambda D: (0, lens(4, 70 if D == 128 else 110, 700, 1000), [1] * (70 if D == 128 else 110), 8, 8, 128), dict(piece=PIECE3, joins=1), 1),
+    "wavefronts' pieces of 12, four rows joined": (lambda D: (0, lens(4, 70 if D == 128 else 110, 700, 900), [1] * (70 if D == 128 else 110), 64, 8, 128),
+                                                   dict(piece=PIECE3, joins=1), 4),
+    "lines cut": (lambda D: (0, [5000, 1, 7000, 333, 2600], [1, 1, 1, 2, 1], 16, 8, 32), dict(piece=CUT, joins=1, items0=0, with_wide=0), 1),
+    "lines cut beside prompts": (lambda D: (0, [9000, 8000, 7000, 9500, 200], [1, 2, 1, 1, 160], 16, 8, 32), dict(piece=CUT, joins=1, wide_piece=SOLO), 1),
+    "one tile behind the prefix, workgroups' pieces": (lambda D: (2000, lens(5, 32, 1, 100), [1] * 32, 8, 8, 64), dict(piece=TEAM, items0=8, rows=32, tiles=0, joins=1), 1),
+    "one tile behind the prefix, wavefronts' pieces of 3": (lambda D: (8000 if D == 128 else 15000, lens(6, 32, 1, 60), [1] * 32, 8, 8, 64),
+                                                            dict(piece=PIECE1, items0=8, rows=32, tiles=0, joins=1), 1),
+    "one tile behind the prefix, wavefronts' pieces of 6": (lambda D: (18000, lens(7, 32, 150, 250), [1] * 32, 8, 8, 64) if D == 128 else
+                                                            (27000, lens(7, 32, 300, 350), [1] * 32, 8, 8, 64), dict(piece=PIECE2, items0=8, rows=32, tiles=0, joins=1), 1),
+    "one tile behind the prefix, lines cut": (lambda D: (15000 if D == 128 else 21000, [40, 300, 5, 17], [1] * 4, 32, 8, 64),
+                                              dict(piece=CUT, items0=8, rows=16, tiles=0, joins=1), 1),
+    "packed rows, a tile": (lambda D: (1300, lens(8, 120, 1, 60), [1] * 120, 8, 8, 32), dict(tiles=1, supers=5, rows=120, joins=1), 1),
+    "packed rows, two tiles": (lambda D: (3000, lens(9, 200, 1, 60), [1] * 200, 8, 8, 32), dict(tiles=2, supers=10, rows=200, joins=1), 1),
+    "packed rows, five tiles, four rows joined": (lambda D: (5000, lens(9, 140, 1, 60), [1] * 140, 32, 8, 32), dict(tiles=5, rows=560, joins=1), 4),
+    "packed rows beside long requests": (lambda D: (9000, lens(10, 150, 1, 60) + [300], [1] * 150 + [260], 2, 2, 64),
+                                         dict(tiles=2, supers=3, rows=150, wide_piece=CUT, joins=1), 1),
+    "packed rows beside long requests, four rows joined": (lambda D: (4200, lens(10, 80, 1, 60) + [150], [1] * 80 + [130], 24, 4, 64),
+                                                           dict(tiles=4, supers=2, rows=480, wide_piece=CUT, joins=1), 4),
+    "prompts cut": (lambda D: (0, [2100, 900], [70, 61], 4, 1, 64), dict(wide_piece=CUT, narrow=0, rows=0, joins=1), 1),
+    "prompts behind a prefix cut": (lambda D: (3000, [300, 300], [70, 90], 4, 1, 64), dict(wide_piece=CUT, narrow=0, rows=0, joins=1), 1),
+    "prompts behind a prefix cut, four rows joined": (lambda D: (2000, [300, 300], [70, 75], 32, 8, 64), dict(wide_piece=CUT, narrow=0, rows=0, joins=1), 4),
+    "prompts whole": (lambda D: (0, [150, 1, 290], [150, 1, 190], 4, 1, 32), dict(wide_piece=SOLO, wide_per=1, joins=0), 1),
+    "prompts whole, two tiles a workgroup": (lambda D: (0, [60] * 110, [40] * 110, 8, 8, 32), dict(wide_piece=SOLO, wide_per=2, joins=0), 4),
+}
+
+
+def check_some(osc, s, got, rows):
+    """check_attention at some rows; all of them are finite"""
+    pick = torch.as_tensor(rows, device=DEV)
+    T, Hq, D, scale = s["Q"].shape[0], s["Hq"], s["D"], s["scale"]
+    wo, wl, av, big = (w[rows] for w in ref.prefix_attention(f64(s["Q"]).reshape(T, Hq, D), f64(s["K"]), f64(s["V"]), s["prefix"].cpu().numpy(), s["P"], s["table"].cpu().numpy(),
+                                                             s["kv"].cpu().numpy(), s["offs"].cpu().numpy(), scale, rows))
+    o, lse = got
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+    n = s["P"] + int(s["kv"].max())
+    score = scale * (D + 4) * 2.0 ** -24 * big
+    err = np.abs(f64(o[pick]).reshape(len(rows), Hq, D) - wo)
+    assert (err <= 2.0 ** -8 * np.abs(wo) + (2.0 ** -8 + 2 * score[..., None] + 2.0 ** -18) * av).all(), (err / (av + 1e-30)).max()
+    assert (np.abs(f64(lse[pick]) - wl) <= score + 2.0 ** -21 * (np.abs(wl) + scale * big) + (n + 8) * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("name", BRANCHES)
+def test_attention_ways(osc, name, D):
+    """each way through the plan: it is the one taken, its results are right, and they are the same bits from run to run and whatever the workspace
+    held: all ones (NaN in the segments), zeros, another call's"""
+    args, want, together = BRANCHES[name]
+    P, kv, n, Hq, Hkv, ps = args(D)
+    s = make(len(name), len(kv), P, kv, n, Hq, Hkv, D, ps)
+    T = s["Q"].shape[0]
+    assert together == (1 if T * Hq <= 4096 else 4)
+    ws = torch.full((osc.osc_prefix_attention_workspace_bytes(T, len(kv), Hq, Hkv, D, P),), 255, dtype=torch.uint8, device=DEV)
+    first = call(osc, s, workspace=ws)
+    plan = dict(zip(PLAN, ws[:4 * len(PLAN)].view(torch.int32).tolist()))
+    assert {k: plan[k] for k in want} == want, plan
+    assert plan["valid"] == 1 and (plan["wide"] > 0) == (plan["with_wide"] > 0)
+    some = 1500000 // (Hq * (P + max(kv)))  # rows that the oracle takes about a second for
+    if T <= some:
+        check_attention(osc, s, got=first)
+    else:
+        check_some(osc, s, first, sorted(set(np.random.default_rng(1).integers(0, T, max(some, 6)).tolist()) | {0, T - 1}))
+    for fill in (0, None):
+        if fill is not None:
+            ws.fill_(fill)
+        again = call(osc, s, workspace=ws)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(32, 8, 128), (24, 8, 64)])
+@pytest.mark.parametrize("n", [2048, 8192])
+def test_attention_long_prompts(osc, Hq, Hkv, D, n):
+    """a prompt of full length, at rows all over it"""
+    s = make(n + D, 1, 0, [n], [n], Hq, Hkv, D, 64)
+    check_some(osc, s, call(osc, s), [0, 1, 31, 32, 127, 128, 1000, n // 2 - 1, n // 2, n - 129, n - 2, n - 1])
+    s = make(n + D + 1, 3, 300, [n // 2 + 40, 5, 900], [n // 2, 1, 700], Hq, Hkv, D, 32)
+    check_some(osc, s, call(osc, s), [0, 255, 256, n // 4, n // 2 - 1, n // 2, n // 2 + 1, n // 2 + 700])
+
+
+@pytest.mark.parametrize("B", [4, 300])
+def test_attention_leaves_other_rows_alone(osc, B):
+    """offsets that fall, or that name rows past the end, compute nothing; rows outside those that the offsets name keep what they hold"""
+    kv, n = [5 + b % 40 for b in range(B)], [1 + b % 3 for b in range(B)]
+    s = make(50 + B, B, 40, kv, n, 4, 2, 64, 16)
+    T = s["Q"].shape[0]
+    offs = s["offs"].cpu().numpy()
+    swapped, high, negative = offs.copy(), offs.copy(), offs.copy()
+    swapped[[1, 2]] = swapped[[2, 1]]
+    high[-1] = T + 1
+    negative[0] = -1
+    for bad in (swapped, high, negative, offs[::-1].copy(), np.full_like(offs, 2 ** 31 - 1), np.full_like(offs, -2 ** 31)):
+        o, lse = torch.full((T, 256), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((T, 4), 7.0, device=DEV)
+        call(osc, dict(s, offs=i32(bad)), out=(o, lse))
+        assert (o == 7).all() and (lse == 7).all()
+    # the same requests, rows before and behind them
+    more = torch.randn(T + 24, 256, device=DEV).bfloat16()
+    more[11:11 + T] = s["Q"]
+    o, lse = torch.full((T + 24, 256), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((T + 24, 4), 7.0, device=DEV)
+    call(osc, dict(s, Q=more, offs=i32(offs + 11)), out=(o, lse))
+    for x in (o, lse):
+        assert (x[:11] == 7).all() and (x[11 + T:] == 7).all()
+    check_attention(osc, s, got=(o[11:11 + T].contiguous(), lse[11:11 + T].contiguous()))
