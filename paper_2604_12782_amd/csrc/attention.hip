@@ -44,28 +44,34 @@ constexpr int attn_wgs() { return D == 128 ? 512 : 768; }
 //   CUT   long lines, cut where the workgroups' pieces end
 // By wavefronts, each its own: items rounded up to pieces of 3, 6 or 12 tiles, the shortest that the wavefronts can take at once; not where
 // items would come to more than FEW_PIECES of the longest each, whose joining costs more than the merges in LDS do.
-// us, 32 heads of 128 on 8, this rule / without the variant:  SOLO 32 requests behind 390 tokens 15.3 / 20.6, and with four times the limits 16
-// of up to 2000 tokens 31.2 instead of 25.1;  TEAM 4 of up to 1000 tokens 16.2 / 17.4;  wavefronts' pieces 100 of up to 100 tokens 15.4 / 25.5 (20.4 without the
-// rule for pieces of 6), 200 behind 200 27.2 / 38.5, 100 behind 3000 35.8 / 43.9;  FEW_PIECES 16 of up to 8000 tokens 55.7 / 62.7, one behind
-// 30000 39.5 / 50.2, 8 behind 12000 with 2000 of their own 31.6 / 41.0.
+// Here and below: us, 32 heads on 8, heads of 128 and in brackets of 64; "of up to n tokens" is n/B, 2n/B .. n, up to 100 of their own where
+// nothing is said.  This rule / without the variant:  SOLO 32 requests behind 390 tokens 17.0 / 21.4 (14.1 / 17.4), and with four times the limits
+// 16 of up to 2000 tokens 32.2 instead of 26.2 (25.4, 20.1);  TEAM 4 of up to 1000 tokens 16.5 / 17.6 (14.4 / 15.0);  wavefronts' pieces 100 of up to
+// 100 tokens 16.7 / 26.1, 20.3 without the rule for pieces of 6 (13.3 / 21.9, 17.2), 200 behind 200 25.8 / 35.8 (22.2 / 27.0), 100 behind 3000
+// 35.3 / 43.1 (25.8 / 29.1);  FEW_PIECES 16 of up to 8000 tokens 65.2 / 69.6 (39.5 / 40.8), one behind 30000 38.8 / 50.9 (26.0 / 35.6), 8 behind
+// 12000 with up to 2000 of their own 33.2 / 42.7 (23.9 / 27.9).
 enum { CUT = 0, SOLO = -1, TEAM = 5, PIECE1 = 3, PIECE2 = 6, PIECE3 = 12 };
 constexpr int SOLO_FEW = 512, SOLO_MANY = 1024, FEW_PIECES = 4;
-// Short requests walk the prefix themselves, tile after tile of their own items, where that is no more than this many tiles a wavefront (us
-// with 0, 4, 8: 32 requests behind 300 tokens 22.5, 15.3, 15.7; behind 1000 21.2, 21.3, 25.3; behind 1500 21.6, 22.0, 32.4).
+// Short requests walk the prefix themselves, tile after tile of their own items, where that is no more than this many tiles a wavefront
+// (with 0, 4, 8: 32 requests behind 300 tokens 23.4, 15.6, 16.0 (18.9, 12.7, 12.5); behind 1000 22.4, 22.3, 25.7 (17.9, 20.8, 21.2: heads of 64 would
+// do with less); behind 1500 22.5, 22.7, 32.7 (17.9, 18.0, 24.2)).
 constexpr int INLINE_TILES = 4;
 // The line of 32-row tiles is measured in tiles of 32 tokens, that of 128-row tiles in tokens.  Starting and ending a segment costs
 // about as much as the EDGEs; no piece is smaller than the MINs.  MIN_WIDE: pieces of packed rows where workgroups have no more than 16 narrow tiles
-// each (us with 256 against 512, 32 heads on 8, 32 requests behind 1000 tokens 21.0 / 25.4, 20 behind 9000 26.0 / 28.5), and prompts' where nothing is packed (66 rows behind 1000 tokens
-// of their own 22.7 / 26.2, with 192 22.0, but a prompt of 2000 then 32.8 / 29.0); twice that otherwise (100 behind 3000 40.7 / 37.0, 64 behind 8192 with 400 of
-// their own 53.9 / 45.4, 38 mixed of up to 107 rows behind 1112 41.5 / 39.4).
+// each (with 256 / 512: 32 requests behind 1000 tokens 22.3 / 26.8 (packed with heads of 128 alone), 20 behind 9000 26.4 / 29.4 (20.5 / 23.3)), and of
+// prompts where nothing is packed (66 new tokens behind 1000 of the request's own 24.3 / 28.5, with 192 25.6 (18.9 / 22.4, 19.7)); twice that otherwise (with 512 / 256: 100
+// behind 2000 with up to 2000 of their own 101 / 109 (60.4 / 62.2), 256 behind 1500 with up to 1000 135 / 145 (73.6 / 81.7); 30 decoding requests and 8
+// prompts of 20 to 107 behind 1112 with up to 600 69.2 / 69.5 (38.8 / 44.0)).
 constexpr int CUT_EDGE = 4, PIECE_EDGE = 1, MIN_NARROW = 8, WIDE_EDGE = 128, MIN_WIDE = 256;
 // Wide tiles are dealt out whole, as many to every workgroup, and not joined, where the longest ones take no more than cut pieces and their joining:
-// JOIN_COST tokens, and one for 2^JOIN_ROWS rows.  us, 32 heads on 8, whole / cut: a prompt of 512 tokens 17 / 28, of 6000 61 / 78, 16 of up to 1000
-// 89 / 118;  12 of up to 20 behind up to 830 tokens of their own 30 / 24, 6 of up to 80 behind 900 36 / 27.
+// JOIN_COST tokens, and one for 2^JOIN_ROWS rows.  Whole / cut, the rule takes the whole ones: a prompt of 512 tokens 21.9 / 31.2 (16.9 / 24.2), of 2048
+// 67 / 80 (48.8 / 57.0), 16 of 500 97 / 129 (61.5 / 91.7);  it cuts: a prompt of 8192 657 / 655 (381 / 380), 66 new tokens behind 4000 of the request's own 89 / 33
+// (63 / 24), 300 behind 6000 132 / 61 (94 / 42), 12 of 20 behind 4000 each 92 / 65 (65 / 42), 30 of 40 behind 2000 87 / 83 (56 / 52), 12 of up to 20 behind 830 32 / 25 (25 / 21).
+// It still cuts where whole tiles would do better: 12 of 20 behind 830 each 29.8 / 32.2 (23.1 / 24.1), 6 of 80 behind 900 32.3 / 40.1 (24.4 / 30.4).
 constexpr int JOIN_COST = 512, JOIN_ROWS = 6;
 constexpr int SUPER = 4096, MAX_SUPER = 16;
-// Rows of a long request, with a prefix and without (us with 128, 256, 512, 24 prompts behind 4000 tokens: of up to 80 tokens 105, 103, 96; of up to 120
-// 144, 149, 155).
+// Rows of a long request, with a prefix and without (with 128, 256, 512, 24 prompts behind 4000 tokens: of 40 tokens 123, 98, 104 (80, 65, 71), of 80 180, 179,
+// 174 (114, 112, 113), of 120 244, 244, 274 (131, 130, 158)).
 constexpr int LONG_PREFIX = 256, LONG = 33;
 
 struct AttnArgs {
