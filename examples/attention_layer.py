@@ -72,9 +72,11 @@ class Batch:
 
 def prefill_prefix(layer, x, free_pages):
     """The shared prompt, run as a single request: -> (its pages, the pages that are left)"""
+    pages = -(-x.shape[0] // layer.page_size)
+    if pages > free_pages.numel():
+        raise ValueError(f"the shared prompt takes {pages} pages, {free_pages.numel()} are free")
     one = Batch(layer, 1, x.shape[0], free_pages)
     one.step(x, torch.tensor([x.shape[0]], dtype=torch.int32, device=DEV))
-    pages = -(-x.shape[0] // layer.page_size)
     return one.table[0, :pages].clone(), free_pages[:free_pages.numel() - pages]
 
 
@@ -110,6 +112,8 @@ def main():
     rows = lambda n: torch.randn(n, layer.hidden, device=DEV).bfloat16()
     prefix_pages, free = prefill_prefix(layer, rows(a.prefix), free)
     batch = Batch(layer, a.requests, a.steps + 16, free, prefix_pages, a.prefix)
+    if a.requests * batch.table.shape[1] > free.numel():
+        raise SystemExit(f"{a.requests} requests of {a.steps + 4} tokens take more than the {free.numel()} pages that are free")
     one = torch.ones(a.requests, dtype=torch.int32, device=DEV)
     x = rows(a.requests)
     for _ in range(4):

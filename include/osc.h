@@ -389,7 +389,7 @@ int osc_dual_gemm_g16(const uint8_t *Xq, const uint8_t *Xs16, float x_tensor_sca
  *            free_pages[n_free - 1 - n]; it goes into block_table[b] behind those the request has
  *   refused  a request whose kv + q tokens do not fit a row of the table (it asks for no page), or whose pages,
  *            counted over all requests up to and with it, exceed n_free while it needs any: it keeps its length, its
- *            table row is not written, its new tokens get slot -1
+ *            table row is not written, its new tokens get slot -1 (they keep their rows, whose results mean nothing)
  *   token i of request b is row q_offsets[b] + i: position pos_base + kv + i, slot as above (-1 where the page number, from the
  *            table or the free list, is negative or its slots exceed 2^31-1)
  *   free_pages   int32 [n_pool];  n_free int32 [1]: how many of them, from the start, are free (limited to n_pool)

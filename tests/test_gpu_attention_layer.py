@@ -61,3 +61,14 @@ def test_pages_run_out(ex):
     assert s[4].tolist() == [0, 1, 2, 3] and s[0].tolist() == [17, 16, 16] and s[3].tolist()[1:] == [-1, -1]
     want = ex.plain_attention(layer, batch, q, s)
     assert ((o[0].double() - want[0]).abs() <= 2.0 ** -8 * want[0].abs() + 2.0 ** -7 * layer.V.abs().max()).all()
+
+
+def test_shared_prompt_without_pages(ex):
+    """A shared prompt that the cache cannot hold is an error, not a prefix of pages that nothing was written to."""
+    layer = ex.Layer(hidden=512, Hq=4, Hkv=2, D=64, pages=8, page_size=16, max_pos=200)
+    x = torch.randn(49, 512, device="cuda").bfloat16()
+    free = torch.arange(5, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="4 pages, 3 are free"):
+        ex.prefill_prefix(layer, x, free[:3])
+    prefix_pages, left = ex.prefill_prefix(layer, x, free)
+    assert sorted(prefix_pages.tolist() + left.tolist()) == [0, 1, 2, 3, 4] and prefix_pages.numel() == 4
