@@ -475,6 +475,132 @@ int osc_prefix_attention(const void *Q, int64_t T, int32_t Hq, int32_t Hkv, int3
                          const int32_t *q_offsets, int32_t B, float scale, void *O, int64_t ldo, float *lse,
                          void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- trees of drafted tokens --------------------------------------------------------------------- */
+
+/*
+ * A step that scores several drafted tokens of a request at once.  A request's new tokens are its rows q_offsets[b] ..
+ * q_offsets[b+1] - 1 of the step, as above; row i continues row parents[i] < i of the same request, or only what is cached (any other
+ * number).  Row 0 is the token that is known, the others are drafts.  A request of more than 64 * words new tokens is no tree but
+ * a piece of a prompt: each of its rows sees all before it, and its mask is not read.
+ * The step: osc_page_slots, osc_tree_mask, osc_qk_norm_rope with the tree's positions, osc_tree_attention; then logits, a token chosen for
+ * every row (the largest logit, or one drawn), osc_tree_accept, osc_cache_move and osc_page_free.
+ *
+ * osc_tree_mask: bits and positions from parents.
+ *   mask       uint64 [T, ldm], ldm >= words: bit j % 64 of word j / 64 of a row is set for itself and every row that it continues, directly or
+ *              not.  Words of rows without a tree or a request are 0
+ *   positions  int32 [T]: pos_base + kv_lens[b] - n + the number of rows that the row continues (i where there is no tree); -1 for rows
+ *              of no request, as osc_page_slots writes them (positions may be written over)
+ *   kv_lens    int32 [B]: lengths after the step, as for the attention;  words  1 to 8
+ * Offsets as for the attention; a request whose offsets fall or leave [0, T] is left out.  No array that is written may overlap another.
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
+ */
+int osc_tree_mask(const int32_t *parents, const int32_t *q_offsets, const int32_t *kv_lens, int32_t B, int64_t T, int32_t pos_base,
+                  int32_t words, uint64_t *mask, int64_t ldm, int32_t *positions, void *stream);
+
+/*
+ * osc_prefix_attention, whose arguments and notes these are, for trees: row i of a request sees the prefix, the request's tokens
+ * 0 .. L - n - 1, and those new tokens j <= i whose bit its words hold.  A row need not see itself; one that sees nothing gives zeros and
+ * -infinity.  Bits of later rows are ignored, so any mask under the diagonal will do, not only a tree's.
+ *   mask       uint64 [T, ldm], 8-byte aligned;  words  1 to 8, ldm >= words
+ *   workspace  osc_tree_attention_workspace_bytes(...) bytes
+ */
+size_t osc_tree_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len);
+int osc_tree_attention(const void *Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void *Kc, const void *Vc,
+                       int64_t n_pages, int32_t page_size, const int32_t *prefix_pages, int64_t prefix_len, const int32_t *block_table,
+                       int64_t ldt, const int32_t *kv_lens, const int32_t *q_offsets, int32_t B, const uint64_t *mask, int32_t words,
+                       int64_t ldm, float scale, void *O, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The path that the model agrees with.  It starts at row 0; from a row it goes on at the lowest row that continues it and whose token
+ * is the one chosen there, and ends where there is none.
+ *   tokens     int32 [T]: the rows' tokens; a negative number is a token that is not drafted (a prompt's): it is accepted
+ *              after the row that it continues, whatever was chosen
+ *   choices    int32, row t's at choices[t * ldc], ldc >= 1: the token that follows row t (osc_token_logprobs' top_ids with ldc = top_k)
+ *   slots      int32 [T] from osc_page_slots.  A request whose row 0 has slot -1 got no pages: it accepts nothing and keeps its length
+ *   path, src_slots  int32 [T]: from row q_offsets[b] on, the accepted rows' numbers inside the request, ascending, and their slots; -1 behind
+ *              them and in rows of no request.  osc_cache_move(src_slots, slots, q_offsets) moves the accepted tokens together
+ *   n_accepted int32 [B];  next_tokens int32 [B]: the choice at the path's end, -1 for a request without rows or pages
+ *   kv_lens_out int32 [B]: kv_lens[b] - n + n_accepted[b] (kv_lens[b] where there are no rows or pages)
+ * Offsets as for osc_tree_mask.  No array that is written may overlap another.
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
+ */
+int osc_tree_accept(const int32_t *parents, const int32_t *tokens, const int32_t *choices, int64_t ldc, const int32_t *q_offsets,
+                    const int32_t *kv_lens, const int32_t *slots, int32_t B, int64_t T, int32_t *path, int32_t *n_accepted,
+                    int32_t *next_tokens, int32_t *kv_lens_out, int32_t *src_slots, void *stream);
+
+/* ---- pages and cached tokens in other hands -------------------------------------------------------- */
+
+/*
+ * Keys and values of slots src_slots[i] written to slots dst_slots[i], every head, in all layers of a cache at once.
+ *   Kc, Vc     bf16 [n_layers][n_pages][Hkv][page_size][D], layers layer_stride elements apart (a multiple of 8), 16-byte aligned;
+ *              D 64 or 128
+ *   src_slots, dst_slots  int32 [T]; a pair with a slot outside the cache (-1), or with the same slot twice, moves nothing
+ *   offsets    int32 [N + 1]: pairs offsets[g] .. offsets[g+1] - 1 are a group (one that leaves [0, T] is left out); NULL: N groups of T / N pairs
+ * Groups are moved at the same time, pairs of a group in order: a slot may be written after it was read in the same group (tokens moved
+ * towards a sequence's start), but not read or written again after it was written, nor be in two groups if one of them writes it.
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
+ */
+int osc_cache_move(void *Kc, void *Vc, int32_t n_layers, int64_t layer_stride, int64_t n_pages, int32_t Hkv, int32_t page_size, int32_t D,
+                   const int32_t *src_slots, const int32_t *dst_slots, const int32_t *offsets, int32_t N, int64_t T, void *stream);
+
+/*
+ * Requests that go on from another one's tokens (several continuations of a prompt, a search).  A page may belong to several
+ * rows of the table: refs[page] is the number of its holders beyond the first, 0 for every page that osc_page_slots deals.
+ * Fork f makes row dst[f] of the table, which must hold no pages (osc_page_free before), hold what row src[f] holds: full pages are shared and
+ * their refs rise by one; a page that is partly full, which both requests would write into, is not shared: the fork gets a fresh one, in the
+ * order of the forks from the end of the free list as in osc_page_slots, and its tokens are to be moved there by osc_cache_move.
+ *   refused    a fork whose src or dst is no request, whose dst is also a src or an earlier fork's dst, whose tokens do not fit a row of the
+ *              table (these ask for no page), or whose page, counted over all forks up to and with it, exceeds n_free while it needs one.
+ *              Its row and length stay as they are
+ *   src, dst   int32 [N];  kv_lens int32 [B], block_table int32 [B, ldt], refs int32 [n_pages]: in and out (pages outside [0, n_pages) are entered
+ *              but not counted, and nothing of them is moved)
+ *   free_pages int32 [n_pool], n_free int32 [1], info[0] the next n_free, as in osc_page_slots
+ *   src_slots, dst_slots  int32 [N, page_size]: the pairs for osc_cache_move (offsets NULL), -1 where nothing is moved
+ *   info       int32 [4]: pages left, pages taken, forks refused, shared entries of the table
+ * N, B <= 8192.  No array that is written may overlap another.
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
+ */
+int osc_page_fork(const int32_t *src, const int32_t *dst, int32_t N, int32_t B, int32_t page_size, int32_t *kv_lens, int32_t *block_table,
+                  int64_t ldt, int32_t *refs, int64_t n_pages, const int32_t *free_pages, int64_t n_pool, const int32_t *n_free,
+                  int32_t *src_slots, int32_t *dst_slots, int32_t *info, void *stream);
+
+/*
+ * Pages that requests no longer need.  Request b had kv_lens[b] tokens and keeps new_lens[b] (0 and less: none; NULL: none of any request): it
+ * lets go of the pages of its row from ceil(new / page_size) up to ceil(kv / page_size) - 1.  A page with refs[page] > 0 loses one
+ * holder; a page that was let go by its last one is appended to the free list.  Pages freed by one call are appended in the
+ * order of their numbers, each once, however often the rows name it.  The table is not written.
+ *   refs       int32 [n_pages] or NULL (every page has one holder), in and out
+ *   free_pages int32 [n_pool], in and out: the first n_free entries stay;  n_free int32 [1] (limited to n_pool); info[0] is the next one
+ *   info       int32 [4]: pages free afterwards, pages appended, entries whose page has other holders, entries ignored (no page of [0, n_pages),
+ *              a page that was already free by this call, a page that the list has no room for)
+ * B <= 8192, B * ldt < 2^31.  No array that is written may overlap another.
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
+ */
+int osc_page_free(const int32_t *kv_lens, const int32_t *new_lens, int32_t B, int32_t page_size, const int32_t *block_table, int64_t ldt,
+                  int32_t *refs, int64_t n_pages, int32_t *free_pages, int64_t n_pool, const int32_t *n_free, int32_t *info, void *stream);
+
+/* ---- log probabilities ------------------------------------------------------------------------------- */
+
+/*
+ * Of every row x of logits, with p_j = exp(scale x_j) / sum_i exp(scale x_i):
+ *   logprobs   float [T, n_tokens]: log p of the given tokens, int32 tokens [T, n_tokens]; 0 for a token outside [0, V) (none is given)
+ *   top_ids, top_logprobs  int32, float [T, top_k]: the top_k tokens of the largest logits, largest first, of equal ones the lowest first
+ *   lse        float [T] or NULL: log sum_i exp(scale x_i)
+ *   entropy    float [T] or NULL: -sum_j p_j log p_j
+ * -infinity is a token that cannot come; a row of nothing else gives lse and log probabilities -infinity, entropy 0.  A row
+ * with NaN or +infinity gives NaN everywhere and ids -1.  Sums are single precision.
+ *   logits     float or bf16 (dtype OSC_DT_F32, OSC_DT_BF16) [T, ldl], ldl >= V >= 1; rows need no alignment but that of an element
+ *   top_k      0 to 64, at most V;  scale > 0 (1 / temperature)
+ *   workspace  osc_token_logprobs_workspace_bytes(T, V, top_k) bytes, 256-byte aligned (NULL where that is 0); contents do not matter and
+ *              are not kept; calls that may overlap need one each
+ * Results are identical from run to run.
+ * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_WORKSPACE, OSC_ERR_HIP.
+ */
+size_t osc_token_logprobs_workspace_bytes(int64_t T, int64_t V, int32_t top_k);
+int osc_token_logprobs(const void *logits, int dtype, int64_t T, int64_t V, int64_t ldl, float scale, const int32_t *tokens, int32_t n_tokens,
+                       int32_t top_k, float *logprobs, int32_t *top_ids, float *top_logprobs, float *lse, float *entropy, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
 /* ---- offline profiling (calibration) ------------------------------------------ */
 
 /*

@@ -70,6 +70,16 @@ _SIGS = {
     "osc_prefix_attention_workspace_bytes": (sz, [i64, i32, i32, i32, i32, i64]),
     "osc_prefix_attention": (C.c_int, [vp, i64, i32, i32, i32, i64, vp, vp, i64, i32, vp, i64, vp, i64, vp, vp, i32, C.c_float, vp, i64, vp,
                                        vp, sz, vp]),
+    "osc_tree_mask": (C.c_int, [vp, vp, vp, i32, i64, i32, i32, vp, i64, vp, vp]),
+    "osc_tree_attention_workspace_bytes": (sz, [i64, i32, i32, i32, i32, i64]),
+    "osc_tree_attention": (C.c_int, [vp, i64, i32, i32, i32, i64, vp, vp, i64, i32, vp, i64, vp, i64, vp, vp, i32, vp, i32, i64, C.c_float, vp,
+                                     i64, vp, vp, sz, vp]),
+    "osc_tree_accept": (C.c_int, [vp, vp, vp, i64, vp, vp, vp, i32, i64, vp, vp, vp, vp, vp, vp]),
+    "osc_cache_move": (C.c_int, [vp, vp, i32, i64, i64, i32, i32, i32, vp, vp, vp, i32, i64, vp]),
+    "osc_page_fork": (C.c_int, [vp, vp, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp]),
+    "osc_page_free": (C.c_int, [vp, vp, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp]),
+    "osc_token_logprobs_workspace_bytes": (sz, [i64, i64, i32]),
+    "osc_token_logprobs": (C.c_int, [vp, C.c_int, i64, i64, i64, C.c_float, vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
 }
 
 
@@ -458,3 +468,56 @@ def osc_prefix_attention(Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_
     [T, Hq] or None).  scale: D^-0.5 if None; workspace: uint8 device tensor of osc_prefix_attention_workspace_bytes(...), made here if None."""
     return (_native or _load_native()).prefix_attention(Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets,
                                                         scale, want_lse, workspace, out)
+
+
+def osc_tree_mask(parents, q_offsets, kv_lens, words=1, pos_base=0, out=None):
+    """Which new tokens every row of a step sees and where it stands, from the rows' parents (int32 [T]) -> (mask int64 [T, words], bit j % 64 of
+    word j / 64 for row j of the request; positions int32 [T])."""
+    return (_native or _load_native()).tree_mask(parents, q_offsets, kv_lens, words, pos_base, out)
+
+
+def osc_tree_attention_workspace_bytes(T, B, Hq, Hkv, D, prefix_len):
+    return lib().osc_tree_attention_workspace_bytes(T, B, Hq, Hkv, D, prefix_len)
+
+
+def osc_tree_attention(Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets, mask, scale=None, want_lse=False,
+                       workspace=None, out=None):
+    """osc_prefix_attention for trees of new tokens: a row sees those of them whose bit `mask` (int64 [T, words], from osc_tree_mask) holds ->
+    (O bf16 [T, Hq D], lse float32 [T, Hq] or None).  workspace: of osc_tree_attention_workspace_bytes(...), made here if None."""
+    return (_native or _load_native()).tree_attention(Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets, scale, want_lse,
+                                                      workspace, out, mask)
+
+
+def osc_tree_accept(parents, tokens, choices, q_offsets, kv_lens, slots, out=None):
+    """The path of every tree that the model agrees with -> (path int32 [T], n_accepted, next_tokens, kv_lens after [B], src_slots [T]).
+    choices int32 [T], or a column of osc_token_logprobs' top ids: the token that follows each row."""
+    return (_native or _load_native()).tree_accept(parents, tokens, choices, q_offsets, kv_lens, slots, out)
+
+
+def osc_cache_move(Kc, Vc, src_slots, dst_slots, offsets=None):
+    """Keys and values of slots src_slots written to slots dst_slots, in place.  Kc, Vc bf16 [pages, Hkv, page_size, D] or
+    [layers, pages, Hkv, page_size, D]; groups of pairs by `offsets` (int32 [groups + 1]), or the rows of 2-D slots."""
+    return (_native or _load_native()).cache_move(Kc, Vc, src_slots, dst_slots, offsets)
+
+
+def osc_page_fork(src, dst, kv_lens, block_table, refs, free_pages, n_free, page_size, out=None):
+    """Rows dst of the table go on from rows src (int32 [N]): kv_lens, block_table and refs are updated in place -> (src_slots, dst_slots int32
+    [N, page_size], the pairs for osc_cache_move; info int32 [4], info[:1] the next n_free)."""
+    return (_native or _load_native()).page_fork(src, dst, kv_lens, block_table, refs, free_pages, n_free, page_size, out)
+
+
+def osc_page_free(kv_lens, new_lens, block_table, free_pages, n_free, page_size, refs=None, n_pages=None, out=None):
+    """Pages behind new_lens (None: all) are let go of; refs and free_pages are updated in place -> info int32 [4], info[:1] the next n_free.
+    n_pages: of the cache; by default as many as refs, or else free_pages, has room for."""
+    return (_native or _load_native()).page_free(kv_lens, new_lens, block_table, free_pages, n_free, page_size, refs, n_pages, out)
+
+
+def osc_token_logprobs_workspace_bytes(T, V, top_k):
+    return lib().osc_token_logprobs_workspace_bytes(T, V, top_k)
+
+
+def osc_token_logprobs(logits, tokens=None, top_k=0, scale=1.0, workspace=None, out=None):
+    """Of rows of logits [T, V] (float32 or bf16), softmax of scale * logits -> (log probabilities of `tokens` (int32 [T] or [T, n]) or None,
+    ids int32 and log probabilities of the top_k [T, top_k] or None twice, lse [T], entropy [T]); float32.
+    workspace: uint8 device tensor of osc_token_logprobs_workspace_bytes(...), made here if None."""
+    return (_native or _load_native()).token_logprobs(logits, tokens, top_k, scale, workspace, out)

@@ -777,11 +777,16 @@ size_t osc_prefix_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, in
     return prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len);
 }
 
-int osc_prefix_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void* Kc, const void* Vc,
-                         int64_t n_pages, int32_t page_size, const int32_t* prefix_pages, int64_t prefix_len, const int32_t* block_table,
-                         int64_t ldt, const int32_t* kv_lens, const int32_t* q_offsets, int32_t B, float scale, void* O, int64_t ldo, float* lse,
-                         void* workspace, size_t workspace_bytes, void* stream) {
-    static const char* who = "osc_prefix_attention";
+// osc_prefix_attention, and osc_tree_attention where there is a mask
+struct TreeRows {
+    const uint64_t* mask;
+    int64_t ldm;
+    int32_t words;
+};
+static int attention(const char* who, const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void* Kc, const void* Vc, int64_t n_pages,
+                     int32_t page_size, const int32_t* prefix_pages, int64_t prefix_len, const int32_t* block_table, int64_t ldt, const int32_t* kv_lens,
+                     const int32_t* q_offsets, int32_t B, const TreeRows* tree, float scale, void* O, int64_t ldo, float* lse, void* workspace,
+                     size_t workspace_bytes, void* stream) {
     int lg = 0, rc = check_heads(who, T, Hq, Hkv, D);
     if (rc) return rc;
     rc = check_page_size(who, page_size, &lg);
@@ -794,7 +799,13 @@ int osc_prefix_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int3
     REQUIRE(ldq >= (int64_t)Hq * D && ldo >= (int64_t)Hq * D, OSC_ERR_SHAPE, "%s: ldq=%lld ldo=%lld", who, (long long)ldq, (long long)ldo);
     REQUIRE(Hq / Hkv <= 128, OSC_ERR_UNSUPPORTED, "%s: %d query heads a key/value head (at most 128)", who, Hq / Hkv);
     REQUIRE(scale > 0.0f && scale <= 1e6f, OSC_ERR_SHAPE, "%s: scale %g (a positive number)", who, (double)scale);
+    if (tree) {
+        REQUIRE(tree->words >= 1 && tree->words <= TREE_MAX_WORDS, OSC_ERR_UNSUPPORTED, "%s: %d words of 64 drafted tokens (1 to %d)", who, tree->words, TREE_MAX_WORDS);
+        REQUIRE(tree->ldm >= tree->words, OSC_ERR_SHAPE, "%s: ldm=%lld", who, (long long)tree->ldm);
+    }
     if (T == 0 || B == 0) return OSC_OK;
+    REQUIRE(!tree || tree->mask, OSC_ERR_NULL, "%s: null mask", who);
+    REQUIRE(!tree || aligned(tree->mask, 8), OSC_ERR_UNSUPPORTED, "%s: the mask must be 8-byte aligned", who);
     REQUIRE(Q && O && kv_lens && q_offsets && workspace && (block_table || ldt == 0) && (prefix_pages || prefix_len == 0), OSC_ERR_NULL,
             "%s: null pointer", who);
     REQUIRE((Kc && Vc && n_pages > 0) || (prefix_len == 0 && ldt == 0), OSC_ERR_NULL, "%s: no cache", who);
@@ -806,7 +817,177 @@ int osc_prefix_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int3
     a.Q = Q, a.T = T, a.Hq = Hq, a.Hkv = Hkv, a.D = D, a.ldq = ldq, a.K = Kc, a.V = Vc, a.n_pages = n_pages, a.lg = lg;
     a.prefix_pages = prefix_pages, a.prefix_len = prefix_len, a.table = block_table, a.ldt = ldt, a.kv_lens = kv_lens, a.q_offsets = q_offsets;
     a.B = B, a.scale = scale, a.O = O, a.ldo = ldo, a.lse = lse, a.workspace = static_cast<uint8_t*>(workspace);
+    a.mask = tree ? tree->mask : nullptr, a.ldm = tree ? tree->ldm : 0, a.words = tree ? tree->words : 0;
     return launch_prefix_attention(a, as_stream(stream));
+}
+
+int osc_prefix_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void* Kc, const void* Vc,
+                         int64_t n_pages, int32_t page_size, const int32_t* prefix_pages, int64_t prefix_len, const int32_t* block_table,
+                         int64_t ldt, const int32_t* kv_lens, const int32_t* q_offsets, int32_t B, float scale, void* O, int64_t ldo, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    return attention("osc_prefix_attention", Q, T, Hq, Hkv, D, ldq, Kc, Vc, n_pages, page_size, prefix_pages, prefix_len, block_table, ldt, kv_lens,
+                     q_offsets, B, nullptr, scale, O, ldo, lse, workspace, workspace_bytes, stream);
+}
+
+size_t osc_tree_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
+    return osc_prefix_attention_workspace_bytes(T, B, Hq, Hkv, D, prefix_len);
+}
+
+int osc_tree_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void* Kc, const void* Vc, int64_t n_pages,
+                       int32_t page_size, const int32_t* prefix_pages, int64_t prefix_len, const int32_t* block_table, int64_t ldt,
+                       const int32_t* kv_lens, const int32_t* q_offsets, int32_t B, const uint64_t* mask, int32_t words, int64_t ldm, float scale,
+                       void* O, int64_t ldo, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    const TreeRows tree{mask, ldm, words};
+    return attention("osc_tree_attention", Q, T, Hq, Hkv, D, ldq, Kc, Vc, n_pages, page_size, prefix_pages, prefix_len, block_table, ldt, kv_lens,
+                     q_offsets, B, &tree, scale, O, ldo, lse, workspace, workspace_bytes, stream);
+}
+
+// ---- trees of drafted tokens, pages in other hands, log probabilities ----
+
+// Arrays of 4-byte elements; the first `written` of them are written and may not overlap any other.
+struct Extent4 {
+    const char* name;
+    const void* at;
+    int64_t n;
+};
+static int check_apart(const char* who, const Extent4* a, int written, int all) {
+    for (int i = 0; i < written; ++i)
+        for (int j = i + 1; j < all; ++j) {
+            const uintptr_t x = (uintptr_t)a[i].at, y = (uintptr_t)a[j].at;
+            REQUIRE(a[i].n == 0 || a[j].n == 0 || !x || !y || x + a[i].n * 4 <= y || y + a[j].n * 4 <= x, OSC_ERR_UNSUPPORTED,
+                    "%s: %s, which is written, overlaps %s", who, a[i].name, a[j].name);
+        }
+    return OSC_OK;
+}
+
+static int check_step(const char* who, int32_t B, int64_t T) {
+    REQUIRE(B >= 0 && T >= 0, OSC_ERR_SHAPE, "%s: B=%d T=%lld", who, B, (long long)T);
+    REQUIRE(B <= PAGED_MAX_REQUESTS, OSC_ERR_UNSUPPORTED, "%s: %d requests (at most %d)", who, B, PAGED_MAX_REQUESTS);
+    REQUIRE(T <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "%s: T=%lld is above 2^31-1", who, (long long)T);
+    return OSC_OK;
+}
+
+int osc_tree_mask(const int32_t* parents, const int32_t* q_offsets, const int32_t* kv_lens, int32_t B, int64_t T, int32_t pos_base, int32_t words, uint64_t* mask,
+                  int64_t ldm, int32_t* positions, void* stream) {
+    static const char* who = "osc_tree_mask";
+    int rc = check_step(who, B, T);
+    if (rc) return rc;
+    REQUIRE(pos_base >= 0, OSC_ERR_SHAPE, "%s: pos_base=%d", who, pos_base);
+    REQUIRE(words >= 1 && words <= TREE_MAX_WORDS, OSC_ERR_UNSUPPORTED, "%s: %d words of 64 drafted tokens (1 to %d)", who, words, TREE_MAX_WORDS);
+    REQUIRE(ldm >= words && ldm <= 0x7fffffff, OSC_ERR_SHAPE, "%s: ldm=%lld", who, (long long)ldm);
+    if (T == 0) return OSC_OK;
+    REQUIRE(mask && positions && (B == 0 || (parents && q_offsets && kv_lens)), OSC_ERR_NULL, "%s: null pointer", who);
+    REQUIRE(aligned(mask, 8), OSC_ERR_UNSUPPORTED, "%s: the mask must be 8-byte aligned", who);
+    const Extent4 arrays[] = {{"mask", mask, ((T - 1) * ldm + words) * 2}, {"positions", positions, T}, {"parents", parents, T}, {"q_offsets", q_offsets, (int64_t)B + 1},
+                              {"kv_lens", kv_lens, B}};
+    rc = check_apart(who, arrays, 2, 5);
+    if (rc) return rc;
+    return launch_tree_mask(parents, q_offsets, kv_lens, B, T, pos_base, words, mask, ldm, positions, as_stream(stream));
+}
+
+int osc_tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* choices, int64_t ldc, const int32_t* q_offsets, const int32_t* kv_lens,
+                    const int32_t* slots, int32_t B, int64_t T, int32_t* path, int32_t* n_accepted, int32_t* next_tokens, int32_t* kv_lens_out, int32_t* src_slots,
+                    void* stream) {
+    static const char* who = "osc_tree_accept";
+    int rc = check_step(who, B, T);
+    if (rc) return rc;
+    REQUIRE(ldc >= 1 && ldc <= 0x7fffffff, OSC_ERR_SHAPE, "%s: ldc=%lld", who, (long long)ldc);
+    if (T == 0 && B == 0) return OSC_OK;
+    REQUIRE(T == 0 || (path && src_slots), OSC_ERR_NULL, "%s: null pointer", who);
+    REQUIRE(B == 0 || (q_offsets && kv_lens && n_accepted && next_tokens && kv_lens_out && (T == 0 || (parents && tokens && choices && slots))), OSC_ERR_NULL,
+            "%s: null pointer", who);
+    const Extent4 arrays[] = {{"path", path, T}, {"n_accepted", n_accepted, B}, {"next_tokens", next_tokens, B}, {"kv_lens_out", kv_lens_out, B}, {"src_slots", src_slots, T},
+                              {"parents", parents, T}, {"tokens", tokens, T}, {"choices", choices, T ? (T - 1) * ldc + 1 : 0}, {"q_offsets", q_offsets, (int64_t)B + 1},
+                              {"kv_lens", kv_lens, B}, {"slots", slots, T}};
+    rc = check_apart(who, arrays, 5, 11);
+    if (rc) return rc;
+    return launch_tree_accept(parents, tokens, choices, ldc, q_offsets, kv_lens, slots, B, T, path, n_accepted, next_tokens, kv_lens_out, src_slots,
+                              as_stream(stream));
+}
+
+int osc_cache_move(void* Kc, void* Vc, int32_t n_layers, int64_t layer_stride, int64_t n_pages, int32_t Hkv, int32_t page_size, int32_t D, const int32_t* src_slots,
+                   const int32_t* dst_slots, const int32_t* offsets, int32_t N, int64_t T, void* stream) {
+    static const char* who = "osc_cache_move";
+    int lg = 0, rc = check_heads(who, 0, Hkv, Hkv, D);
+    if (rc) return rc;
+    rc = check_page_size(who, page_size, &lg);
+    if (rc) return rc;
+    rc = check_cache(who, n_pages, lg, Hkv, Kc, Vc);
+    if (rc) return rc;
+    REQUIRE(n_layers >= 0 && N >= 0 && T >= 0 && (n_layers <= 1 || layer_stride >= (n_pages * Hkv << lg) * D), OSC_ERR_SHAPE,
+            "%s: n_layers=%d layer_stride=%lld N=%d T=%lld", who, n_layers, (long long)layer_stride, N, (long long)T);
+    REQUIRE(layer_stride % 8 == 0 || n_layers <= 1, OSC_ERR_UNSUPPORTED, "%s: layers must be 16-byte aligned", who);
+    REQUIRE(n_layers <= 65535 && T <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "%s: n_layers=%d T=%lld (at most 65535 and 2^31-1)", who, n_layers, (long long)T);
+    REQUIRE(offsets || N == 0 || T % N == 0, OSC_ERR_SHAPE, "%s: %lld pairs are not %d groups of the same size, and there are no offsets", who, (long long)T, N);
+    if (N == 0 || T == 0 || n_layers == 0 || n_pages == 0) return OSC_OK;
+    REQUIRE(Kc && Vc && src_slots && dst_slots, OSC_ERR_NULL, "%s: null pointer", who);
+    return launch_cache_move(Kc, Vc, n_layers, layer_stride, n_pages, Hkv, lg, D, src_slots, dst_slots, offsets, N, T, as_stream(stream));
+}
+
+int osc_page_fork(const int32_t* src, const int32_t* dst, int32_t N, int32_t B, int32_t page_size, int32_t* kv_lens, int32_t* block_table, int64_t ldt, int32_t* refs,
+                  int64_t n_pages, const int32_t* free_pages, int64_t n_pool, const int32_t* n_free, int32_t* src_slots, int32_t* dst_slots, int32_t* info,
+                  void* stream) {
+    static const char* who = "osc_page_fork";
+    int lg = 0, rc = check_page_size(who, page_size, &lg);
+    if (rc) return rc;
+    REQUIRE(N >= 0 && B >= 0 && ldt >= 0 && n_pages >= 0 && n_pool >= 0, OSC_ERR_SHAPE, "%s: N=%d B=%d ldt=%lld n_pages=%lld n_pool=%lld", who, N, B, (long long)ldt,
+            (long long)n_pages, (long long)n_pool);
+    REQUIRE(N <= PAGED_MAX_REQUESTS && B <= PAGED_MAX_REQUESTS, OSC_ERR_UNSUPPORTED, "%s: %d forks of %d requests (at most %d)", who, N, B, PAGED_MAX_REQUESTS);
+    REQUIRE(n_pages << lg <= 0x7fffffff && n_pages <= 0x7fffffff && n_pool <= 0x7fffffff && ldt <= 0x7fffffff && B * ldt <= 0x7fffffff, OSC_ERR_UNSUPPORTED,
+            "%s: an extent above 2^31-1", who);
+    REQUIRE(n_free && info, OSC_ERR_NULL, "%s: null pointer", who);
+    REQUIRE(N == 0 || (src && dst && src_slots && dst_slots && (B == 0 || kv_lens) && (block_table || B * ldt == 0) && (refs || n_pages == 0) && (free_pages || n_pool == 0)),
+            OSC_ERR_NULL, "%s: null pointer to an array that is not empty", who);
+    const int64_t pairs = (int64_t)N << lg;
+    const Extent4 arrays[] = {{"kv_lens", kv_lens, B}, {"block_table", block_table, B * ldt}, {"refs", refs, n_pages}, {"src_slots", src_slots, pairs}, {"dst_slots", dst_slots, pairs},
+                              {"info", info, 4}, {"src", src, N}, {"dst", dst, N}, {"free_pages", free_pages, n_pool}, {"n_free", n_free, 1}};
+    rc = check_apart(who, arrays, 6, 10);
+    if (rc) return rc;
+    return launch_page_fork(src, dst, N, B, lg, kv_lens, block_table, ldt, refs, n_pages, free_pages, n_pool, n_free, src_slots, dst_slots, info, as_stream(stream));
+}
+
+int osc_page_free(const int32_t* kv_lens, const int32_t* new_lens, int32_t B, int32_t page_size, const int32_t* block_table, int64_t ldt, int32_t* refs, int64_t n_pages,
+                  int32_t* free_pages, int64_t n_pool, const int32_t* n_free, int32_t* info, void* stream) {
+    static const char* who = "osc_page_free";
+    int lg = 0, rc = check_page_size(who, page_size, &lg);
+    if (rc) return rc;
+    REQUIRE(B >= 0 && ldt >= 0 && n_pages >= 0 && n_pool >= 0, OSC_ERR_SHAPE, "%s: B=%d ldt=%lld n_pages=%lld n_pool=%lld", who, B, (long long)ldt, (long long)n_pages,
+            (long long)n_pool);
+    REQUIRE(B <= PAGED_MAX_REQUESTS, OSC_ERR_UNSUPPORTED, "%s: %d requests (at most %d)", who, B, PAGED_MAX_REQUESTS);
+    REQUIRE(n_pages <= 0x7fffffff && n_pool <= 0x7fffffff && ldt <= 0x7fffffff && B * ldt <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "%s: an extent above 2^31-1", who);
+    REQUIRE(n_free && info, OSC_ERR_NULL, "%s: null pointer", who);
+    REQUIRE(B == 0 || (kv_lens && (block_table || ldt == 0) && (free_pages || n_pool == 0)), OSC_ERR_NULL, "%s: null pointer to an array that is not empty", who);
+    const Extent4 arrays[] = {{"refs", refs, n_pages}, {"free_pages", free_pages, n_pool}, {"info", info, 4}, {"kv_lens", kv_lens, B}, {"new_lens", new_lens, B},
+                              {"block_table", block_table, B * ldt}, {"n_free", n_free, 1}};
+    rc = check_apart(who, arrays, 3, 7);
+    if (rc) return rc;
+    return launch_page_free(kv_lens, new_lens, B, lg, block_table, ldt, refs, n_pages, free_pages, n_pool, n_free, info, as_stream(stream));
+}
+
+static bool logprobs_fit(int64_t T, int64_t V, int32_t top_k) {
+    return T >= 0 && V >= 1 && T <= 0x7fffffff && V <= 0x7fffffff && top_k >= 0 && top_k <= LOGPROB_MAX_TOP && top_k <= V;
+}
+
+size_t osc_token_logprobs_workspace_bytes(int64_t T, int64_t V, int32_t top_k) { return logprobs_fit(T, V, top_k) ? token_logprobs_workspace(T, V, top_k) : 0; }
+
+int osc_token_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t ldl, float scale, const int32_t* tokens, int32_t n_tokens, int32_t top_k,
+                       float* logprobs, int32_t* top_ids, float* top_logprobs, float* lse, float* entropy, void* workspace, size_t workspace_bytes, void* stream) {
+    static const char* who = "osc_token_logprobs";
+    REQUIRE(dtype == OSC_DT_F32 || dtype == OSC_DT_BF16, OSC_ERR_UNSUPPORTED, "%s: dtype %d", who, dtype);
+    REQUIRE(T >= 0 && V >= 1 && ldl >= V && n_tokens >= 0 && top_k >= 0 && top_k <= V, OSC_ERR_SHAPE, "%s: T=%lld V=%lld ldl=%lld n_tokens=%d top_k=%d", who, (long long)T,
+            (long long)V, (long long)ldl, n_tokens, top_k);
+    REQUIRE(top_k <= LOGPROB_MAX_TOP, OSC_ERR_UNSUPPORTED, "%s: the top %d (at most %d)", who, top_k, LOGPROB_MAX_TOP);
+    REQUIRE(T <= 0x7fffffff && V <= 0x7fffffff, OSC_ERR_UNSUPPORTED, "%s: T=%lld V=%lld (at most 2^31-1)", who, (long long)T, (long long)V);
+    REQUIRE(scale > 0.0f && scale <= 1e6f, OSC_ERR_SHAPE, "%s: scale %g (a positive number)", who, (double)scale);
+    if (T == 0) return OSC_OK;
+    REQUIRE(logits && (n_tokens == 0 || (tokens && logprobs)) && (top_k == 0 || (top_ids && top_logprobs)), OSC_ERR_NULL, "%s: null pointer", who);
+    REQUIRE(aligned(logits, dtype == OSC_DT_F32 ? 4 : 2), OSC_ERR_UNSUPPORTED, "%s: logits must be aligned to their size", who);
+    const size_t need = token_logprobs_workspace(T, V, top_k);
+    REQUIRE(need == 0 || workspace, OSC_ERR_NULL, "%s: null workspace", who);
+    REQUIRE(need == 0 || aligned(workspace, 256), OSC_ERR_UNSUPPORTED, "%s: workspace must be 256-byte aligned", who);
+    REQUIRE(workspace_bytes >= need, OSC_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
+    return launch_token_logprobs(logits, dtype == OSC_DT_F32, T, V, ldl, scale, tokens, n_tokens, top_k, logprobs, top_ids, top_logprobs, lse, entropy,
+                                 static_cast<uint8_t*>(workspace), as_stream(stream));
 }
 
 }  // extern "C"

@@ -100,6 +100,10 @@ struct AttnArgs {
     int* records;
     uint8_t* blocks;
     int64_t joint_blocks, packed_blocks, narrow_blocks;
+    // trees of new tokens (the kernel's own variant): bits of the new tokens that a row sees, `words` of 64 a row
+    const uint64_t* mask;
+    int64_t ldm;
+    int words;
 };
 template <int D>
 constexpr int block_bytes() { return 32 * (D + 2) * 4; }  // [32][D] sums, [32] base and weight
@@ -406,6 +410,30 @@ __device__ __forceinline__ void mask(v16f (&s)[N], int lane, int seen) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[u][e] = 32 * u + (e & 3) + 8 * (e >> 2) < left ? s[u][e] : -INFINITY;
 }
+// Rows of a tree.  The tokens from j0 on that a row sees, as bits: all before the request's new ones, which start at `fresh`, then those
+// of the row's words, none from `seen` on.
+template <int N>
+__device__ __forceinline__ uint64_t tree_bits(const AttnArgs& p, const uint64_t* words, int fresh, int seen, int j0) {
+    const int skip = j0 - fresh;
+    uint64_t w;
+    if (skip < 0) {
+        w = skip <= -64 ? ~0ull : words[0] << -skip | ((1ull << -skip) - 1);
+    } else {
+        const int at = skip >> 6, shift = skip & 63;
+        w = at < p.words ? words[at] >> shift : 0;
+        if (shift > 64 - 32 * N && at + 1 < p.words) w |= words[at + 1] << (64 - shift);
+    }
+    const int left = seen - j0;
+    return left >= 64 ? w : left <= 0 ? 0 : w & ((1ull << left) - 1);
+}
+template <int N>
+__device__ __forceinline__ void mask_tree(v16f (&s)[N], int lane, uint64_t bits) {
+    bits >>= 4 * (lane >> 5);
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[u][e] = (uint32_t)(bits >> 32 * u) >> ((e & 3) + 8 * (e >> 2)) & 1 ? s[u][e] : -INFINITY;
+}
 template <int D, int N>
 __device__ __forceinline__ void weigh(State<D>& st, v16f (&s)[N], float c) {
     float top = s[0][0];
@@ -564,7 +592,7 @@ __device__ __forceinline__ void merge(const AttnArgs& p, const State<D>& st, uin
 // A wavefront's tiles of 32 tokens are in LDS that no other wavefront uses.  Keys of the next tile are asked for once this tile's
 // scores are there, values once they are summed, so half a tile or more is on its way at any time, and no wavefront
 // waits for another before a team's sums are merged.
-template <int D>
+template <int D, bool TREE>
 __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, float* stats) {
     constexpr int TILE = 32 * D * 2, NI = D / 16;
     int tid = threadIdx.x;
@@ -595,6 +623,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             h = k / nt;
             r0 = (k - h * nt) * 32, rows = rq.n * p.G;
             tokens = max(0, rq.L - rq.n + min(r0 + 31, rows - 1) / p.G + 1), clear_to = rq.L - rq.n + r0 / p.G + 1;
+            if (TREE && rq.n <= 64 * p.words) clear_to = rq.L - rq.n;
             n_prefix = p.pre_tiles;
         }
         const int stop = min(end, start + length);
@@ -650,7 +679,10 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             if (more) fetch(tile + step, na, nb, 0, kt);
             const bool pre = tile < n_prefix;
             const int j0 = (pre ? tile : tile - n_prefix) * 32;
-            if (j0 + 32 > (pre ? p.P : clear_to)) mask<1>(s, lane, (pre ? p.P : seen) - j0);
+            if (j0 + 32 > (pre ? p.P : clear_to)) {
+                if (TREE && !pre && rq.n <= 64 * p.words) mask_tree<1>(s, lane, tree_bits<1>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j0));
+                else mask<1>(s, lane, (pre ? p.P : seen) - j0);
+            }
             weigh<D, 1>(st, s, p.c);
             if (more) wait_vmcnt<NI>();
             else wait_vmcnt<0>();
@@ -677,7 +709,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
 
 // ---- a piece of the line of 128-row tiles -----------------------------------------------------------------------------------------
 // Every wavefront has 32 rows; all read the same 64 tokens from LDS, of which each has asked for 16, a block ahead.
-template <int D>
+template <int D, bool TREE>
 __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, int w) {
     constexpr int TILE = 64 * D * 2;
     int tid = threadIdx.x;
@@ -744,7 +776,8 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             seen = rq.L - rq.n + t_base + ti + 1;
             ti += rq.q0 + t_base;
         }
-        const int clear_to = rq.L - rq.n + t_base + (wave * 32) / p.G + 1;  // own tokens that all of the wavefront's rows see
+        const bool tree = TREE && b >= 0 && rq.n <= 64 * p.words;
+        const int clear_to = rq.L - rq.n + (tree ? 0 : t_base + (wave * 32) / p.G + 1);  // own tokens that all of the wavefront's rows see
         v8bf q[D / 16];
         const uint16_t* qp = p.Q + (int64_t)ti * p.ldq + (h * p.G + g) * D + (lane >> 5) * 8;
 #pragma unroll
@@ -801,7 +834,10 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
                 scores<D, 2>(s, q, buffer + kl);
                 Values<D> f;  // on their way while the weights are made
                 read_values<D>(f, buffer + TILE + vl, 0);
-                if (j0 + 64 > (pre ? p.P : clear_to)) mask<2>(s, lane, (pre ? p.P : seen) - j0);
+                if (j0 + 64 > (pre ? p.P : clear_to)) {
+                    if (tree && !pre) mask_tree<2>(s, lane, tree_bits<2>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j0));
+                    else mask<2>(s, lane, (pre ? p.P : seen) - j0);
+                }
                 weigh<D, 2>(st, s, p.c);
                 gather<D, 2>(st, s, f, buffer + TILE + vl);
             }
@@ -836,7 +872,7 @@ __device__ __forceinline__ int wave_scan(int v, Op op) {
     return v;
 }
 
-template <int D>
+template <int D, bool TREE>
 __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(const AttnArgs p) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     AttnShared& sh = *reinterpret_cast<AttnShared*>(lds + 8 * 32 * D * 2);  // behind the tiles, which start at 0
@@ -914,9 +950,9 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
         if ((turn == 0) == swap) {
-            narrow_piece<D>(p, plan, sums, lds, sh.stats);
+            narrow_piece<D, TREE>(p, plan, sums, lds, sh.stats);
             if (turn == 0 && with_wide) lds_barrier();  // the tiles of both are in the same place
-        } else if (with_wide) wide_piece<D>(p, plan, sums, lds, xcd * run + i);
+        } else if (with_wide) wide_piece<D, TREE>(p, plan, sums, lds, xcd * run + i);
     }
 }
 
@@ -1098,19 +1134,19 @@ size_t prefix_attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv,
     return attn_space(T, B, Hq, Hkv, D, prefix_len).total;
 }
 
-template <int D>
+template <int D, bool TREE>
 static int launch(const AttnArgs& p, hipStream_t st) {
     static LdsReserved r;
     constexpr size_t lds = 8 * 32 * D * 2 + sizeof(AttnShared);
-    const int rc = reserve_lds((const void*)prefix_attention_kernel<D>, lds, r);
+    const int rc = reserve_lds((const void*)prefix_attention_kernel<D, TREE>, lds, r);
     if (rc) return rc;
-    prefix_attention_kernel<D><<<dim3(attn_wgs<D>()), WG, lds, st>>>(p);
+    prefix_attention_kernel<D, TREE><<<dim3(attn_wgs<D>()), WG, lds, st>>>(p);
     // a wavefront a row while the card holds them at once, four rows beyond that
     const bool few = p.T * p.Hq <= 4096;
     const int64_t wgs = (p.T * (few ? p.Hq : (p.Hq + 3) / 4) + 3) / 4;
     if (few) prefix_attention_join_kernel<D, 1><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
     else prefix_attention_join_kernel<D, 4><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
-    return check_launch("osc_prefix_attention");
+    return check_launch(TREE ? "osc_tree_attention" : "osc_prefix_attention");
 }
 
 int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
@@ -1134,7 +1170,9 @@ int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
     const int64_t narrow = (int64_t)p.Hkv * (rows / 32 + some + 1) * (std::max<int64_t>(p.P, p.max_kv) / 32 + p.pre_tiles + CUT_EDGE + PIECE3 + 1);
     for (p.ws = 0; wide >> p.ws > 1 << 30;) ++p.ws;
     for (p.ns = 0; narrow >> p.ns > 1 << 30;) ++p.ns;
-    return a.D == 64 ? launch<64>(p, st) : launch<128>(p, st);
+    p.mask = a.mask, p.ldm = a.ldm, p.words = a.words;
+    if (p.mask) return a.D == 64 ? launch<64, true>(p, st) : launch<128, true>(p, st);
+    return a.D == 64 ? launch<64, false>(p, st) : launch<128, false>(p, st);
 }
 
 }  // namespace osc

@@ -398,6 +398,12 @@ const at::Tensor& rows_bf16(PyObject* o) {
 void on_gpu(const at::Tensor& t) {
     if (!t.is_cuda()) reject("need tensors on the GPU");
 }
+// and the current one's, whose stream the call is on
+void on_this_gpu(const at::Tensor& t) {
+    on_gpu(t);
+    device_ready();
+    if (t.device().index() != c10::hip::getCurrentHIPStream().device_index()) reject("the tensors are on another GPU than the current one");
+}
 int64_t rows_pitch(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
 // rows of bf16, at least `width` columns, on `like`'s device
 const at::Tensor& rows_bf16_of(PyObject* o, int64_t n, int64_t width, const at::Tensor& like, const char* what) {
@@ -513,8 +519,9 @@ PyObject* qk_norm_rope(PyObject* const* a) {
     return y.give();
 }
 
-// Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets, scale, want_lse, workspace, out
-PyObject* prefix_attention(PyObject* const* a) {
+// Q, Hq, Hkv, D, Kc, Vc, prefix_pages, prefix_len, block_table, kv_lens, q_offsets, scale, want_lse, workspace, out; for trees also mask
+template <bool TREE>
+PyObject* attention(PyObject* const* a) {
     const at::Tensor& Q = rows_bf16(a[0]);
     const int64_t T = Q.size(0), Hq = num(a[1]), Hkv = num(a[2]), D = num(a[3]), P = num(a[7]);
     if (Hq <= 0 || Hkv <= 0 || D <= 0 || Hq > 65536 || Hkv > 65536 || D > 65536 || Q.size(1) < Hq * D) reject("Q: bf16 [T, Hq D]");
@@ -527,6 +534,15 @@ PyObject* prefix_attention(PyObject* const* a) {
     if (B > 0x7fffffff) reject("too many requests");
     const int32_t *kl = ints(a[9], B, Q, "kv_lens: int32 [B]"), *qo = ints(a[10], B + 1, Q, "q_offsets: int32 [B + 1]");
     const float scale = none(a[11]) ? 1.0f / sqrtf((float)D) : real(a[11]);
+    const uint64_t* mask = nullptr;
+    int64_t words = 0, ldm = 0;
+    if (TREE) {
+        const at::Tensor& m = tensor(a[15]);
+        if (!(m.dim() == 2 && (m.scalar_type() == at::kLong || m.scalar_type() == at::kUInt64) && m.size(0) >= T && (m.stride(1) == 1 || m.size(1) <= 1) &&
+              m.size(1) <= 0x7fffffff && m.device() == Q.device()))
+            reject("mask: int64 [T, words]");
+        mask = (const uint64_t*)m.data_ptr(), words = m.size(1), ldm = rows_pitch(m);
+    }
     Ref o, lse, ws;
     const Outs outs(a[14], 2);
     if (outs) {
@@ -543,7 +559,8 @@ PyObject* prefix_attention(PyObject* const* a) {
         if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() < T * Hq || t.device() != Q.device()) reject("lse: float32 [T, Hq]");
     }
     if (none(a[13])) {
-        const int64_t n = (int64_t)osc_prefix_attention_workspace_bytes(T, (int32_t)B, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, P);
+        const auto bytes = TREE ? osc_tree_attention_workspace_bytes : osc_prefix_attention_workspace_bytes;
+        const int64_t n = (int64_t)bytes(T, (int32_t)B, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, P);
         ws.own(fresh(Q, {n}, at::kByte));
     } else ws.share(a[13]);
     const at::Tensor& W = tensor(ws.o);
@@ -551,12 +568,241 @@ PyObject* prefix_attention(PyObject* const* a) {
     void *q = Q.data_ptr(), *po = O.data_ptr(), *pl = ptr(lse.o), *pw = W.data_ptr();
     const int64_t ldq = rows_pitch(Q), ldo = rows_pitch(O), ldt = table.size(1);
     const int32_t* pt = table.data_ptr<int32_t>();
-    on_gpu(Q);
+    if (TREE) on_this_gpu(Q);
+    else on_gpu(Q);
     enqueue([&](void* st) {
+        if (TREE)
+            return osc_tree_attention(q, T, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, ldq, K.data, V.data, K.pages, K.page_size, pp, P, pt, ldt, kl, qo, (int32_t)B,
+                                      mask, (int32_t)words, ldm, scale, po, ldo, (float*)pl, pw, W.nbytes(), st);
         return osc_prefix_attention(q, T, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, ldq, K.data, V.data, K.pages, K.page_size, pp, P, pt, ldt, kl, qo,
                                     (int32_t)B, scale, po, ldo, (float*)pl, pw, W.nbytes(), st);
     });
     return tuple({&o, &lse});
+}
+
+// `count` int32 tensors in one allocation: each on its own took longer than a small kernel
+void fresh_ints(const at::Tensor& like, Ref** refs, const int64_t* sizes, int count) {
+    Ref all;
+    int64_t at = 0;
+    for (int i = 0; i < count; ++i) at += (sizes[i] + 15) / 16 * 16;
+    all.own(fresh(like, {at}, at::kInt));
+    const at::Tensor& whole = tensor(all.o);
+    at = 0;
+    for (int i = 0; i < count; ++i) {
+        at::Tensor part = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+        part.unsafeGetTensorImpl()->set_storage_offset(at);
+        part.unsafeGetTensorImpl()->set_sizes_contiguous({sizes[i]});
+        refs[i]->own(THPVariable_Wrap(part));
+        if (!refs[i]->o) throw PyFailed();
+        at += (sizes[i] + 15) / 16 * 16;
+    }
+}
+// int32 [rows, cols], contiguous
+void table_of(const at::Tensor& t, const at::Tensor& like, int64_t rows, const char* what) {
+    if (!(t.dim() == 2 && t.scalar_type() == at::kInt && t.size(0) == rows && t.is_contiguous() && t.device() == like.device())) reject(what);
+}
+int32_t few(int64_t n) {
+    if (n > 0x7fffffff) reject("too many requests");
+    return (int32_t)n;
+}
+
+// parents, q_offsets, kv_lens, words, pos_base, out
+PyObject* tree_mask(PyObject* const* a) {
+    const at::Tensor &par = tensor(a[0]), &kv = tensor(a[2]);
+    const int64_t T = par.numel(), B = kv.numel();
+    const int32_t words = num32(a[3]), base = num32(a[4]);
+    const int32_t *pp = ints(a[0], T, par, "parents: int32 [T]"), *po = ints(a[1], B + 1, par, "q_offsets: int32 [B + 1]"), *pk = ints(a[2], B, par, "kv_lens: int32 [B]");
+    if (words < 1 || words > 64) reject("words: 1 to 8");
+    Ref mask, pos;
+    const Outs outs(a[5], 2);
+    if (outs) {
+        mask.share(outs.item[0]);
+        pos.share(outs.item[1]);
+    } else {
+        mask.own(fresh(par, {T, words}, at::kLong));
+        pos.own(fresh(par, {T}, at::kInt));
+    }
+    const at::Tensor& m = tensor(mask.o);
+    if (!(m.dim() == 2 && (m.scalar_type() == at::kLong || m.scalar_type() == at::kUInt64) && m.size(0) >= T && m.size(1) == words && (m.stride(1) == 1 || words == 1) &&
+          m.device() == par.device()))
+        reject("mask: int64 [T, words]");
+    int32_t* ps = ints(pos.o, T, par, "positions: int32 [T]");
+    const int64_t ldm = rows_pitch(m);
+    const int32_t b = few(B);
+    on_this_gpu(par);
+    enqueue([&](void* st) { return osc_tree_mask(pp, po, pk, b, T, base, words, (uint64_t*)m.data_ptr(), ldm, ps, st); });
+    return tuple({&mask, &pos});
+}
+
+// parents, tokens, choices, q_offsets, kv_lens, slots, out
+PyObject* tree_accept(PyObject* const* a) {
+    const at::Tensor &par = tensor(a[0]), &kv = tensor(a[4]), &ch = tensor(a[2]);
+    const int64_t T = par.numel(), B = kv.numel();
+    const int32_t *pp = ints(a[0], T, par, "parents: int32 [T]"), *pt = ints(a[1], T, par, "tokens: int32 [T]"), *po = ints(a[3], B + 1, par, "q_offsets: int32 [B + 1]"),
+                  *pk = ints(a[4], B, par, "kv_lens: int32 [B]"), *psl = ints(a[5], T, par, "slots: int32 [T]");
+    if (!(ch.dim() == 1 && ch.scalar_type() == at::kInt && ch.size(0) >= T && ch.device() == par.device())) reject("choices: int32 [T]");
+    const int64_t ldc = ch.size(0) > 1 ? ch.stride(0) : 1;
+    Ref path, count, next, lens, src;
+    Ref* r[5] = {&path, &count, &next, &lens, &src};
+    const Outs outs(a[6], 5);
+    if (outs)
+        for (int i = 0; i < 5; ++i) r[i]->share(outs.item[i]);
+    else {
+        const int64_t sizes[5] = {T, B, B, B, T};
+        fresh_ints(par, r, sizes, 5);
+    }
+    int32_t *o0 = ints(path.o, T, par, "path: int32 [T]"), *o1 = ints(count.o, B, par, "n_accepted: int32 [B]"), *o2 = ints(next.o, B, par, "next_tokens: int32 [B]"),
+            *o3 = ints(lens.o, B, par, "kv_lens after: int32 [B]"), *o4 = ints(src.o, T, par, "src_slots: int32 [T]");
+    const int32_t b = few(B), *pc = ch.data_ptr<int32_t>();
+    on_this_gpu(par);
+    enqueue([&](void* st) { return osc_tree_accept(pp, pt, pc, ldc, po, pk, psl, b, T, o0, o1, o2, o3, o4, st); });
+    return tuple({&path, &count, &next, &lens, &src});
+}
+
+// Kc, Vc, src_slots, dst_slots, offsets
+PyObject* cache_move(PyObject* const* a) {
+    const at::Tensor &K = tensor(a[0]), &V = tensor(a[1]), &src = tensor(a[2]), &dst = tensor(a[3]);
+    const int64_t d = K.dim();
+    const auto whole = [&](const at::Tensor& t) {  // layers may lie apart, each is contiguous
+        if (!(d == 4 || d == 5) || t.dim() != d || !is_bf16(t) || t.sizes() != K.sizes() || t.device() != K.device()) return false;
+        int64_t n = 1;
+        for (int64_t i = d - 1; i >= d - 4; n *= t.size(i--))
+            if (t.size(i) > 1 && t.stride(i) != n) return false;
+        return t.size(d - 2) > 0 && t.size(d - 4 + 1) > 0 && t.size(d - 2) <= 0x7fffffff && t.size(d - 3) <= 0x7fffffff && t.size(d - 1) <= 0x7fffffff;
+    };
+    if (!whole(K) || !whole(V)) reject("need bf16 caches [pages, Hkv, page_size, D] or [layers, pages, Hkv, page_size, D]");
+    const int64_t layers = d == 5 ? K.size(0) : 1, stride = layers > 1 ? K.stride(0) : 0;
+    if (layers > 1 && V.stride(0) != stride) reject("the two caches differ in their layers' stride");
+    const int64_t T = src.numel();
+    const int32_t *ps = ints(a[2], T, K, "src_slots: int32 [T] or [groups, pairs]"), *pd = ints(a[3], T, K, "dst_slots: int32, as src_slots");
+    if (dst.numel() != T && none(a[4])) reject("dst_slots: int32, as src_slots");
+    int64_t N;
+    const int32_t* po = nullptr;
+    if (none(a[4])) N = src.dim() == 2 ? src.size(0) : T > 0;
+    else {
+        N = tensor(a[4]).numel() - 1;
+        if (N < 0) reject("offsets: int32 [groups + 1]");
+        po = ints(a[4], N + 1, K, "offsets: int32 [groups + 1]");
+    }
+    const int32_t n = few(N), nl = few(layers);
+    on_this_gpu(K);
+    void *pk = K.data_ptr(), *pv = V.data_ptr();
+    enqueue([&](void* st) {
+        return osc_cache_move(pk, pv, nl, stride, K.size(d - 4), (int32_t)K.size(d - 3), (int32_t)K.size(d - 2), (int32_t)K.size(d - 1), ps, pd, po, n, T, st);
+    });
+    Py_RETURN_NONE;
+}
+
+// src, dst, kv_lens, block_table, refs, free_pages, n_free, page_size, out
+PyObject* page_fork(PyObject* const* a) {
+    const at::Tensor &src = tensor(a[0]), &kv = tensor(a[2]), &table = tensor(a[3]), &refs = tensor(a[4]), &fp = tensor(a[5]);
+    const int64_t N = src.numel(), B = kv.numel();
+    const int32_t ps = num32(a[7]);
+    if (ps < 1 || ps > 65536) reject("page_size: 16, 32, 64, 128 or 256");
+    const int32_t *s = ints(a[0], N, kv, "src: int32 [N]"), *d = ints(a[1], N, kv, "dst: int32 [N]"), *pn = ints(a[6], 1, kv, "n_free: int32 [1]");
+    int32_t *pk = ints(a[2], B, kv, "kv_lens: int32 [B]"), *pr = ints(a[4], 0, kv, "refs: int32 [pages]");
+    const int32_t* pf = ints(a[5], 0, kv, "free_pages: int32 [pool]");
+    table_of(table, kv, B, "block_table: contiguous int32 [B, pages]");
+    Ref from, to, info;
+    const Outs outs(a[8], 3);
+    if (outs) {
+        from.share(outs.item[0]);
+        to.share(outs.item[1]);
+        info.share(outs.item[2]);
+    } else {
+        Ref* r[3] = {&from, &to, &info};
+        const int64_t sizes[3] = {N * ps, N * ps, 4};
+        fresh_ints(kv, r, sizes, 3);
+        for (int i = 0; i < 2; ++i) tensor(r[i]->o).unsafeGetTensorImpl()->set_sizes_contiguous({N, ps});
+    }
+    int32_t *o0 = ints(from.o, N * ps, kv, "src_slots: int32 [N, page_size]"), *o1 = ints(to.o, N * ps, kv, "dst_slots: int32 [N, page_size]"),
+            *o2 = ints(info.o, 4, kv, "info: int32 [4]");
+    const int32_t n = few(N), b = few(B);
+    const int64_t width = table.size(1), pages = refs.numel(), pool = fp.numel();
+    int32_t* pt = table.data_ptr<int32_t>();
+    on_this_gpu(kv);
+    enqueue([&](void* st) { return osc_page_fork(s, d, n, b, ps, pk, pt, width, pr, pages, pf, pool, pn, o0, o1, o2, st); });
+    return tuple({&from, &to, &info});
+}
+
+// kv_lens, new_lens, block_table, free_pages, n_free, page_size, refs, n_pages, out
+PyObject* page_free(PyObject* const* a) {
+    const at::Tensor &kv = tensor(a[0]), &table = tensor(a[2]), &fp = tensor(a[3]);
+    const int64_t B = kv.numel();
+    const int32_t ps = num32(a[5]);
+    const int32_t *pk = ints(a[0], B, kv, "kv_lens: int32 [B]"), *pnew = ints(a[1], B, kv, "new_lens: int32 [B]"), *pn = ints(a[4], 1, kv, "n_free: int32 [1]");
+    int32_t *pf = ints(a[3], 0, kv, "free_pages: int32 [pool]"), *pr = ints(a[6], 0, kv, "refs: int32 [pages]");
+    table_of(table, kv, B, "block_table: contiguous int32 [B, pages]");
+    const int64_t held = none(a[6]) ? -1 : tensor(a[6]).numel(), pages = none(a[7]) ? held < 0 ? fp.numel() : held : num(a[7]);
+    if (held >= 0 && pages > held) reject("refs: int32 [pages]");
+    Ref info;
+    if (none(a[8])) info.own(fresh(kv, {4}, at::kInt));
+    else info.share(a[8]);
+    int32_t* o = ints(info.o, 4, kv, "info: int32 [4]");
+    const int32_t b = few(B);
+    const int64_t width = table.size(1), pool = fp.numel();
+    const int32_t* pt = table.data_ptr<int32_t>();
+    on_this_gpu(kv);
+    enqueue([&](void* st) { return osc_page_free(pk, pnew, b, ps, pt, width, pr, pages, pf, pool, pn, o, st); });
+    return info.give();
+}
+
+// logits, tokens, top_k, scale, workspace, out
+PyObject* token_logprobs(PyObject* const* a) {
+    const at::Tensor& X = tensor(a[0]);
+    const bool f32 = X.scalar_type() == at::kFloat;
+    if (!(X.dim() == 2 && (f32 || is_bf16(X)) && (X.stride(1) == 1 || X.size(1) == 1))) reject("logits: float32 or bf16 [T, V]");
+    const int64_t T = X.size(0), V = X.size(1);
+    const int32_t k = num32(a[2]);
+    const float scale = real(a[3]);
+    if (k < 0 || k > 65536) reject("top_k: 0 to 64");
+    int64_t n = 0;
+    const int32_t* pt = nullptr;
+    Ref lp, ids, top, lse, ent, ws;
+    if (!none(a[1])) {
+        const at::Tensor& t = tensor(a[1]);
+        if (!(t.dim() >= 1 && t.dim() <= 2 && t.size(0) == T)) reject("tokens: int32 [T] or [T, n]");
+        n = t.dim() == 2 ? t.size(1) : 1;
+        pt = ints(a[1], T * n, X, "tokens: int32 [T] or [T, n]");
+    }
+    const Outs outs(a[5], 5);
+    if (outs) {
+        Ref* r[5] = {&lp, &ids, &top, &lse, &ent};
+        for (int i = 0; i < 5; ++i) r[i]->share(outs.item[i]);
+    } else {
+        if (!none(a[1])) lp.own(fresh(X, tensor(a[1]).sizes(), at::kFloat));
+        else lp.share(Py_None);
+        if (k) {
+            ids.own(fresh(X, {T, k}, at::kInt));
+            top.own(fresh(X, {T, k}, at::kFloat));
+        } else {
+            ids.share(Py_None);
+            top.share(Py_None);
+        }
+        lse.own(fresh(X, {T}, at::kFloat));
+        ent.own(fresh(X, {T}, at::kFloat));
+    }
+    const auto floats = [&](PyObject* o, int64_t count, const char* what) -> float* {
+        if (none(o)) return nullptr;
+        const at::Tensor& t = tensor(o);
+        if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() < count || t.device() != X.device()) reject(what);
+        return t.data_ptr<float>();
+    };
+    float *plp = floats(lp.o, T * n, "logprobs: float32, as tokens"), *ptop = floats(top.o, T * k, "top_logprobs: float32 [T, top_k]"),
+          *pl = floats(lse.o, T, "lse: float32 [T]"), *pe = floats(ent.o, T, "entropy: float32 [T]");
+    int32_t* pi = ints(ids.o, T * k, X, "top_ids: int32 [T, top_k]");
+    if (none(a[4])) ws.own(fresh(X, {(int64_t)osc_token_logprobs_workspace_bytes(T, V, k)}, at::kByte));
+    else ws.share(a[4]);
+    const at::Tensor& W = tensor(ws.o);
+    if (!W.is_contiguous() || W.device() != X.device()) reject("workspace: a contiguous device tensor");
+    void *x = X.data_ptr(), *pw = W.data_ptr();
+    const int64_t ldl = rows_pitch(X);
+    const int32_t nt = few(n);
+    on_this_gpu(X);
+    enqueue([&](void* st) {
+        return osc_token_logprobs(x, f32 ? OSC_DT_F32 : OSC_DT_BF16, T, V, ldl, scale, pt, nt, k, plp, pi, ptop, pl, pe, pw, W.nbytes(), st);
+    });
+    return tuple({&lp, &ids, &top, &lse, &ent});
 }
 
 PyObject* current_stream(PyObject* const*) { return PyLong_FromVoidPtr(stream()); }
@@ -588,7 +834,14 @@ PyMethodDef methods[] = {
     OSC_NATIVE("quantize_act_dynamic", quantize_act_dynamic, 4),
     OSC_NATIVE("page_slots", page_slots, 9),
     OSC_NATIVE("qk_norm_rope", qk_norm_rope, 16),
-    OSC_NATIVE("prefix_attention", prefix_attention, 15),
+    OSC_NATIVE("prefix_attention", attention<false>, 15),
+    OSC_NATIVE("tree_mask", tree_mask, 6),
+    OSC_NATIVE("tree_attention", attention<true>, 16),
+    OSC_NATIVE("tree_accept", tree_accept, 7),
+    OSC_NATIVE("cache_move", cache_move, 5),
+    OSC_NATIVE("page_fork", page_fork, 9),
+    OSC_NATIVE("page_free", page_free, 9),
+    OSC_NATIVE("token_logprobs", token_logprobs, 6),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling of the per-step calls", -1, methods,

@@ -150,12 +150,32 @@ struct AttnCall {
     int64_t ldo;
     float* lse;  // or null
     uint8_t* workspace;
+    const uint64_t* mask;  // trees of new tokens, or null
+    int64_t ldm;
+    int32_t words;
 };
 constexpr int32_t PAGED_MAX_REQUESTS = 8192;  // both kernels hold the requests' running sums in LDS
 // A tile's length on the line is made of a prefix and up to ATTN_MAX_TOKENS tokens of a request's own and of up to 255 more, in 31 bits.
 constexpr int64_t ATTN_MAX_TOKENS = 0x3fffffff, ATTN_MAX_PREFIX = 0x7fffffff - ATTN_MAX_TOKENS - 256;
 size_t prefix_attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len);
 int launch_prefix_attention(const AttnCall& a, hipStream_t st);
+
+// trees of drafted tokens (tree.hip), pages and cached tokens in other hands (pages.hip), log probabilities (logprob.hip)
+constexpr int32_t TREE_MAX_WORDS = 8;
+int launch_tree_mask(const int32_t* parents, const int32_t* q_offsets, const int32_t* kv_lens, int32_t B, int64_t T, int32_t pos_base, int32_t words, uint64_t* mask,
+                     int64_t ldm, int32_t* positions, hipStream_t st);
+int launch_tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* choices, int64_t ldc, const int32_t* q_offsets, const int32_t* kv_lens, const int32_t* slots,
+                       int32_t B, int64_t T, int32_t* path, int32_t* n_accepted, int32_t* next_tokens, int32_t* kv_lens_out, int32_t* src_slots, hipStream_t st);
+int launch_cache_move(void* K, void* V, int32_t n_layers, int64_t layer_stride, int64_t n_pages, int32_t Hkv, int lg, int32_t D, const int32_t* src, const int32_t* dst,
+                      const int32_t* offsets, int32_t N, int64_t T, hipStream_t st);
+int launch_page_fork(const int32_t* src, const int32_t* dst, int32_t N, int32_t B, int lg, int32_t* kv_lens, int32_t* table, int64_t ldt, int32_t* refs, int64_t n_pages,
+                     const int32_t* free_pages, int64_t n_pool, const int32_t* n_free, int32_t* src_slots, int32_t* dst_slots, int32_t* info, hipStream_t st);
+int launch_page_free(const int32_t* kv_lens, const int32_t* new_lens, int32_t B, int lg, const int32_t* table, int64_t ldt, int32_t* refs, int64_t n_pages, int32_t* free_pages,
+                     int64_t n_pool, const int32_t* n_free, int32_t* info, hipStream_t st);
+constexpr int32_t LOGPROB_MAX_TOP = 64;  // a lane each
+size_t token_logprobs_workspace(int64_t T, int64_t V, int32_t k);
+int launch_token_logprobs(const void* X, bool f32, int64_t T, int64_t V, int64_t ldl, float scale, const int32_t* tokens, int32_t n_tok, int32_t k, float* lp, int32_t* ids,
+                          float* top, float* lse, float* entropy, uint8_t* workspace, hipStream_t st);
 
 struct GemmProblem {
     // activations
