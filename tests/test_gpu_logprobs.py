@@ -214,3 +214,19 @@ def test_logits_past_32_bits(osc):
     want = np.log(V - 1 + np.exp(20.0))
     # sums of 2^20 terms a lane at most, in single precision
     assert abs(lse[19].item() - want) < 1e-3 and abs(lse[0].item() - np.log(V)) < V / 4096 * u + 1e-5
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [300, 700, 1100])
+def test_many_long_rows(osc, T, dtype):
+    """a workgroup a row, more chunks than a lane has marks: the same as of a few rows, which are checked above"""
+    V = 280001 if T == 1100 else 66000
+    x = logits(T, 8, V, dtype).repeat(-(-T // 8), 1)[:T]
+    tok = i32(np.arange(T) % 8 * 1000)
+    few, got = osc.osc_token_logprobs(x[:8].contiguous(), tok[:8], 20), osc.osc_token_logprobs(x, tok, 20)
+    assert torch.equal(got[1], few[1].repeat(-(-T // 8), 1)[:T])
+    for a, b in zip(got, few):
+        if a.dtype == torch.float32:
+            b = b.repeat(-(-T // 8), *[1] * (b.dim() - 1))[:T].double()
+            assert ((a.double() - b).abs() <= 2 * (V / 4096 + 250) * u + 16 * u * b.abs()).all()
+    check(osc, x[3:5], tok[3:5].cpu().numpy(), 20)
