@@ -770,11 +770,15 @@ int osc_qk_norm_rope(const void* QKV, int64_t T, int32_t Hq, int32_t Hkv, int32_
                                n_axes, sections, slots, Qn, ldq, Kc, Vc, n_pages, lg, as_stream(stream));
 }
 
-size_t osc_prefix_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
-    // as osc_prefix_attention: no size for what it refuses
+static size_t attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len, bool tree) {
+    // as the calls: no size for what they refuse
     if (T < 0 || B < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || prefix_len < 0 || Hq / Hkv > 128) return 0;
     if (Hq > 65536 / D || T > 0x7fffffff / Hq || B > PAGED_MAX_REQUESTS || prefix_len > ATTN_MAX_PREFIX) return 0;
-    return prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len);
+    return prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len, tree);
+}
+
+size_t osc_prefix_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
+    return attention_workspace(T, B, Hq, Hkv, D, prefix_len, false);
 }
 
 // osc_prefix_attention, and osc_tree_attention where there is a mask
@@ -811,7 +815,7 @@ static int attention(const char* who, const void* Q, int64_t T, int32_t Hq, int3
     REQUIRE((Kc && Vc && n_pages > 0) || (prefix_len == 0 && ldt == 0), OSC_ERR_NULL, "%s: no cache", who);
     REQUIRE(aligned(Q, 16) && ldq % 8 == 0 && aligned(O, 16) && ldo % 8 == 0, OSC_ERR_UNSUPPORTED, "%s: rows must be 16-byte aligned", who);
     REQUIRE(aligned(workspace, 256), OSC_ERR_UNSUPPORTED, "%s: workspace must be 256-byte aligned", who);
-    const size_t need = prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len);
+    const size_t need = prefix_attention_workspace(T, B, Hq, Hkv, D, prefix_len, tree != nullptr);
     REQUIRE(workspace_bytes >= need, OSC_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
     AttnCall a;
     a.Q = Q, a.T = T, a.Hq = Hq, a.Hkv = Hkv, a.D = D, a.ldq = ldq, a.K = Kc, a.V = Vc, a.n_pages = n_pages, a.lg = lg;
@@ -830,7 +834,7 @@ int osc_prefix_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int3
 }
 
 size_t osc_tree_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
-    return osc_prefix_attention_workspace_bytes(T, B, Hq, Hkv, D, prefix_len);
+    return attention_workspace(T, B, Hq, Hkv, D, prefix_len, true);
 }
 
 int osc_tree_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void* Kc, const void* Vc, int64_t n_pages,

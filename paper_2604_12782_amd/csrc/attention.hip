@@ -73,6 +73,14 @@ constexpr int SUPER = 4096, MAX_SUPER = 16;
 // Rows of a long request, with a prefix and without (with 128, 256, 512, 24 prompts behind 4000 tokens: of 40 tokens 123, 98, 104 (80, 65, 71), of 80 180, 179,
 // 174 (114, 112, 113), of 120 244, 244, 274 (131, 130, 158)).
 constexpr int LONG_PREFIX = 256, LONG = 33;
+// Trees behind a prefix are long from LONG_TREE rows on, and from LONG on where those between have LONG_OWN times as many tokens of their own as the
+// prefix has, all together (some requests long and others like them not is worse than either).  With LONG_TREE / LONG_PREFIX: 16 trees of up to 60 tokens (4 heads
+// a key/value head) behind 1000 with up to 1500 of their own 73 / 125, 8 of 32 behind 500 with up to 8000 65 / 123, 48 of 32 (8 heads) behind 4096 with
+// up to 700 146 / 157.  With LONG / LONG_TREE for all between, the rule takes the first: 8 trees of up to 16 behind 500 with up to 8000 of their own 55 / 80, behind
+// 3000 64 / 81, 32 behind 1000 with up to 300 46 / 56, with up to 1000 56 / 68, 8 behind 3000 with up to 3000 51 / 48;  the second: 64 of up to 12 behind 6000 with up to
+// 1000 199 / 149, 128 of up to 12 behind 2000 with up to 300 151 / 121.
+constexpr int LONG_TREE = 65;
+constexpr float LONG_OWN = 1.0f / 6;
 
 struct AttnArgs {
     const uint16_t* Q;
@@ -89,6 +97,7 @@ struct AttnArgs {
     const int32_t *kv_lens, *q_offsets;
     int B, per;  // per: requests of a group
     int pre_tiles;  // tiles of the prefix that short requests' items start with, or 0: their rows are packed
+    int long_rows;  // trees behind a prefix: rows of a long request
     int ns, ws;  // a step on the line of 32-row (128-row) tiles is 2^ns (2^ws) of its units: 0 unless the lines could pass 2^30
     float c;     // scale * log2(e): scores leave the matrix core unscaled, and powers are of two
     uint16_t* O;
@@ -124,7 +133,8 @@ __device__ __forceinline__ Request request(const AttnArgs& p, int b) {
     r.L = min(max(p.kv_lens[b], 0), p.max_kv);
     return r;
 }
-__device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? LONG_PREFIX : LONG); }
+template <bool TREE>
+__device__ __forceinline__ bool is_long(const AttnArgs& p, int n) { return n * p.G >= (p.P ? TREE ? p.long_rows : LONG_PREFIX : LONG); }
 __device__ __forceinline__ int narrow_tiles(const AttnArgs& p, int n) { return (n * p.G + 31) >> 5; }
 // `piece`: CUT or the length that items are rounded up to
 __device__ __forceinline__ int narrow_edge(int piece) { return piece == CUT ? CUT_EDGE : PIECE_EDGE; }
@@ -140,10 +150,11 @@ __device__ __forceinline__ int wide_sum(int step, int seen, int k) { return k * 
 __device__ __forceinline__ int wide_length(int step, int seen, int tile) { return seen + (tile + 1) * step; }
 __device__ __forceinline__ int wide_tiles(const AttnArgs& p, int n) { return (n + p.tpt - 1) / p.tpt; }
 __device__ __forceinline__ int packed_length(const AttnArgs& p, int blocks) { return ((blocks * 64 + WIDE_EDGE) >> p.ws) + 1; }
+template <bool TREE>
 __device__ __forceinline__ Extent extent(const AttnArgs& p, const Request& r, int piece) {
     Extent e{0, 0, 0, 0};
     if (r.n == 0) return e;
-    if (is_long(p, r.n)) {
+    if (is_long<TREE>(p, r.n)) {
         e.wide = p.Hkv * wide_sum(wide_step(p, piece), wide_seen(p, r, piece), wide_tiles(p, r.n));
     } else {
         e.items = narrow_tiles(p, r.n) * p.Hkv;
@@ -169,6 +180,7 @@ struct Plan {
     int rows, tiles, supers, super, nbp;  // packed rows, their wide tiles; pieces of the prefix, blocks of 64 tokens in one, in the prefix
     int valid;  // offsets are in order
     int joins;  // anything to join
+    int long_rows;  // as AttnArgs'
 };
 // Many packed tiles walk the prefix in pieces that stay in an XCD's L2 meanwhile.
 __device__ __host__ inline int super_count(int64_t P, int64_t tiles) {
@@ -180,6 +192,7 @@ __device__ __forceinline__ Plan make_plan(const AttnArgs& p, int narrow, int tea
     constexpr int N = attn_wgs<D>(), WAVES = 4 * N;
     Plan a;
     a.valid = 1;
+    a.long_rows = p.long_rows;
     a.rows = rows;
     a.nbp = (p.P + 63) >> 6;
     a.narrow0 = a.items0 = a.wide0 = a.head = 0;
@@ -253,14 +266,14 @@ __device__ __forceinline__ int find_group(const int (&sums)[GROUPS], int x, int 
     return n - 1;
 }
 // The request that holds place x of a line: its number and what is before it.  All lanes of a wavefront take part.
-template <bool WIDE>
+template <bool WIDE, bool TREE>
 __device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, int piece, int x, int lane, Extent& before) {
     const int g = uni(find_group(WIDE ? s.wide : s.narrow, x, lane));
     before = Extent{uni(s.narrow[g]), uni(s.items[g]), uni(s.rows[g]), uni(s.wide[g])};
     int b = g * p.per;
     if (p.per > 1) {  // at most 32 requests of a group: one a lane
         Extent e{0, 0, 0, 0};
-        if (lane < p.per && b + lane < p.B) e = extent(p, request(p, b + lane), piece);
+        if (lane < p.per && b + lane < p.B) e = extent<TREE>(p, request(p, b + lane), piece);
         Extent sum = e;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -278,6 +291,7 @@ __device__ __forceinline__ int find_request(const AttnArgs& p, const Sums& s, in
     return uni(b);
 }
 // The token and head of packed row r (below the total), each lane its own.
+template <bool TREE>
 __device__ __forceinline__ void packed_row(const AttnArgs& p, const Sums& s, int r, int& t, int& g) {
     int lo = 0, hi = GROUPS;
     while (hi - lo > 1) {
@@ -289,7 +303,7 @@ __device__ __forceinline__ void packed_row(const AttnArgs& p, const Sums& s, int
     int b = lo * p.per;
     Request q = request(p, b);
     for (int last = min(p.B, b + p.per) - 1; b < last; q = request(p, ++b)) {
-        const int n = extent(p, q, CUT).rows;
+        const int n = extent<TREE>(p, q, CUT).rows;
         if (at + n > r) break;
         at += n;
     }
@@ -317,19 +331,22 @@ __device__ __forceinline__ const uint8_t* run_of(const AttnArgs& p, int page_num
 // 16 bytes a lane from memory to LDS, at `to` + 16 lane.  (The request's own instruction, not the compiler's builtin: that
 // makes every later LDS read wait for all requests on their way, also those for other tiles.  It has no result in
 // registers; the waits are counted by hand below.)
+// ONCE: bytes that nobody else reads do not displace others in the caches.
+template <bool ONCE>
 __device__ __forceinline__ void request16(const uint8_t* base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");  // m0 is not the compiler's to keep: it sets it before any use
+    if (ONCE) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(offset), "s"(base), "s"(to) : "memory");
+    else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory");  // m0 is not the compiler's to keep: it sets it before any use
 }
 // Asks for 16 rows, tile rows 16 * half .., of which `last` + 1 exist from the run's start: rows past the last token repeat it, so that
 // whatever a page holds there is never multiplied.
-template <int D>
+template <int D, bool ONCE = false>
 __device__ __forceinline__ void fetch16(const uint8_t* run, int half, int last, uint32_t to, int lane) {
     constexpr int CH = D / 8, RPI = 64 / CH, NI = 16 / RPI;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int r = i * RPI + lane / CH, piece = (lane % CH) ^ spread<D>(r);  // spread() repeats after 16 rows
         const uint32_t whole = r * (D * 2) + piece * 16, cut = min(r, last) * (D * 2) + piece * 16;
-        request16(run, last == 15 ? whole : cut, to + half * (16 * D * 2) + i * 1024);
+        request16<ONCE>(run, last == 15 ? whole : cut, to + half * (16 * D * 2) + i * 1024);
     }
 }
 
@@ -608,6 +625,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
         // the item at x: its start and length on the line, its rows, its tokens
         int start, item, length, h, r0, rows, n_prefix, tokens = 0, seen = 0, clear_to = 0, b = -1;  // tiles of the prefix, then own tokens
         Request rq{0, 0, 0};
+        bool once = false;
         if (x < plan.narrow0) {
             length = rounded(narrow_units(p, p.P, plan.piece), plan.piece);
             h = x / length;
@@ -615,7 +633,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             r0 = 0, rows = plan.rows, n_prefix = (p.P + 31) >> 5;
         } else {
             Extent before;
-            b = find_request<false>(p, sums, plan.piece, x - plan.narrow0, lane, before);
+            b = find_request<false, TREE>(p, sums, plan.piece, x - plan.narrow0, lane, before);
             rq = request(p, b);
             length = narrow_length(p, rq.L, plan.piece);
             const int nt = narrow_tiles(p, rq.n), k = (x - plan.narrow0 - before.narrow) / length;
@@ -624,6 +642,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             r0 = (k - h * nt) * 32, rows = rq.n * p.G;
             tokens = max(0, rq.L - rq.n + min(r0 + 31, rows - 1) / p.G + 1), clear_to = rq.L - rq.n + r0 / p.G + 1;
             if (TREE && rq.n <= 64 * p.words) clear_to = rq.L - rq.n;
+            once = nt == 1;
             n_prefix = p.pre_tiles;
         }
         const int stop = min(end, start + length);
@@ -634,7 +653,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
         const int rc = min(r0 + (lane & 31), rows - 1);
         int ti = rc / p.G, g = rc - ti * p.G;
         if (b < 0) {
-            packed_row(p, sums, rc, ti, g);
+            packed_row<TREE>(p, sums, rc, ti, g);
         } else {
             seen = rq.L - rq.n + ti + 1;
             ti += rq.q0;
@@ -656,8 +675,9 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
         auto fetch = [&](int tile, const uint8_t* a, const uint8_t* c, int64_t shift, uint32_t dst) {
             const bool pre = tile < n_prefix;
             const int last = (pre ? p.P : tokens) - 1, left = last - (pre ? tile : tile - n_prefix) * 32;
-            fetch16<D>(a + shift, 0, min(left, 15), dst, lane);
-            fetch16<D>(c + shift, 1, left >= 16 ? min(left - 16, 15) : last & 15, dst, lane);
+            const int first = min(left, 15), second = left >= 16 ? min(left - 16, 15) : last & 15;
+            if (TREE && once && !pre) fetch16<D, true>(a + shift, 0, first, dst, lane), fetch16<D, true>(c + shift, 1, second, dst, lane);
+            else fetch16<D>(a + shift, 0, first, dst, lane), fetch16<D>(c + shift, 1, second, dst, lane);
         };
         int tile = t0;
         const uint8_t *ra = nullptr, *rb = nullptr, *na = nullptr, *nb = nullptr;
@@ -738,7 +758,7 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             slot = p.joint_blocks + ((int64_t)(h * plan.supers + s) * plan.tiles + tile + w) * 4;
         } else {
             Extent before;
-            b = find_request<true>(p, sums, plan.wide_piece, x - plan.wide0, lane, before);
+            b = find_request<true, TREE>(p, sums, plan.wide_piece, x - plan.wide0, lane, before);
             rq = request(p, b);
             const int nt = wide_tiles(p, rq.n);
             const int step = wide_step(p, plan.wide_piece), seen = wide_seen(p, rq, plan.wide_piece), head = wide_sum(step, seen, nt), y = x - plan.wide0 - before.wide;
@@ -771,12 +791,12 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
 
         const int r = wave * 32 + (lane & 31), rc = min(r, rows - 1);
         int ti = rc / p.G, g = rc - ti * p.G, seen = 0;
-        if (b < 0) packed_row(p, sums, r0 + rc, ti, g);
+        if (b < 0) packed_row<TREE>(p, sums, r0 + rc, ti, g);
         else {
             seen = rq.L - rq.n + t_base + ti + 1;
             ti += rq.q0 + t_base;
         }
-        const bool tree = TREE && b >= 0 && rq.n <= 64 * p.words;
+        const bool tree = TREE && b >= 0 && rq.n <= 64 * p.words, once = TREE && b >= 0 && wide_tiles(p, rq.n) == 1;
         const int clear_to = rq.L - rq.n + (tree ? 0 : t_base + (wave * 32) / p.G + 1);  // own tokens that all of the wavefront's rows see
         v8bf q[D / 16];
         const uint16_t* qp = p.Q + (int64_t)ti * p.ldq + (h * p.G + g) * D + (lane >> 5) * 8;
@@ -803,8 +823,8 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             const int j = token(k, last);
             const uint8_t* run = run_of<D>(p, page, h, j);
             const uint32_t dst = lds_at(lds) + (k & 1) * 2 * TILE;
-            fetch16<D>(run, wave, last, dst, lane);
-            fetch16<D>(run + to_v, wave, last, dst + TILE, lane);
+            if (TREE && once && k >= n_prefix) fetch16<D, true>(run, wave, last, dst, lane), fetch16<D, true>(run + to_v, wave, last, dst + TILE, lane);
+            else fetch16<D>(run, wave, last, dst, lane), fetch16<D>(run + to_v, wave, last, dst + TILE, lane);
         };
         int page = 0;
         if (k0 < k1) {
@@ -873,7 +893,8 @@ __device__ __forceinline__ int wave_scan(int v, Op op) {
 }
 
 template <int D, bool TREE>
-__global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(const AttnArgs p) {
+__global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(const AttnArgs args) {
+    AttnArgs p = args;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     AttnShared& sh = *reinterpret_cast<AttnShared*>(lds + 8 * 32 * D * 2);  // behind the tiles, which start at 0
     Sums& sums = sh.sums;
@@ -885,11 +906,23 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     bool wrong = false, few = true, many = true;  // no more than SOLO_FEW, SOLO_MANY tokens
     int longest = 0;  // the wide tile that sees most
     const int b0 = min(p.B, tid * p.per), b1 = min(p.B, b0 + p.per);
+    if (TREE && p.P) {
+        float own = 0.0f;  // in the same order in every workgroup
+        for (int b = b0; b < b1; ++b) {
+            const Request r = request(p, b);
+            if (r.n > 0 && r.n < LONG_TREE && r.n * p.G >= LONG && r.n * p.G < LONG_TREE) own += (float)r.L - LONG_OWN * (float)p.P;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) own += __shfl_xor(own, d);
+        if (lane == 0) sh.stats[wave] = own;
+        __syncthreads();
+        p.long_rows = sh.stats[0] + sh.stats[1] + sh.stats[2] + sh.stats[3] >= 0.0f ? LONG : LONG_TREE;
+    }
     for (int b = b0; b < b1; ++b) {
         const Request r = request(p, b);
         wrong |= r.q0 < 0 || r.n < 0 || r.q0 > T - r.n;
         if (wrong) break;
-        const Extent e = extent(p, r, CUT);
+        const Extent e = extent<TREE>(p, r, CUT);
         few &= p.P + r.L <= SOLO_FEW, many &= p.P + r.L <= SOLO_MANY;
         const int n = narrow_units(p, r.L, TEAM) + p.pre_tiles;
         if (e.wide > 0) {
@@ -933,10 +966,10 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
     if (blockIdx.x == 0) {  // what the second kernel looks its segments up with
         if (tid == 0) *p.plan = plan;
         for (int b = b0; b < b1; ++b) {
-            const Extent e = extent(p, request(p, b), plan.piece);
+            const Extent e = extent<TREE>(p, request(p, b), plan.piece);
             int* r = p.records + (int64_t)b * 4;
             r[0] = v[0], r[1] = v[4], r[2] = v[5], r[3] = v[6];
-            v[0] += e.narrow, v[4] += e.items, v[5] += e.rows, v[6] += plan.wide_piece == plan.piece ? e.wide : extent(p, request(p, b), plan.wide_piece).wide;
+            v[0] += e.narrow, v[4] += e.items, v[5] += e.rows, v[6] += plan.wide_piece == plan.piece ? e.wide : extent<TREE>(p, request(p, b), plan.wide_piece).wide;
         }
     }
     __syncthreads();
@@ -960,7 +993,7 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
 // A wavefront joins H = 1 or 4 rows (heads) of a token.  First 64 / H lanes a row find one segment each and read its base and
 // weight; then D/4 lanes hold four channels each of a row's sums: all groups of lanes share one row's segments (H = 1: few
 // rows, of many segments), or have rows of their own (H = 4: more rows than the card holds wavefronts).
-template <int D, int H>
+template <int D, int H, bool TREE>
 __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnArgs p) {
     constexpr int LANES = D / 4, GRP = 64 / LANES, S = 64 / H, ROWS = H == 1 ? 1 : H / GRP, STEP = H == 1 ? GRP : 1;
     const int lane = threadIdx.x & 63, sub = lane / LANES, l = lane % LANES, jl = lane % S;
@@ -991,7 +1024,7 @@ __global__ __launch_bounds__(256) void prefix_attention_join_kernel(const AttnAr
                         __builtin_amdgcn_readlane(all.w, found)};
     const int i = t - rq.q0;
     if (i < 0 || i >= rq.n) return;
-    const bool joint = is_long(p, rq.n);
+    const bool joint = rq.n * p.G >= (p.P ? TREE ? plan.long_rows : LONG_PREFIX : LONG);
     const int cp = rounded(narrow_units(p, p.P, plan.piece), plan.piece), packed_item = packed_length(p, plan.super);
     const int pre_pieces = packed_item == plan.wide_per ? 1 : plan.tiles ? (packed_item - 1) / plan.wide_per + 2 : 0;  // of a piece of the prefix, at most
 
@@ -1116,11 +1149,11 @@ struct AttnSpace {
     int64_t joint, packed, narrow;  // blocks
     size_t records, blocks, total;  // offsets
 };
-static AttnSpace attn_space(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t P) {
+static AttnSpace attn_space(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t P, bool tree) {
     const int64_t G = Hq / Hkv, rows = T * G, wgs = D == 128 ? attn_wgs<128>() : attn_wgs<64>(), some = std::min<int64_t>(B, T);
     const int64_t is_short = P && !inline_tiles(T, B, Hq, Hkv, D, P) ? std::min<int64_t>(rows, (LONG_PREFIX - 1) * (int64_t)B) : 0;  // rows that walk the prefix packed, at most
     AttnSpace a;
-    a.joint = rows >= (P ? LONG_PREFIX : LONG) ? 2 * wgs * 4 : 0;
+    a.joint = rows >= (P && !tree ? LONG_PREFIX : LONG) ? 2 * wgs * 4 : 0;
     const int64_t tiles = (is_short + WROWS - 1) / WROWS;
     a.packed = is_short > 32 ? (std::max(Hkv * tiles * super_count(P, tiles), wgs) + wgs) * 4 : 0;
     a.narrow = Hkv * (1 + (P ? std::min<int64_t>(rows, (LONG_PREFIX - 1) * (int64_t)B) / 32 + some : some)) + 4 * wgs;
@@ -1130,8 +1163,8 @@ static AttnSpace attn_space(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32
     return a;
 }
 
-size_t prefix_attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len) {
-    return attn_space(T, B, Hq, Hkv, D, prefix_len).total;
+size_t prefix_attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len, bool tree) {
+    return attn_space(T, B, Hq, Hkv, D, prefix_len, tree).total;
 }
 
 template <int D, bool TREE>
@@ -1144,8 +1177,8 @@ static int launch(const AttnArgs& p, hipStream_t st) {
     // a wavefront a row while the card holds them at once, four rows beyond that
     const bool few = p.T * p.Hq <= 4096;
     const int64_t wgs = (p.T * (few ? p.Hq : (p.Hq + 3) / 4) + 3) / 4;
-    if (few) prefix_attention_join_kernel<D, 1><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
-    else prefix_attention_join_kernel<D, 4><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
+    if (few) prefix_attention_join_kernel<D, 1, TREE><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
+    else prefix_attention_join_kernel<D, 4, TREE><<<dim3((unsigned)wgs), 256, 0, st>>>(p);
     return check_launch(TREE ? "osc_tree_attention" : "osc_prefix_attention");
 }
 
@@ -1159,17 +1192,18 @@ int launch_prefix_attention(const AttnCall& a, hipStream_t st) {
     p.kv_lens = a.kv_lens, p.q_offsets = a.q_offsets, p.B = a.B, p.per = (a.B + GROUPS - 1) / GROUPS, p.c = a.scale * 1.44269504088896341f;
     p.O = static_cast<uint16_t*>(a.O), p.ldo = a.ldo, p.lse = a.lse;
     p.pre_tiles = inline_tiles(a.T, a.B, a.Hq, a.Hkv, a.D, a.prefix_len);
-    const AttnSpace s = attn_space(a.T, a.B, a.Hq, a.Hkv, a.D, a.prefix_len);
+    const AttnSpace s = attn_space(a.T, a.B, a.Hq, a.Hkv, a.D, a.prefix_len, a.mask != nullptr);
     p.plan = reinterpret_cast<Plan*>(a.workspace), p.records = reinterpret_cast<int*>(a.workspace + s.records);
     p.blocks = a.workspace + s.blocks;
     p.joint_blocks = s.joint, p.packed_blocks = s.packed, p.narrow_blocks = s.narrow;
     // the longest that the lines can be
-    const int64_t rows = a.T * p.G, is_long = rows / (p.P ? LONG_PREFIX : LONG), tiles = rows / WROWS + 1, some = std::min<int64_t>(a.B, a.T);
+    const int64_t rows = a.T * p.G, is_long = rows / (p.P && !a.mask ? LONG_PREFIX : LONG), tiles = rows / WROWS + 1, some = std::min<int64_t>(a.B, a.T);
     const int64_t wide = (int64_t)p.Hkv * (a.T / p.tpt + is_long) * (WIDE_EDGE + p.P + (int64_t)p.max_kv + a.T + WROWS) +
                          (int64_t)p.Hkv * tiles * 2 * (p.P + (WIDE_EDGE + 64) * MAX_SUPER);
     const int64_t narrow = (int64_t)p.Hkv * (rows / 32 + some + 1) * (std::max<int64_t>(p.P, p.max_kv) / 32 + p.pre_tiles + CUT_EDGE + PIECE3 + 1);
     for (p.ws = 0; wide >> p.ws > 1 << 30;) ++p.ws;
     for (p.ns = 0; narrow >> p.ns > 1 << 30;) ++p.ns;
+    p.long_rows = LONG_TREE;
     p.mask = a.mask, p.ldm = a.ldm, p.words = a.words;
     if (p.mask) return a.D == 64 ? launch<64, true>(p, st) : launch<128, true>(p, st);
     return a.D == 64 ? launch<64, false>(p, st) : launch<128, false>(p, st);

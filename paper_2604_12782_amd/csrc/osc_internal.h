@@ -157,7 +157,7 @@ struct AttnCall {
 constexpr int32_t PAGED_MAX_REQUESTS = 8192;  // both kernels hold the requests' running sums in LDS
 // A tile's length on the line is made of a prefix and up to ATTN_MAX_TOKENS tokens of a request's own and of up to 255 more, in 31 bits.
 constexpr int64_t ATTN_MAX_TOKENS = 0x3fffffff, ATTN_MAX_PREFIX = 0x7fffffff - ATTN_MAX_TOKENS - 256;
-size_t prefix_attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len);
+size_t prefix_attention_workspace(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len, bool tree);
 int launch_prefix_attention(const AttnCall& a, hipStream_t st);
 
 // trees of drafted tokens (tree.hip), pages and cached tokens in other hands (pages.hip), log probabilities (logprob.hip)
