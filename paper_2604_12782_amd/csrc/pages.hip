@@ -5,9 +5,13 @@
 namespace osc {
 
 // ---- keys and values from slot to slot -----------------------------------------------------------------------------------
-// A wavefront has a group of pairs, one head of one layer.  It holds 64 pairs a round, those that move anything put together, and
-// takes a few of them at a time: a lane moves 16 bytes of a row, all loads of a batch before its stores, batches and rounds in
-// order, so a slot may be read by a pair and written by a later one.  Bound by HBM where much is moved, by latency otherwise.
+// A wavefront has a group of pairs, one head of one layer, and its keys or its values.  It holds 64 pairs a round, those that move anything put
+// together, and takes 32 (heads of 64: 64) of them at a time: a lane moves 16 bytes of a row, all loads of a batch before its stores, batches
+// and rounds in order, so a slot may be read by a pair and written by a later one.  Bound by HBM where much is moved, by
+// latency otherwise: the pairs' read, the rows' read, the store.  Stores go past the caches: plain ones stay there until the kernel's end, and are
+// all written then.  150 (1000) groups of 32 pairs, 4 heads of 128 in 4 layers, 79 (524) MB read and written: 12 (103) us, with plain stores
+// 30 (155), with loads past the caches too 16 (102).
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 struct MoveArgs {
     uint8_t *K, *V;
     int64_t layer;  // bytes from layer to layer
@@ -18,18 +22,17 @@ struct MoveArgs {
 };
 template <int D>
 __global__ __launch_bounds__(256) void cache_move_kernel(const MoveArgs p) {
-    constexpr int LANES = D / 8, ROWS = 64 / LANES, BATCH = 4;  // lanes a row, rows a load, loads of K and of V in a batch
+    constexpr int LANES = D / 8, ROWS = 64 / LANES, BATCH = 8;  // lanes a row, rows a load, loads in a batch
     const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = (int)(unit % p.Hkv);
-    const int g = (int)(unit / p.Hkv);
+    const unsigned unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = unit / (unsigned)p.Hkv, h = unit - g * p.Hkv;
     if (g >= p.N) return;
     int64_t from = (int64_t)g * p.per, to = from + p.per;
     if (p.offsets) {
         from = p.offsets[g], to = p.offsets[g + 1];
         if (from < 0 || to > p.T) return;
     }
-    uint8_t *K = p.K + blockIdx.y * p.layer, *V = p.V + blockIdx.y * p.layer;
+    uint8_t* C = (blockIdx.y & 1 ? p.V : p.K) + (blockIdx.y >> 1) * p.layer;
     auto row = [&](int slot) { return ((((int64_t)(slot >> p.lg) * p.Hkv + h) << p.lg) + (slot & ((1 << p.lg) - 1))) * (D * 2) + lane % LANES * 16; };
     for (int64_t t = from; t < to; t += 64) {
         int a = -1, b = -1;
@@ -41,24 +44,19 @@ __global__ __launch_bounds__(256) void cache_move_kernel(const MoveArgs p) {
         const int below = __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0)), at = moves ? below : m + lane - below;
         a = __builtin_amdgcn_ds_permute(at * 4, a), b = __builtin_amdgcn_ds_permute(at * 4, b);
         for (int k = 0; k < m; k += ROWS * BATCH) {
-            uint4 kv[2][BATCH];
-            int64_t put[BATCH];
-            bool has[BATCH];
+            uint4v v[BATCH];
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
-                const int j = k + i * ROWS + lane / LANES;
-                const int sa = __shfl(a, min(j, 63)), sb = __shfl(b, min(j, 63));
-                has[i] = j < m;
-                if (has[i]) {
-                    put[i] = row(sb);
-                    kv[0][i] = *reinterpret_cast<const uint4*>(K + row(sa)), kv[1][i] = *reinterpret_cast<const uint4*>(V + row(sa));
-                }
+                const int j = k + i * ROWS + lane / LANES, slot = __shfl(a, j & 63);
+                if (j < m) v[i] = *reinterpret_cast<const uint4v*>(C + row(slot));
             }
             wait_vmcnt<0>();  // what a store overwrites has been read
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int i = 0; i < BATCH; ++i)
-                if (has[i]) *reinterpret_cast<uint4*>(K + put[i]) = kv[0][i], *reinterpret_cast<uint4*>(V + put[i]) = kv[1][i];
+            for (int i = 0; i < BATCH; ++i) {
+                const int j = k + i * ROWS + lane / LANES, slot = __shfl(b, j & 63);
+                if (j < m) __builtin_nontemporal_store(v[i], reinterpret_cast<uint4v*>(C + row(slot)));
+            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
@@ -69,7 +67,7 @@ int launch_cache_move(void* K, void* V, int32_t n_layers, int64_t layer_stride, 
     MoveArgs p;
     p.K = static_cast<uint8_t*>(K), p.V = static_cast<uint8_t*>(V), p.layer = layer_stride * 2, p.Hkv = Hkv, p.lg = lg, p.slots = (int)(n_pages << lg);
     p.src = src, p.dst = dst, p.offsets = offsets, p.T = T, p.N = N, p.per = offsets ? 0 : (int)(T / N);
-    const dim3 grid((unsigned)(((int64_t)N * Hkv + 3) / 4), (unsigned)n_layers);
+    const dim3 grid((unsigned)(((int64_t)N * Hkv + 3) / 4), (unsigned)n_layers * 2);
     if (D == 64) cache_move_kernel<64><<<grid, 256, 0, st>>>(p);
     else cache_move_kernel<128><<<grid, 256, 0, st>>>(p);
     return check_launch("osc_cache_move");
