@@ -502,7 +502,8 @@ int osc_tree_mask(const int32_t *parents, const int32_t *q_offsets, const int32_
  * 0 .. L - n - 1, and those new tokens j <= i whose bit its words hold.  A row need not see itself; one that sees nothing gives zeros and
  * -infinity.  Bits of later rows are ignored, so any mask under the diagonal will do, not only a tree's.
  *   mask       uint64 [T, ldm], 8-byte aligned;  words  1 to 8, ldm >= words
- *   workspace  osc_tree_attention_workspace_bytes(...) bytes
+ *   workspace  osc_tree_attention_workspace_bytes(...) bytes: osc_prefix_attention's, and 68 MB (D = 64: 52) more behind a prefix where the step has
+ *              33 to 255 rows (tokens times Hq / Hkv)
  */
 size_t osc_tree_attention_workspace_bytes(int64_t T, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int64_t prefix_len);
 int osc_tree_attention(const void *Q, int64_t T, int32_t Hq, int32_t Hkv, int32_t D, int64_t ldq, const void *Kc, const void *Vc,

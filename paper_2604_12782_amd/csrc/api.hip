@@ -1,5 +1,6 @@
 // C ABI of libosc: argument checking and dispatch.  Every check runs on the host before
 // anything is enqueued, so the error paths need no GPU.
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 
@@ -858,8 +859,9 @@ static int check_apart(const char* who, const Extent4* a, int written, int all) 
     for (int i = 0; i < written; ++i)
         for (int j = i + 1; j < all; ++j) {
             const uintptr_t x = (uintptr_t)a[i].at, y = (uintptr_t)a[j].at;
-            REQUIRE(a[i].n == 0 || a[j].n == 0 || !x || !y || x + a[i].n * 4 <= y || y + a[j].n * 4 <= x, OSC_ERR_UNSUPPORTED,
-                    "%s: %s, which is written, overlaps %s", who, a[i].name, a[j].name);
+            const uint64_t most = (uint64_t)1 << 60, nx = std::min<uint64_t>(a[i].n, most) * 4, ny = std::min<uint64_t>(a[j].n, most) * 4;  // pitches may be anything
+            REQUIRE(nx == 0 || ny == 0 || !x || !y || x + nx <= y || y + ny <= x, OSC_ERR_UNSUPPORTED, "%s: %s, which is written, overlaps %s", who, a[i].name,
+                    a[j].name);
         }
     return OSC_OK;
 }
@@ -878,11 +880,11 @@ int osc_tree_mask(const int32_t* parents, const int32_t* q_offsets, const int32_
     if (rc) return rc;
     REQUIRE(pos_base >= 0, OSC_ERR_SHAPE, "%s: pos_base=%d", who, pos_base);
     REQUIRE(words >= 1 && words <= TREE_MAX_WORDS, OSC_ERR_UNSUPPORTED, "%s: %d words of 64 drafted tokens (1 to %d)", who, words, TREE_MAX_WORDS);
-    REQUIRE(ldm >= words && ldm <= 0x7fffffff, OSC_ERR_SHAPE, "%s: ldm=%lld", who, (long long)ldm);
+    REQUIRE(ldm >= words && ldm <= 0x3fffffff, OSC_ERR_SHAPE, "%s: ldm=%lld", who, (long long)ldm);
     if (T == 0) return OSC_OK;
     REQUIRE(mask && positions && (B == 0 || (parents && q_offsets && kv_lens)), OSC_ERR_NULL, "%s: null pointer", who);
     REQUIRE(aligned(mask, 8), OSC_ERR_UNSUPPORTED, "%s: the mask must be 8-byte aligned", who);
-    const Extent4 arrays[] = {{"mask", mask, ((T - 1) * ldm + words) * 2}, {"positions", positions, T}, {"parents", parents, T}, {"q_offsets", q_offsets, (int64_t)B + 1},
+    const Extent4 arrays[] = {{"mask", mask, (T - 1) * ldm * 2 + words * 2}, {"positions", positions, T}, {"parents", parents, T}, {"q_offsets", q_offsets, (int64_t)B + 1},
                               {"kv_lens", kv_lens, B}};
     rc = check_apart(who, arrays, 2, 5);
     if (rc) return rc;

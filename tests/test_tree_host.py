@@ -176,3 +176,9 @@ def test_plain_logprobs_against_torch():
     want = torch.log_softmax(1.5 * x, 1)
     assert np.allclose(lp[:3, 0], want[[0, 1, 2], [1, 2, 49]]) and lp[3, 0] == 0 and np.allclose(lse, torch.logsumexp(1.5 * x, 1))
     assert np.allclose(top, want.topk(5).values) and np.array_equal(ids, want.topk(5).indices) and np.allclose(ent, -(want.exp() * want).sum(1))
+
+
+def test_extents_past_32_bits():
+    """overlap checks hold for pitches whose last element lies past 2^32 bytes, and past 2^64"""
+    assert rc(ACCEPT, ch=8 * P, ldc=2 ** 31 - 1, T=2 ** 31 - 1, par=P) == UNSUPPORTED   # whatever is behind it is inside
+    assert rc(MASK, T=2 ** 31 - 1, ldm=2 ** 30 - 1, pos=2 ** 40) == UNSUPPORTED
