@@ -22,6 +22,16 @@
 // exponentials and LDS reads take turns with them, and power brings the clock from 2.4 to 1.9 GHz meanwhile; no one part left out makes
 // up the difference.  12 long requests without a prefix 66 us (42, bytes): 5.3 TB/s in the first kernel, then the second.  Small
 // batches are bound by latency: the plan's reads, a few tiles that depend on one another, the second kernel's reads.
+//
+// Trees (a variant of the first kernel, TREE).  A row's bits cut what it sees of the request's new tokens, beside the limit by its place; tiles, lines and
+// joining are the same.  Only blocks that reach a new token look at bits.  Three things differ: which requests are long behind a prefix (LONG_TREE),
+// keys and values that one tile alone walks go past the caches (24 trees of up to 16 tokens with up to 3100 of their own 68.7 -> 61.7 us; tiles that
+// share them would lose: 95.6 -> 97.4, 192 -> 220), and so the workspace.  Those 24 trees (209 MB, 30 us at a reading pass's rate): 4.6 us until the
+// plan is there, 5 to an item's first request, 30 to 35 walking at 6 TB/s, 9 for the second kernel.  6 trees of up to 97 tokens, 3 heads of
+// 64 a key/value head, with up to 24000 of their own: 94 us, vector ALU 57 %, matrix cores 30 % busy (43 GFLOP; reads beyond L2 are a fifth above
+// the cache's size).  Tried for trees and dropped: blocks of 32 tokens three ahead (62 -> 68 us), a block's tokens split between
+// wavefronts without rows (62 -> 63), rows on other wavefronts in the workgroups of a CU, priorities for three workgroups a CU, tiles of a request
+// cut at the same tokens (8 trees of 64 with up to 12000 141 -> 155, 6 of 97 95.6 -> 93.9).
 #include <algorithm>
 
 #include "osc_internal.h"

@@ -236,3 +236,13 @@ def test_deal_fork_free(osc):
         assert np.array_equal(np.maximum(holders - 1, 0), refs.cpu().numpy())
         listed = free[:n_free.item()].tolist()
         assert len(set(listed)) == len(listed) and all(holders[p] == 0 for p in listed) and len(listed) == (holders == 0).sum()
+
+
+def test_most_requests_and_many_pages(osc):
+    gen = np.random.default_rng(9)
+    n_pages, B = 2 ** 19 + 77, 8192
+    table = gen.integers(0, n_pages, (B, 9))
+    refs = gen.integers(0, 2, n_pages)
+    check_free(osc, gen.integers(0, 145, B), gen.integers(0, 60, B), 16, table, n_pages, 90000, 40, refs=refs)
+    rows = gen.permutation(B)
+    check_fork(osc, gen.choice(rows[4096:], 4096), rows[:4096], gen.integers(0, 65, B), 16, 4, 5000, 4100)

@@ -273,3 +273,64 @@ def test_accept_refused_and_idle_requests(osc):
     lens = i32([9, 4])
     out = osc.osc_tree_accept(i32([-1, 0]), i32([0, 0]), i32([0, 0]), i32([0, 9, 2]), lens, i32([1, 2]))  # offsets that leave the step: no rows
     assert out[1].tolist() == [0, 0] and out[3].tolist() == [9, 4]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_queries_that_are_not_finite(osc, D):
+    """NaN or infinity in one head of one row: that head is NaN, others are what they were; a head that sees nothing stays zero"""
+    for P, counts, kv in ((0, [9, 40, 3], [30, 300, 3]), (400, [9, 40, 3], [30, 300, 3])):
+        s = make(7 + P, 3, P, kv, counts, 4, 2, D, 16)
+        mask = tree_of(0, s, counts, 1)
+        mask[49] = 0  # the last request's first row sees no new token
+        before, lse0 = check(osc, s, mask)
+        for row, bad in ((3, float("nan")), (20, float("inf")), (49, float("nan"))):
+            t = dict(s, Q=s["Q"].clone())
+            t["Q"][row, 5] = bad
+            o, lse = call(osc, t, mask)
+            hit = torch.zeros(52, 4, dtype=torch.bool, device=DEV)
+            hit[row, 0] = P > 0 or row != 49
+            nan = torch.isnan(o.view(52, 4, D))
+            assert torch.equal(torch.isnan(lse), hit) and torch.equal(nan.all(-1), hit) and torch.equal(nan.any(-1), hit)
+            keep = ~hit
+            assert torch.equal(o.view(52, 4, D)[keep], before.view(52, 4, D)[keep]) and torch.equal(lse[keep], lse0[keep])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("own", [20, 900])
+def test_attention_of_trees_of_33_to_64_rows_behind_a_prefix(osc, own, D):
+    """their requests walk the prefix themselves where they have many tokens of their own, and packed otherwise"""
+    counts = [9, 10, 16, 12, 8, 17, 33]
+    kv = [c + own + 5 * i for i, c in enumerate(counts)]
+    s = make(own, len(kv), 700, kv, counts, 8, 2, D, 32)
+    mask = tree_of(1, s, counts, 1)
+    check(osc, s, mask)
+
+
+def test_attention_most_requests(osc):
+    gen = np.random.default_rng(2)
+    counts, kv = gen.integers(0, 3, 8192), gen.integers(0, 20, 8192)
+    counts[5000], kv[5000] = 70, 120
+    kv = np.maximum(kv, counts)
+    s = make(20, 8192, 18, kv.tolist(), counts.tolist(), 1, 1, 64, 16)
+    check(osc, s, tree_of(0, s, counts.tolist(), 2))
+
+
+def test_two_calls_at_once(osc):
+    """two streams, a workspace each, neither the default one: each as if alone"""
+    sets, counts = [], ([7] * 12, [40, 3, 12] * 4)
+    for i, c in enumerate(counts):
+        s = make(40 + i, 12, 300 * i, [k + 700 for k in c], c, 8, 2, 128, 16)
+        mask = tree_of(i, s, c, 1)
+        o, lse = call(osc, s, mask)
+        n = osc.osc_tree_attention_workspace_bytes(sum(c), 12, 8, 2, 128, 300 * i)
+        sets.append((s, mask, o.clone(), lse.clone(), torch.empty(n, dtype=torch.uint8, device=DEV), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = ([], [])
+    for _ in range(10):
+        for i, (s, mask, _, _, ws, stream) in enumerate(sets):
+            with torch.cuda.stream(stream):
+                got[i].append(call(osc, s, mask, workspace=ws))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o, lse in got[i]:
+            assert torch.equal(o, sets[i][2]) and torch.equal(lse, sets[i][3])
