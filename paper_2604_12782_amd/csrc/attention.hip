@@ -36,6 +36,7 @@
 
 #include "osc_internal.h"
 #include "lds_dma.h"
+#include "wave_util.h"
 
 namespace osc {
 
@@ -889,18 +890,6 @@ struct AttnShared {
     int part[4][11];
     float stats[256];
 };
-
-// of the lanes below and this one, on the vector ALU: four steps inside rows of 16 lanes, then the rows' last lanes; op(x, 0) is x
-template <class Op>
-__device__ __forceinline__ int wave_scan(int v, Op op) {
-    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true));   // from one lane below
-    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true));   // two
-    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true));   // four
-    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true));   // eight
-    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));  // lane 15 of a row to the next, in rows 1 and 3
-    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));  // lane 31 to rows 2 and 3
-    return v;
-}
 
 template <int D, bool TREE>
 __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(const AttnArgs args) {

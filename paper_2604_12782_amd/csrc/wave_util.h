@@ -49,6 +49,18 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
     return max(max(a, b), max(c, d));
 }
 
+// of the lanes below and this one, on the vector ALU: four steps inside rows of 16 lanes, then the rows' last lanes; op(x, 0) is x
+template <class Op>
+__device__ __forceinline__ int wave_scan(int v, Op op) {
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true));   // from one lane below
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true));   // two
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true));   // four
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true));   // eight
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));  // lane 15 of a row to the next, in rows 1 and 3
+    v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));  // lane 31 to rows 2 and 3
+    return v;
+}
+
 // ---- packed 16-bit magnitudes and 8-bit codes ------------------------------------------------
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 // element-wise maximum of two pairs of 16-bit magnitudes (one packed instruction)
