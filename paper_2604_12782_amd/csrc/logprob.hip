@@ -279,7 +279,8 @@ __global__ __launch_bounds__(64 * WAVES, NV == 2 ? 8 : 4) void token_logprobs_ke
     const float c = p.c;
     const int shift = rounds > 64 ? 26 - __builtin_clz(rounds - 1) : 0;  // 2^shift rounds a bit
     bool usual = false;  // every lane has a base, and c times it is an ordinary number
-    float B = 0.0f, mine = -INFINITY, passed = -INFINITY;  // passed: k lanes of the wavefront have reached it
+    float B = 0.0f, mine = -INFINITY, second = -INFINITY, passed = -INFINITY;  // chunks' largest logits, the best two; passed: k lanes of the wavefront have reached it
+    int best_it = 0;
     uint64_t marks = 0;
     for (int it = 0; it < rounds; ++it) {
         const int ch = chunk_of(it);
@@ -300,6 +301,8 @@ __global__ __launch_bounds__(64 * WAVES, NV == 2 ? 8 : 4) void token_logprobs_ke
                 if (mine < passed) marks = 0;
             }
             if (largest >= passed) marks |= 1ull << (it >> shift);
+            second = __builtin_amdgcn_fmed3f(second, mine, largest);
+            best_it = largest > mine ? it : best_it;
             mine = fmaxf(mine, largest);
         }
         float s = 0.0f, u = 0.0f;
@@ -347,8 +350,9 @@ __global__ __launch_bounds__(64 * WAVES, NV == 2 ? 8 : 4) void token_logprobs_ke
         const uint32_t bound = reached_by<4>({tops[lane], tops[lane + 64], tops[lane + 128], tops[lane + 192]}, p.k);
         if (top >= bound) {
             const float from = value_of(bound);
-            for (uint64_t left = marks; left; left &= left - 1) {
-                const int it0 = __builtin_ctzll(left) << shift, it1 = min(rounds, it0 + (1 << shift));
+            const bool one = ordered(second) < bound;  // one chunk has all that the lane can give
+            for (uint64_t left = one ? 1 : marks; left; left &= left - 1) {
+                const int it0 = one ? best_it : __builtin_ctzll(left) << shift, it1 = one ? it0 + 1 : min(rounds, it0 + (1 << shift));
                 for (int it = it0; it < it1; ++it) {
                     const int ch = chunk_of(it);
                     float v[PER];
