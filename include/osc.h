@@ -536,7 +536,8 @@ int osc_tree_accept(const int32_t *parents, const int32_t *tokens, const int32_t
  *   Kc, Vc     bf16 [n_layers][n_pages][Hkv][page_size][D], layers layer_stride elements apart (a multiple of 8), 16-byte aligned;
  *              D 64 or 128
  *   src_slots, dst_slots  int32 [T]; a pair with a slot outside the cache (-1), or with the same slot twice, moves nothing
- *   offsets    int32 [N + 1]: pairs offsets[g] .. offsets[g+1] - 1 are a group (one that leaves [0, T] is left out); NULL: N groups of T / N pairs
+ *   offsets    int32 [N + 1]: pairs offsets[g] .. offsets[g+1] - 1 are a group (one that leaves [0, T] is left out); NULL: N groups of T / N pairs.
+ *              N * Hkv < 2^26
  * Groups are moved at the same time, pairs of a group in order: a slot may be written after it was read in the same group (tokens moved
  * towards a sequence's start), but not read or written again after it was written, nor be in two groups if one of them writes it.
  * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.
@@ -594,7 +595,7 @@ int osc_page_free(const int32_t *kv_lens, const int32_t *new_lens, int32_t B, in
  *   top_k      0 to 64, at most V;  scale > 0 (1 / temperature)
  *   workspace  osc_token_logprobs_workspace_bytes(T, V, top_k) bytes, 256-byte aligned (NULL where that is 0); contents do not matter and
  *              are not kept; calls that may overlap need one each
- * Results are identical from run to run.
+ * No array that is written may overlap another.  Results are identical from run to run.
  * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_WORKSPACE, OSC_ERR_HIP.
  */
 size_t osc_token_logprobs_workspace_bytes(int64_t T, int64_t V, int32_t top_k);

@@ -849,17 +849,18 @@ int osc_tree_attention(const void* Q, int64_t T, int32_t Hq, int32_t Hkv, int32_
 
 // ---- trees of drafted tokens, pages in other hands, log probabilities ----
 
-// Arrays of 4-byte elements; the first `written` of them are written and may not overlap any other.
+// Arrays, of 4-byte elements if nothing else is said; the first `written` of them are written and may not overlap any other.
 struct Extent4 {
     const char* name;
     const void* at;
     int64_t n;
+    int size = 4;
 };
 static int check_apart(const char* who, const Extent4* a, int written, int all) {
     for (int i = 0; i < written; ++i)
         for (int j = i + 1; j < all; ++j) {
             const uintptr_t x = (uintptr_t)a[i].at, y = (uintptr_t)a[j].at;
-            const uint64_t most = (uint64_t)1 << 60, nx = std::min<uint64_t>(a[i].n, most) * 4, ny = std::min<uint64_t>(a[j].n, most) * 4;  // pitches may be anything
+            const uint64_t most = (uint64_t)1 << 60, nx = std::min<uint64_t>(a[i].n, most) * a[i].size, ny = std::min<uint64_t>(a[j].n, most) * a[j].size;  // pitches may be anything
             REQUIRE(nx == 0 || ny == 0 || !x || !y || x + nx <= y || y + ny <= x, OSC_ERR_UNSUPPORTED, "%s: %s, which is written, overlaps %s", who, a[i].name,
                     a[j].name);
         }
@@ -923,8 +924,8 @@ int osc_cache_move(void* Kc, void* Vc, int32_t n_layers, int64_t layer_stride, i
     REQUIRE(n_layers >= 0 && N >= 0 && T >= 0 && (n_layers <= 1 || layer_stride >= (n_pages * Hkv << lg) * D), OSC_ERR_SHAPE,
             "%s: n_layers=%d layer_stride=%lld N=%d T=%lld", who, n_layers, (long long)layer_stride, N, (long long)T);
     REQUIRE(layer_stride % 8 == 0 || n_layers <= 1, OSC_ERR_UNSUPPORTED, "%s: layers must be 16-byte aligned", who);
-    REQUIRE(n_layers <= 32767 && T <= 0x7fffffff && (int64_t)N * Hkv <= 0x7fffffff, OSC_ERR_UNSUPPORTED,
-            "%s: n_layers=%d N=%d T=%lld (at most 32767 layers, 2^31-1 pairs and heads of groups)", who, n_layers, N, (long long)T);
+    REQUIRE(n_layers <= 32767 && T <= 0x7fffffff && (int64_t)N * Hkv < 1 << 26, OSC_ERR_UNSUPPORTED,  // a launch has less than 2^32 threads along an axis
+            "%s: n_layers=%d N=%d T=%lld (at most 32767 layers, 2^31-1 pairs; heads of groups below 2^26)", who, n_layers, N, (long long)T);
     REQUIRE(offsets || N == 0 || T % N == 0, OSC_ERR_SHAPE, "%s: %lld pairs are not %d groups of the same size, and there are no offsets", who, (long long)T, N);
     if (N == 0 || T == 0 || n_layers == 0 || n_pages == 0) return OSC_OK;
     REQUIRE(Kc && Vc && src_slots && dst_slots, OSC_ERR_NULL, "%s: null pointer", who);
@@ -993,6 +994,12 @@ int osc_token_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int6
     REQUIRE(need == 0 || workspace, OSC_ERR_NULL, "%s: null workspace", who);
     REQUIRE(need == 0 || aligned(workspace, 256), OSC_ERR_UNSUPPORTED, "%s: workspace must be 256-byte aligned", who);
     REQUIRE(workspace_bytes >= need, OSC_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
+    const int64_t seen = ldl > ((int64_t)1 << 60) / T ? (int64_t)1 << 60 : (T - 1) * ldl + V;
+    const Extent4 arrays[] = {{"logprobs", logprobs, T * n_tokens}, {"top_ids", top_ids, T * top_k}, {"top_logprobs", top_logprobs, T * top_k}, {"lse", lse, T},
+                              {"entropy", entropy, T}, {"workspace", workspace, (int64_t)need, 1}, {"tokens", tokens, T * n_tokens},
+                              {"logits", logits, seen, dtype == OSC_DT_F32 ? 4 : 2}};
+    const int rc = check_apart(who, arrays, 6, 8);
+    if (rc) return rc;
     return launch_token_logprobs(logits, dtype == OSC_DT_F32, T, V, ldl, scale, tokens, n_tokens, top_k, logprobs, top_ids, top_logprobs, lse, entropy,
                                  static_cast<uint8_t*>(workspace), as_stream(stream));
 }

@@ -491,6 +491,16 @@ int launch_token_logprobs(const void* X, bool f32, int64_t T, int64_t V, int64_t
     LogpArgs p;
     p.X = static_cast<const uint8_t*>(X), p.T = T, p.V = V, p.ldl = ldl, p.scale = scale, p.c = scale * 1.44269504088896341f;
     p.tokens = tokens, p.n_tok = n_tok, p.k = k, p.lp = lp, p.ids = ids, p.top = top, p.lse = lse, p.entropy = entropy;
+    constexpr int64_t MOST = 1 << 23;  // rows of a launch, which has less than 2^32 threads along an axis
+    if (T > MOST) {
+        for (int64_t r = 0; r < T; r += MOST) {
+            const int rc = launch_token_logprobs(p.X + r * ldl * (f32 ? 4 : 2), f32, T - r < MOST ? T - r : MOST, V, ldl, scale, tokens + (tokens ? r * n_tok : 0), n_tok, k,
+                                                 lp + (lp ? r * n_tok : 0), ids + (ids ? r * k : 0), top + (top ? r * k : 0), lse + (lse ? r : 0),
+                                                 entropy + (entropy ? r : 0), workspace, st);
+            if (rc) return rc;
+        }
+        return OSC_OK;
+    }
     const LogpShape shape = logprob_shape(T, V);
     p.splits = shape.splits;
     p.stats = reinterpret_cast<float4*>(workspace), p.keys = reinterpret_cast<uint64_t*>(workspace + (size_t)T * p.splits * 16);

@@ -230,3 +230,21 @@ def test_many_long_rows(osc, T, dtype):
             b = b.repeat(-(-T // 8), *[1] * (b.dim() - 1))[:T].double()
             assert ((a.double() - b).abs() <= 2 * (V / 4096 + 250) * u + 16 * u * b.abs()).all()
     check(osc, x[3:5], tok[3:5].cpu().numpy(), 20)
+
+
+def test_more_rows_than_a_launch_has(osc):
+    T, V = 2 ** 23 + 300, 4
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    X = torch.randint(-8, 9, (T, V), generator=g, device=DEV).bfloat16()
+    tokens = torch.randint(0, V, (T,), generator=g, device=DEV).int()
+    lp, ids, top, lse, entropy = osc.osc_token_logprobs(X, tokens, 2)
+    rows = torch.cat([torch.arange(0, 200), torch.arange(2 ** 23 - 200, T)]).to(DEV)
+    out = [torch.empty_like(v[rows]) for v in (lp, ids, top, lse, entropy)]
+    osc.osc_token_logprobs(X[rows], tokens[rows], 2, out=out)
+    for a, b in zip((lp, ids, top, lse, entropy), out):
+        assert torch.equal(a[rows], b)
+    check(osc, X[rows], tokens[rows].cpu().numpy(), 2)
+    want = torch.log_softmax(X.double(), 1).gather(1, tokens.long()[:, None])[:, 0]
+    # check()'s bound for V = 4 and logits 16 apart at most: A1 <= 32, 173 u a row and 99 u for the size of the result
+    assert (lp - want).abs().max() <= 300 * u

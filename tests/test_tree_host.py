@@ -182,3 +182,16 @@ def test_extents_past_32_bits():
     """overlap checks hold for pitches whose last element lies past 2^32 bytes, and past 2^64"""
     assert rc(ACCEPT, ch=8 * P, ldc=2 ** 31 - 1, T=2 ** 31 - 1, par=P) == UNSUPPORTED   # whatever is behind it is inside
     assert rc(MASK, T=2 ** 31 - 1, ldm=2 ** 30 - 1, pos=2 ** 40) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("change", [
+    dict(lp=100 * P), dict(lse=100 * P + 799996), dict(lp=P), dict(ids=P - 76), dict(top=3 * P + 76), dict(ent=5 * P + 12), dict(ws=2 * P), dict(tok=7 * P + 1532),
+    dict(dtype=1, T=3, V=1, ldl=2 ** 62, k=0, n=0, tok=None, lse=2 ** 50)])
+def test_logprobs_outputs_apart(change):
+    good = dict(x=100 * P, tok=P, lp=2 * P, ids=3 * P, top=4 * P, lse=5 * P, ent=6 * P, ws=7 * P)
+    assert rc(LOGP, **dict(good, **change)) == UNSUPPORTED and "overlaps" in osc.osc_last_error()
+
+
+@pytest.mark.parametrize("change", [dict(N=2 ** 26, T=2 ** 26, Hkv=1, offs=None), dict(N=2 ** 23, T=2 ** 23, Hkv=8, offs=None)])
+def test_move_of_too_many_groups(change):
+    assert rc(MOVE, **change) == UNSUPPORTED
