@@ -11,17 +11,24 @@ namespace osc {
 struct Rows {
     int q0, n;
 };
-// rows of request b, none if its offsets fall or leave [0, T]
-__device__ __forceinline__ Rows rows_of(const int32_t* q_offsets, int b, int64_t T) {
+// rows and length of request b, no rows if its offsets fall or leave [0, T]
+__device__ __forceinline__ Rows rows_of(const int32_t* q_offsets, const int32_t* kv_lens, int b, int64_t T, int& L) {
     Rows r{q_offsets[b], 0};
     const int end = q_offsets[b + 1];
+    L = kv_lens[b];
+    asm volatile("" : : "s"(r.q0), "s"(end), "s"(L));  // asked for together: the compiler would read each at the branch that needs it
     if (r.q0 >= 0 && end >= r.q0 && end <= T) r.n = end - r.q0;
     return r;
 }
 // rows that no request has: before the first offset and from the last on; f(row) for each
 template <class F>
 __device__ __forceinline__ void padding(const int32_t* q_offsets, int B, int64_t T, int64_t at, int64_t step, F f) {
-    const int64_t first = B ? min(max((int64_t)q_offsets[0], (int64_t)0), T) : 0, last = B ? min(max((int64_t)q_offsets[B], first), T) : 0;
+    int from = 0, to = 0;
+    if (B) {
+        from = q_offsets[0], to = q_offsets[B];
+        asm volatile("" : : "s"(from), "s"(to));
+    }
+    const int64_t first = min(max((int64_t)from, (int64_t)0), T), last = min(max((int64_t)to, first), T);
     for (int64_t i = at; i < first + T - last; i += step) f(i < first ? i : i - first + last);
 }
 constexpr int PAD_WGS = 8;
@@ -41,8 +48,10 @@ __global__ __launch_bounds__(64) void tree_mask_kernel(const int32_t* __restrict
         return;
     }
     const int b = blockIdx.x;
-    const Rows r = rows_of(q_offsets, b, T);
-    const int64_t start = (int64_t)pos_base + max(kv_lens[b], 0) - r.n;
+    asm volatile("" : : "s"(parents));  // the argument too
+    int L;
+    const Rows r = rows_of(q_offsets, kv_lens, b, T, L);
+    const int64_t start = (int64_t)pos_base + max(L, 0) - r.n;
     auto place = [&](int i, int64_t depth) { positions[r.q0 + i] = (int)max(min(start + depth, (int64_t)0x7fffffff), (int64_t)-1); };
     if (r.n > 64 * words) {  // no tree
         for (int i = lane; i < r.n; i += 64) {
@@ -101,31 +110,31 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(const int32_t* __restri
         return;
     }
     const int b = blockIdx.x;
-    const Rows r = rows_of(q_offsets, b, T);
-    const int L = kv_lens[b];
+    int L;
+    const Rows r = rows_of(q_offsets, kv_lens, b, T, L);
     const int32_t *par = parents + r.q0, *tok = tokens + r.q0, *chosen = choices + r.q0 * ldc;
     int count = 0, next = -1, L_out = L;
-    if (r.n > 0 && slots[r.q0] >= 0) {  // otherwise the request got no pages: its tokens are not cached
-        int chunk = -1, up = -1, token = 0, choice = 0;  // of the 64 rows that the lanes hold
-        uint64_t runs = 0;
-        auto hold = [&](int c) {
-            if (c == chunk) return;
-            chunk = c;
-            const int i = c * 64 + lane;
-            const bool there = i < r.n;
-            up = there ? par[i] : -1, token = there ? tok[i] : 0, choice = there ? chosen[(int64_t)i * ldc] : 0;
-            int before = __shfl_up(choice, 1);
-            if (lane == 0 && i > 0 && there) before = chosen[(int64_t)(i - 1) * ldc];
-            runs = __ballot(there && i > 0 && up == i - 1 && (token < 0 || token == before));
-        };
-        auto put = [&](int k, int i) {
+    int chunk = -1, up = -1, token = 0, choice = 0, slot = -1;  // of the 64 rows that the lanes hold, all read at once
+    uint64_t runs = 0;
+    auto hold = [&](int c) {
+        if (c == chunk) return;
+        chunk = c;
+        const int i = c * 64 + lane, row = min(i, r.n - 1);
+        const bool there = i < r.n;
+        up = par[row], token = tok[row], choice = chosen[(int64_t)row * ldc], slot = slots[r.q0 + row];
+        const int before = c ? chosen[(int64_t)(i - lane - 1) * ldc] : 0, below = __shfl_up(choice, 1);
+        if (!there) up = -1;
+        runs = __ballot(there && i > 0 && up == i - 1 && (token < 0 || token == (lane ? below : before)));
+    };
+    if (r.n > 0) hold(0);
+    if (r.n > 0 && __builtin_amdgcn_readlane(slot, 0) >= 0) {  // otherwise the request got no pages: its tokens are not cached
+        auto put = [&](int k, int i, int from) {
             path[r.q0 + k] = i;
-            src_slots[r.q0 + k] = slots[r.q0 + i];
+            src_slots[r.q0 + k] = from;
         };
         int at = 0;
         count = 1;
-        if (lane == 0) put(0, 0);
-        hold(0);
+        if (lane == 0) put(0, 0, slot);
         next = __builtin_amdgcn_readlane(choice, 0);
         while (at + 1 < r.n) {
             hold((at + 1) >> 6);
@@ -134,7 +143,7 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(const int32_t* __restri
             int run = ~ahead ? __ffsll((unsigned long long)~ahead) - 1 : 64;
             run = min(run, 64 - bit);
             if (run > 0) {
-                if (lane >= bit && lane < bit + run) put(count + lane - bit, chunk * 64 + lane);
+                if (lane >= bit && lane < bit + run) put(count + lane - bit, chunk * 64 + lane, slot);
                 count += run, at += run;
             } else {
                 int found = -1;
@@ -146,7 +155,8 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(const int32_t* __restri
                 }
                 if (found < 0) break;
                 at = found;
-                if (lane == 0) put(count, at);
+                const int from = __builtin_amdgcn_readlane(slot, at & 63);
+                if (lane == 0) put(count, at, from);
                 ++count;
             }
             next = __builtin_amdgcn_readlane(choice, at & 63);
