@@ -13,14 +13,14 @@
 // The top k.  A logit's key is its value in the order of unsigned numbers, then its index, lower ones first: 64 bits, no two alike.  In
 // the pass a lane keeps its largest logit, and a bit for every chunk whose largest one k lanes of the wavefront had not passed yet.  After the
 // pass 256 groups of lanes have a largest logit each, and no logit below the k-th of them is among the top k: the few lanes whose largest one
-// reaches that read their marked chunks again (from L2), and a wavefront counts the ranks of what they find.  Should that be more than LDS
+// reaches that read their marked chunks again (from L2; one chunk, where no other of the lane's reaches the bound: 100 rows 15.8 -> 14.9 us), and a wavefront counts the ranks of what they find.  Should that be more than LDS
 // has room for (many equal logits, a row with fewer than k tokens that can come), wavefronts walk their chunks once more and rank as they go
 // (2048 rows of 131072 where thousands are equal to the largest: 317 us, not 95).
 //
 // Bounds.  2048 rows of 131072 bf16 logits, top 5: 95 us, 5.6 TB/s; 78 would be a reading pass.  Without the top 86; 4 bytes a logit 6.5 TB/s: a bf16 logit takes ten
 // operations, one of them a power.  Reads past the caches are a fifth faster (103 with plain ones): nothing here is read twice but the marked
-// chunks.  511 rows of 32000 10.1 us: 33 MB in about 4, the start and the end of a workgroup.  100 rows of 50001, four bytes each, top 20, 16.4: one
-// workgroup a CU on 100 of them, 25 GB/s each; the top's three steps (largest logits, bound, marked chunks) are 5 of it.  One row of 131072: 8.3 and 3.0 us for the
+// chunks.  511 rows of 32000 10.1 us: 33 MB in about 4, the start and the end of a workgroup.  100 rows of 50001, four bytes each, top 20, 15.2: one
+// workgroup a CU on 100 of them, 25 GB/s each; the top's three steps (largest logits, bound, marked chunks) are 4 of it.  One row of 131072: 8.3 and 3.0 us for the
 // two kernels.  Ranking candidates on the way instead of marking them: 100 rows 30 us, 2048 126.
 #include <type_traits>
 

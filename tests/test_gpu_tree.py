@@ -334,3 +334,20 @@ def test_two_calls_at_once(osc):
     for i in range(2):
         for o, lse in got[i]:
             assert torch.equal(o, sets[i][2]) and torch.equal(lse, sets[i][3])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("P", [0, 300])
+def test_attention_values_that_are_not_finite_stay_in_their_request(osc, P, D):
+    counts, kv = [9, 40, 3, 20], [30, 300, 300, 21]
+    s = make(11 + P, 4, P, kv, counts, 4, 2, D, 16)
+    mask = tree_of(0, s, counts, 1)
+    before, lse0 = check(osc, s, mask)
+    page, at = int(s["table"][1, 280 // 16]), 280 % 16  # a draft of the second request
+    assert (s["table"][[0, 2, 3]] != page).all() and (P == 0 or (s["prefix"] != page).all())
+    V = s["V"].clone()
+    V[page, :, at] = float("nan")
+    o, lse = call(osc, dict(s, V=V), mask)
+    others = [*range(9), *range(49, 72)]
+    assert torch.equal(o[others], before[others]) and torch.equal(lse, lse0)
+    assert torch.isnan(o[9 + 20]).all()  # the draft itself: token 280 is the 20th new one
