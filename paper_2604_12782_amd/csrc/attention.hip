@@ -438,6 +438,7 @@ __device__ __forceinline__ void mask(v16f (&s)[N], int lane, int seen) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[u][e] = 32 * u + (e & 3) + 8 * (e >> 2) < left ? s[u][e] : -INFINITY;
 }
+__device__ __forceinline__ uint64_t first_bits(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0 : (1ull << n) - 1; }
 // Rows of a tree.  The tokens from j0 on that a row sees, as bits: all before the request's new ones, which start at `fresh`, then those
 // of the row's words, none from `seen` on.
 template <int N>
@@ -451,8 +452,7 @@ __device__ __forceinline__ uint64_t tree_bits(const AttnArgs& p, const uint64_t*
         w = at < p.words ? words[at] >> shift : 0;
         if (shift > 64 - 32 * N && at + 1 < p.words) w |= words[at + 1] << (64 - shift);
     }
-    const int left = seen - j0;
-    return left >= 64 ? w : left <= 0 ? 0 : w & ((1ull << left) - 1);
+    return w & first_bits(seen - j0);
 }
 template <int N>
 __device__ __forceinline__ void mask_tree(v16f (&s)[N], int lane, uint64_t bits) {
@@ -461,6 +461,49 @@ __device__ __forceinline__ void mask_tree(v16f (&s)[N], int lane, uint64_t bits)
     for (int u = 0; u < N; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[u][e] = (uint32_t)(bits >> 32 * u) >> ((e & 3) + 8 * (e >> 2)) & 1 ? s[u][e] : -INFINITY;
+}
+// Values that are not finite, of new tokens that some rows of a tile do not see: a weight of zero times them would be NaN.  So before a
+// block that is masked is used they are set to zero where they lie, and the sums of rows that do see such a token (`tokens`, bits) become NaN.
+// ROWS rows from `at`, which the wavefront has asked for itself: which of them, as bits.  (With this and without: 48 trees of 32 behind 4096 167 / 164 us, 6
+// of 97 96 / 94, 24 of 16 61.4 / 61.0, one of 8 the same.  Weights marked instead of sums cost the overlap of powers and products: 172; values of a product checked in
+// registers spill 200 of them.)
+template <int D, int ROWS>
+__device__ __forceinline__ uint32_t clear_values(uint32_t at, int lane) {
+    typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+    constexpr int LANES = D / 8, RPI = 64 / LANES, NI = ROWS / RPI;  // lanes a row, rows a read, reads
+    auto place = [&](int i) { return (__attribute__((address_space(3))) v4u*)(uintptr_t)(at + i * 1024 + lane * 16); };
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const v4u x = *place(i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) most = max_pair(most, x[k] & 0x7f807f80u);
+    }
+    if (__ballot((most & 0xffffu) == 0x7f80u || most >> 16 == 0x7f80u) == 0) return 0;
+    uint32_t found = 0;
+#pragma unroll 1
+    for (int i = 0; i < NI; ++i) {
+        v4u x = *place(i);
+        uint32_t any = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t bad = ((x[k] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((x[k] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+            any |= bad, x[k] &= ~bad;
+        }
+        if (any) *place(i) = x;
+        const uint64_t who = __ballot(any != 0);
+#pragma unroll
+        for (int r = 0; r < RPI; ++r) found |= (who >> r * LANES & ((1u << LANES) - 1) ? 1u : 0u) << (i * RPI + r);
+    }
+    return found;
+}
+// `seen`: tokens of the block that the lane's row sees, as bits; what the row has summed stays NaN
+template <int D>
+__device__ __forceinline__ void mark_sums(State<D>& st, uint64_t seen, uint64_t tokens) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st.o[d][e] = seen & tokens ? NAN : st.o[d][e];
 }
 template <int D, int N>
 __device__ __forceinline__ void weigh(State<D>& st, v16f (&s)[N], float c) {
@@ -713,6 +756,13 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
             if (j0 + 32 > (pre ? p.P : clear_to)) {
                 if (TREE && !pre && rq.n <= 64 * p.words) mask_tree<1>(s, lane, tree_bits<1>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j0));
                 else mask<1>(s, lane, (pre ? p.P : seen) - j0);
+                if (TREE && !pre) {
+                    if (more) wait_vmcnt<NI>();
+                    else wait_vmcnt<0>();
+                    lds_order();
+                    const uint32_t bad = clear_values<D, 32>(vt, lane);
+                    if (bad) mark_sums<D>(st, rq.n <= 64 * p.words ? tree_bits<1>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j0) : first_bits(seen - j0), bad);
+                }
             }
             weigh<D, 1>(st, s, p.c);
             if (more) wait_vmcnt<NI>();
@@ -741,7 +791,7 @@ __device__ __forceinline__ void narrow_piece(const AttnArgs& p, const Plan& plan
 // ---- a piece of the line of 128-row tiles -----------------------------------------------------------------------------------------
 // Every wavefront has 32 rows; all read the same 64 tokens from LDS, of which each has asked for 16, a block ahead.
 template <int D, bool TREE>
-__device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, int w) {
+__device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, const Sums& sums, uint8_t* lds, uint32_t (&bad)[2][4], int w) {
     constexpr int TILE = 64 * D * 2;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // what follows from it is made here, not kept in registers from the kernel's start
@@ -796,7 +846,8 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             const int edge = EDGE >> p.ws;
             return y >= length ? blocks : min(blocks, (int)((float)max(y - edge, 0) * (float)blocks / (float)(length - edge)));
         };
-        const int k0 = block_at(x - start), k1 = block_at(stop - start);
+        int k0 = block_at(x - start), k1 = block_at(stop - start);
+        if (TREE) k0 = uni(k0), k1 = uni(k1);
         const bool whole = x == start && stop == start + length;
         if (b >= 0) slot = (2 * (int64_t)w + (x == start)) * 4;
 
@@ -842,8 +893,16 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
             fetch(k0, page_of(k0));
             if (k0 + 1 < k1) page = page_of(k0 + 1);
         }
+        // Trees: blocks from `checked` on have tokens that some rows of the tile do not see, `part` is the prefix's last block where it is not full.
+        const int part = TREE && (p.P & 63) ? uni(plan.nbp - 1 - first_block) : -1;
+        const int checked = TREE && b >= 0 ? uni(n_prefix + (max(rq.L - rq.n + (tree ? 0 : t_base), 0) >> 6)) : 0x7fffffff;
         auto next = [&](int k) {
             wait_vmcnt<0>();
+            if (TREE && k >= checked) {
+                lds_order();
+                const uint32_t found = clear_values<D, 16>(lds_at(lds) + (k & 1) * 2 * TILE + TILE + wave * (16 * D * 2), lane);
+                if (lane == 0) bad[k & 1][wave] = found;
+            }
             __syncthreads();  // everyone's part of block k is there, and everyone is done with block k - 1
             if (k + 1 < k1) {
                 fetch(k + 1, page);
@@ -865,9 +924,14 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
                 scores<D, 2>(s, q, buffer + kl);
                 Values<D> f;  // on their way while the weights are made
                 read_values<D>(f, buffer + TILE + vl, 0);
-                if (j0 + 64 > (pre ? p.P : clear_to)) {
+                if (TREE ? (int)(k >= checked) | (int)(k == part) : j0 + 64 > (pre ? p.P : clear_to)) {
                     if (tree && !pre) mask_tree<2>(s, lane, tree_bits<2>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j0));
                     else mask<2>(s, lane, (pre ? p.P : seen) - j0);
+                    if (TREE && !pre) {
+                        const uint32_t* at = bad[k & 1];
+                        const uint64_t tokens = (uint64_t)(uint32_t)uni(at[2] | at[3] << 16) << 32 | (uint32_t)uni(at[0] | at[1] << 16);
+                        if (tokens) mark_sums<D>(st, tree ? tree_bits<2>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j0) : first_bits(seen - j0), tokens);
+                    }
                 }
                 weigh<D, 2>(st, s, p.c);
                 gather<D, 2>(st, s, f, buffer + TILE + vl);
@@ -889,6 +953,7 @@ struct AttnShared {
     Sums sums;
     int part[4][11];
     float stats[256];
+    uint32_t bad[2][4];
 };
 
 template <int D, bool TREE>
@@ -984,7 +1049,7 @@ __global__ __launch_bounds__(WG, D == 128 ? 2 : 3) void prefix_attention_kernel(
         if ((turn == 0) == swap) {
             narrow_piece<D, TREE>(p, plan, sums, lds, sh.stats);
             if (turn == 0 && with_wide) lds_barrier();  // the tiles of both are in the same place
-        } else if (with_wide) wide_piece<D, TREE>(p, plan, sums, lds, xcd * run + i);
+        } else if (with_wide) wide_piece<D, TREE>(p, plan, sums, lds, sh.bad, xcd * run + i);
     }
 }
 

@@ -338,16 +338,52 @@ def test_two_calls_at_once(osc):
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("P", [0, 300])
-def test_attention_values_that_are_not_finite_stay_in_their_request(osc, P, D):
-    counts, kv = [9, 40, 3, 20], [30, 300, 300, 21]
-    s = make(11 + P, 4, P, kv, counts, 4, 2, D, 16)
+@pytest.mark.parametrize("what,bad", [("V", float("nan")), ("V", float("inf")), ("K", float("nan")), ("V", float("-inf"))])
+def test_attention_of_drafts_that_are_not_finite(osc, what, bad, P, D):
+    """rows that see such a draft are NaN in its head, all others what they were: requests of few rows, of more, of two tiles, a piece of a prompt"""
+    counts, kv = [9, 40, 60, 20, 100, 16], [30, 300, 461, 21, 130, 16]
+    s = make(11 + P, 6, P, kv, counts, 4, 2, D, 16)
     mask = tree_of(0, s, counts, 1)
     before, lse0 = check(osc, s, mask)
-    page, at = int(s["table"][1, 280 // 16]), 280 % 16  # a draft of the second request
-    assert (s["table"][[0, 2, 3]] != page).all() and (P == 0 or (s["prefix"] != page).all())
-    V = s["V"].clone()
-    V[page, :, at] = float("nan")
-    o, lse = call(osc, dict(s, V=V), mask)
-    others = [*range(9), *range(49, 72)]
-    assert torch.equal(o[others], before[others]) and torch.equal(lse, lse0)
-    assert torch.isnan(o[9 + 20]).all()  # the draft itself: token 280 is the 20th new one
+    bits, offs = words_of(mask)[:, 0], np.concatenate([[0], np.cumsum(counts)])
+    for b, draft, h in ((0, 3, 1), (1, 17, 0), (2, 40, 1), (3, 19, 0), (4, 70, 1), (5, 0, 0), (2, 59, 0)):
+        j = kv[b] - counts[b] + draft
+        page = int(s["table"][b, j // 16])
+        T = s[what].clone()
+        T[page, h, j % 16, 5 if what == "V" and b % 2 else slice(None)] = bad
+        o, lse = call(osc, dict(s, **{what: T}), mask)
+        sees = np.zeros((sum(counts), 4), bool)
+        for i in range(counts[b]):
+            r = offs[b] + i
+            sees[r, 2 * h:2 * h + 2] = i >= draft if counts[b] > 64 else bits[r] >> np.uint64(draft) & np.uint64(1)
+        assert sees.any()
+        sees = torch.from_numpy(sees).to(DEV)
+        got, was = o.view(-1, 4, D), before.view(-1, 4, D)
+        hit = torch.isnan(got)  # a prompt's later rows see a value in its channel alone
+        assert torch.equal(hit[:, :, 5] if what == "V" else hit.all(-1), sees) and torch.equal(hit.any(-1), sees)
+        assert torch.equal(got[~sees], was[~sees])
+        if what == "V":
+            assert torch.equal(lse, lse0)
+        else:
+            assert torch.equal(torch.isnan(lse), sees) and torch.equal(lse[~sees], lse0[~sees])
+
+
+def test_attention_of_drafts_that_are_not_finite_in_long_requests(osc):
+    """the same where the new tokens are in several blocks, words and pieces of a request"""
+    counts, kv = [97, 5, 300], [5000, 40, 320]
+    s = make(3, 3, 0, kv, counts, 6, 2, 64, 32)
+    mask = tree_of(1, s, counts, 2)
+    before, lse0 = check(osc, s, mask)
+    bits = words_of(mask)
+    for b, draft in ((0, 2), (0, 63), (0, 64), (0, 96), (2, 0), (2, 150), (2, 299)):
+        j, at = kv[b] - counts[b] + draft, [0, 97, 102][b]
+        V = s["V"].clone()
+        V[int(s["table"][b, j // 32]), 1, j % 32] = float("nan")
+        o, lse = call(osc, dict(s, V=V), mask)
+        sees = np.zeros((402, 6), bool)
+        for i in range(counts[b]):
+            sees[at + i, 3:] = i >= draft if b == 2 else bits[at + i, draft // 64] >> np.uint64(draft % 64) & np.uint64(1)
+        sees = torch.from_numpy(sees).to(DEV)
+        got, was = o.view(-1, 6, 64), before.view(-1, 6, 64)
+        assert torch.equal(torch.isnan(got).all(-1), sees) and torch.equal(torch.isnan(got).any(-1), sees)
+        assert torch.equal(got[~sees], was[~sees]) and torch.equal(lse, lse0)
