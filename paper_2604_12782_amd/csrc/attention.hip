@@ -464,9 +464,9 @@ __device__ __forceinline__ void mask_tree(v16f (&s)[N], int lane, uint64_t bits)
 }
 // Values that are not finite, of new tokens that some rows of a tile do not see: a weight of zero times them would be NaN.  So before a
 // block that is masked is used they are set to zero where they lie, and the sums of rows that do see such a token (`tokens`, bits) become NaN.
-// ROWS rows from `at`, which the wavefront has asked for itself: which of them, as bits.  (With this and without: 48 trees of 32 behind 4096 167 / 164 us, 6
-// of 97 96 / 94, 24 of 16 61.4 / 61.0, one of 8 the same.  Weights marked instead of sums cost the overlap of powers and products: 172; values of a product checked in
-// registers spill 200 of them.)
+// ROWS rows from `at`, which the wavefront has asked for itself: which of them, as bits.  (With this and without: 48 trees of 32 behind 4096 166.1 / 165.2 us, 6
+// of 97 97.9 / 97.8, 24 of 16 61.5 / 61.1, one of 8 19.2 / 19.0.  Weights marked instead of sums cost the overlap of powers and products: 172; values of a
+// product checked in registers spill 200 of them.)
 template <int D, int ROWS>
 __device__ __forceinline__ uint32_t clear_values(uint32_t at, int lane) {
     typedef uint32_t v4u __attribute__((ext_vector_type(4)));
@@ -925,13 +925,16 @@ __device__ __forceinline__ void wide_piece(const AttnArgs& p, const Plan& plan, 
                 Values<D> f;  // on their way while the weights are made
                 read_values<D>(f, buffer + TILE + vl, 0);
                 if (TREE ? (int)(k >= checked) | (int)(k == part) : j0 + 64 > (pre ? p.P : clear_to)) {
-                    if (tree && !pre) mask_tree<2>(s, lane, tree_bits<2>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j0));
-                    else mask<2>(s, lane, (pre ? p.P : seen) - j0);
+                    auto visible = [&](int j) { return tree && !pre ? tree_bits<2>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j) : first_bits((pre ? p.P : seen) - j); };
                     if (TREE && !pre) {
                         const uint32_t* at = bad[k & 1];
                         const uint64_t tokens = (uint64_t)(uint32_t)uni(at[2] | at[3] << 16) << 32 | (uint32_t)uni(at[0] | at[1] << 16);
-                        if (tokens) mark_sums<D>(st, tree ? tree_bits<2>(p, p.mask + ti * p.ldm, rq.L - rq.n, seen, j0) : first_bits(seen - j0), tokens);
+                        int j = j0;
+                        asm volatile("" : "+s"(j));  // bits are made anew below: they would be held in registers over all of this
+                        if (tokens) mark_sums<D>(st, visible(j), tokens);
                     }
+                    if (TREE) mask_tree<2>(s, lane, visible(j0));
+                    else mask<2>(s, lane, (pre ? p.P : seen) - j0);
                 }
                 weigh<D, 2>(st, s, p.c);
                 gather<D, 2>(st, s, f, buffer + TILE + vl);
