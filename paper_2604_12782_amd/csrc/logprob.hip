@@ -7,8 +7,9 @@
 // The base is the lane's first chunk's largest logit and follows only when a chunk's weights reach 2^8, so sums are rarely scaled; a change of
 // base by d = B - B' turns (S, U) into 2^d (S, U + S d), which is also how lanes, wavefronts and parts of a row are joined.  Then log p_j
 // = scale (x_j - b) - log S and the entropy is log S - ln 2 U / S; logits enter by their distance from the base alone, so large
-// ones lose nothing.  Everything is single precision.  Where c b itself would overflow (a row of the type's lowest value) powers are made of
-// c (x_j - b).
+// ones lose nothing.  Everything is single precision.  B is rounded by up to half its last place, and the base's own weight is 2 to that:
+// 2^-5 at 2^20, but 64 at 1e9 and infinite or 0 beyond 1e10.  So from LP_FAR on (fills for tokens that may not come, rows of large logits) powers are
+// made of c (x_j - b), relative to c b itself, and the usual path is left.
 //
 // The top k.  A logit's key is its value in the order of unsigned numbers, then its index, lower ones first: 64 bits, no two alike.  In
 // the pass a lane keeps its largest logit, and a bit for every chunk whose largest one k lanes of the wavefront had not passed yet.  After the
@@ -44,18 +45,21 @@ struct LogpArgs {
 
 constexpr int LP_BUF = 128, LP_MAX_SPLITS = 64, LP_FOUND = 512;
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
-constexpr float LP_HUGE = 0x1p126f, LN2 = 0.69314718055994531f;
+constexpr float LP_FAR = 0x1p20f, LN2 = 0.69314718055994531f;
 
 struct Weights {
     float b, S, U;
 };
-// turned to base nb >= b; nothing seen is b = -infinity, S = U = 0
+__device__ __forceinline__ bool is_far(float B) { return !(fabsf(B) < LP_FAR); }
+// turned to base nb >= b; nothing seen is b = -infinity, S = U = 0.  Weights are relative to 2^B, of a far base to 2^(c b): d is the difference of the
+// two as they are, in one rounding each.
 __device__ __forceinline__ void rebase(Weights& w, float nb, float c) {
 #pragma clang fp contract(off)  // products are rounded before their difference, as B is
     if (w.b == -INFINITY) {
         w.S *= nb == INFINITY ? NAN : 0.0f, w.U = 0.0f;  // 0 stays 0, NaN stays NaN
     } else {
-        const float from = w.b * c, to = nb * c, d = fmaxf(fmaxf(fabsf(from), fabsf(to)) < LP_HUGE ? from - to : (w.b - nb) * c, -1e4f);
+        const float from = w.b * c, to = nb * c;
+        const float d = fmaxf(is_far(from) ? is_far(to) ? (w.b - nb) * c : fmaf(w.b, c, -to) : is_far(to) ? fmaf(-nb, c, from) : from - to, -1e4f);
         const float f = __builtin_amdgcn_exp2f(d);
         w.U = (w.U + w.S * d) * f;
         w.S *= f;
@@ -180,7 +184,7 @@ __device__ __forceinline__ float given_logit(const LogpArgs& p, const uint8_t* x
 template <bool F32>
 __device__ __forceinline__ void finish(const LogpArgs& p, int64_t row, const Weights& w, const uint64_t* sorted, int lane, const uint8_t* x, int32_t token, float its) {
     const bool bad = !(w.S < INFINITY) || w.b == INFINITY;  // NaN or infinity among the logits
-    const float B = w.b * p.c, off = fabsf(B) < LP_HUGE ? fmaf(w.b, p.c, -B) : 0.0f;
+    const float B = w.b * p.c, off = is_far(B) ? 0.0f : fmaf(w.b, p.c, -B);
     const float logS = logf(w.S), logZ = logS - off * LN2;  // of the powers of c (x - b)
     auto log_p = [&](float v) { return bad ? NAN : w.S > 0.0f ? p.scale * (v - w.b) - logZ : -INFINITY; };
     if (lane == 0) {
@@ -278,7 +282,7 @@ __global__ __launch_bounds__(64 * WAVES, NV == 2 ? 8 : 4) void token_logprobs_ke
     Weights w{-INFINITY, 0.0f, 0.0f};
     const float c = p.c;
     const int shift = rounds > 64 ? 26 - __builtin_clz(rounds - 1) : 0;  // 2^shift rounds a bit
-    bool usual = false;  // every lane has a base, and c times it is an ordinary number
+    bool usual = false;  // every lane has a base, and none a far one
     float B = 0.0f, mine = -INFINITY, second = -INFINITY, passed = -INFINITY;  // chunks' largest logits, the best two; passed: k lanes of the wavefront have reached it
     int best_it = 0;
     uint64_t marks = 0;
@@ -322,12 +326,12 @@ __global__ __launch_bounds__(64 * WAVES, NV == 2 ? 8 : 4) void token_logprobs_ke
             if (nb > w.b) rebase(w, nb, c);
             const float b = w.b == -INFINITY ? 0.0f : w.b;
             B = __fmul_rn(b, c);
-            const bool huge = !(fabsf(B) < LP_HUGE);
-            usual = __ballot(w.b == -INFINITY || huge) == 0;
+            const bool far = is_far(B);
+            usual = __ballot(w.b == -INFINITY || far) == 0;
             s = u = 0.0f;
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
-                const float y = huge ? (v[e] - b) * c : fmaf(v[e], c, -B), g = __builtin_amdgcn_exp2f(y);
+                const float y = far ? (v[e] - b) * c : fmaf(v[e], c, -B), g = __builtin_amdgcn_exp2f(y);
                 s += g;
                 u = fmaf(g, fmaxf(y, -1e3f), u);  // 0 times -infinity counts as 0
             }

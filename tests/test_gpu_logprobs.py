@@ -248,3 +248,49 @@ def test_more_rows_than_a_launch_has(osc):
     want = torch.log_softmax(X.double(), 1).gather(1, tokens.long()[:, None])[:, 0]
     # check()'s bound for V = 4 and logits 16 apart at most: A1 <= 32, 173 u a row and 99 u for the size of the result
     assert (lp - want).abs().max() <= 300 * u
+
+
+def far_rows(V, dtype, scale):
+    """rows of ordinary logits with fills at any distance, rows of large logits alone, rows on both sides of where c x is 2^20"""
+    inf, low = float("inf"), torch.finfo(dtype).min
+    rows, x = [], logits(8, 1, V, dtype)[0].clone()
+    for fill in (-1e4, -1e9, -1e10, -1e12, -1e15, -1e20, -1e30, low, -inf):
+        for i, part in enumerate((slice(5, None), slice(None, V - 1), slice(None), slice(100, V - 100), slice(None, None, 2), slice(None, V // 2), slice(V // 2, None), slice(7, 8))):
+            r = x.roll(i)
+            r[part] = fill
+            rows.append(r)
+        r = torch.full_like(x, fill)  # two tokens that can come
+        r[[3, V // 2]] = 3.0
+        rows.append(r)
+    for v in (1e6, 1e9, 1e10, 1e15, 1e20, 1e30, 1e37):
+        rows += [torch.full_like(x, v), torch.full_like(x, -v)]
+        for a in (v, -v, 1.5 * v):
+            r = x.clone()
+            r[V // 3] = a
+            rows.append(r)
+        r = torch.full_like(x, -v)
+        r[::3], r[1::5] = v, 0.0
+        rows.append(r)
+    line = 2.0 ** 20 * np.log(2) / scale
+    for at in (line, -line):
+        g = torch.Generator().manual_seed(int(scale * 10))
+        near = (at + torch.randn(V, generator=g) * 2 / scale).to(dtype).to(DEV)
+        rows += [near, torch.cat([near[:V // 2] * 1.25, near[V // 2:]]), torch.cat([near[:V // 2] * 0.75, near[V // 2:]]), torch.where(torch.arange(V, device=DEV) % 64 < 32, near, near * 0.999)]
+    return torch.stack(rows)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [0.7, 1.0, 1.6, 3.0])
+def test_far_logits(osc, dtype, scale):
+    """logits are as good as their distance from the row's largest one, however far all of them are from 0: rows in parts, and of every number of wavefronts"""
+    V = 33003
+    x = far_rows(V, dtype, scale)
+    tok = lambda n: [[0, 3, V // 2, V - 1]] * n
+    check(osc, x, tok(len(x)), 5, scale=scale)
+    for r in range(0, len(x), 12):
+        check(osc, x[r:r + 12], tok(len(x[r:r + 12])), 5, scale=scale)
+    x = far_rows(5001, dtype, scale)
+    tok = [[0, 3, 2500, 5000]]
+    for T in (300, 700, 1100):
+        many = torch.cat([x, logits(T, T - len(x), 5001, dtype)])
+        check(osc, many, tok * T, 64 if T == 700 else 0, scale=scale)
