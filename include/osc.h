@@ -592,7 +592,8 @@ int osc_page_free(const int32_t *kv_lens, const int32_t *new_lens, int32_t B, in
  *   lse        float [T] or NULL: log sum_i exp(scale x_i)
  *   entropy    float [T] or NULL: -sum_j p_j log p_j
  * -infinity is a token that cannot come; a row of nothing else gives lse and log probabilities -infinity, entropy 0.  A row
- * with NaN or +infinity gives NaN everywhere and ids -1.  Sums are single precision.
+ * with NaN or +infinity gives NaN everywhere and ids -1.  Sums are single precision; finite logits may be as far from 0 and from one another as
+ * their type allows, and a result is infinite only where its value is past single precision's range.
  *   logits     float or bf16 (dtype OSC_DT_F32, OSC_DT_BF16) [T, ldl], ldl >= V >= 1; rows need no alignment but that of an element
  *   top_k      0 to 64, at most V;  scale > 0 (1 / temperature)
  *   workspace  osc_token_logprobs_workspace_bytes(T, V, top_k) bytes, 256-byte aligned (NULL where that is 0); contents do not matter and

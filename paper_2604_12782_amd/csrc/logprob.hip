@@ -186,7 +186,10 @@ __device__ __forceinline__ void finish(const LogpArgs& p, int64_t row, const Wei
     const bool bad = !(w.S < INFINITY) || w.b == INFINITY;  // NaN or infinity among the logits
     const float B = w.b * p.c, off = is_far(B) ? 0.0f : fmaf(w.b, p.c, -B);
     const float logS = logf(w.S), logZ = logS - off * LN2;  // of the powers of c (x - b)
-    auto log_p = [&](float v) { return bad ? NAN : w.S > 0.0f ? p.scale * (v - w.b) - logZ : -INFINITY; };
+    auto log_p = [&](float v) {
+        const float far = v - w.b, d = far == -INFINITY && v > -INFINITY ? fmaf(p.scale, v, -(p.scale * w.b)) : p.scale * far;  // a distance past the type's range, times scale perhaps inside it
+        return bad ? NAN : w.S > 0.0f ? d - logZ : -INFINITY;
+    };
     if (lane == 0) {
         if (p.lse) p.lse[row] = bad ? NAN : w.S > 0.0f ? fmaf(p.scale, w.b, logZ) : -INFINITY;
         if (p.entropy) p.entropy[row] = bad ? NAN : w.S > 0.0f ? logS - w.U / w.S * LN2 : 0.0f;

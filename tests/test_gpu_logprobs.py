@@ -294,3 +294,30 @@ def test_far_logits(osc, dtype, scale):
     for T in (300, 700, 1100):
         many = torch.cat([x, logits(T, T - len(x), 5001, dtype)])
         check(osc, many, tok * T, 64 if T == 700 else 0, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [1e-38, 0.01, 0.3, 0.5, 1.0, 2.0])
+def test_distances_past_the_types_range(osc, dtype, scale):
+    """logits further apart than the type's largest number: their log probabilities are numbers where scale makes them so"""
+    x = logits(4, 6, 3001, dtype).clone()
+    top = torch.finfo(dtype).max
+    x[0, 5], x[0, 6] = 3e38, -3e38
+    x[1, 5], x[1, 6] = top, -top
+    x[2] = -top
+    x[2, 9], x[2, 6] = 2e38, -1e38
+    x[3, 5], x[3, 6] = 3e38, -float("inf")
+    x[4, 6] = -top
+    tok = i32([[0, 5, 6, 9]] * 6)
+    past = scale * x.double().max(1).values >= 2.0 ** 128  # their lse is infinity in single precision: 2 * 2e38 and more
+    assert past.any() == (scale == 2.0)
+    for k in (0, 64):
+        check(osc, x[~past], tok[~past].cpu().numpy(), k, scale=scale)
+        lp, ids, top, lse, ent = osc.osc_token_logprobs(x, tok, k, scale)
+        want = scale * (x.double() - x.double().max(1, keepdim=True).values)  # a single token: 0, and no other above -2^128
+        assert torch.isposinf(lse[past]).all() and (ent[past] == 0).all()
+        for got, at in ((lp, tok), (top, ids)) if k else ((lp, tok),):
+            w = want.gather(1, at.long())[past]
+            assert ((w == 0) | (w < -2.0 ** 128)).all() and torch.equal(got[past], torch.where(w == 0, 0.0, -float("inf")).float())
+    if not past.any():
+        check(osc, x[:2, 4:7], [[0, 1, 2]] * 2, 3, scale=scale)
