@@ -496,33 +496,30 @@ size_t token_logprobs_workspace(int64_t T, int64_t V, int32_t k) {
 int launch_token_logprobs(const void* X, bool f32, int64_t T, int64_t V, int64_t ldl, float scale, const int32_t* tokens, int32_t n_tok, int32_t k, float* lp,
                           int32_t* ids, float* top, float* lse, float* entropy, uint8_t* workspace, hipStream_t st) {
     LogpArgs p;
-    p.X = static_cast<const uint8_t*>(X), p.T = T, p.V = V, p.ldl = ldl, p.scale = scale, p.c = scale * 1.44269504088896341f;
-    p.tokens = tokens, p.n_tok = n_tok, p.k = k, p.lp = lp, p.ids = ids, p.top = top, p.lse = lse, p.entropy = entropy;
-    constexpr int64_t MOST = 1 << 23;  // rows of a launch, which has less than 2^32 threads along an axis
-    if (T > MOST) {
-        for (int64_t r = 0; r < T; r += MOST) {
-            const int rc = launch_token_logprobs(p.X + r * ldl * (f32 ? 4 : 2), f32, T - r < MOST ? T - r : MOST, V, ldl, scale, tokens + (tokens ? r * n_tok : 0), n_tok, k,
-                                                 lp + (lp ? r * n_tok : 0), ids + (ids ? r * k : 0), top + (top ? r * k : 0), lse + (lse ? r : 0),
-                                                 entropy + (entropy ? r : 0), workspace, st);
-            if (rc) return rc;
-        }
-        return OSC_OK;
-    }
-    const LogpShape shape = logprob_shape(T, V);
+    p.V = V, p.ldl = ldl, p.scale = scale, p.c = scale * 1.44269504088896341f, p.n_tok = n_tok, p.k = k;
+    const LogpShape shape = logprob_shape(T, V);  // of the whole call, as its workspace
     p.splits = shape.splits;
     p.stats = reinterpret_cast<float4*>(workspace), p.keys = reinterpret_cast<uint64_t*>(workspace + (size_t)T * p.splits * 16);
     auto go = [&](auto f, auto t) {
         constexpr bool F32 = decltype(f)::value, TOP = decltype(t)::value;
-        const dim3 grid = p.splits == 1 ? dim3((unsigned)T) : dim3((unsigned)p.splits, (unsigned)T);
+        const dim3 grid = p.splits == 1 ? dim3((unsigned)p.T) : dim3((unsigned)p.splits, (unsigned)p.T);
         if (shape.waves == 4) token_logprobs_kernel<F32, TOP, 4, 2><<<grid, 256, 0, st>>>(p);
         else if (shape.waves == 8) token_logprobs_kernel<F32, TOP, 8, 2><<<grid, 512, 0, st>>>(p);
         else if (T > 256 || p.splits > 1) token_logprobs_kernel<F32, TOP, 16, 2><<<grid, 1024, 0, st>>>(p);
         else token_logprobs_kernel<F32, TOP, 16, 4><<<grid, 1024, 0, st>>>(p);
-        if (p.splits > 1) token_logprobs_join_kernel<F32, TOP><<<dim3((unsigned)T), 64, 0, st>>>(p);
+        if (p.splits > 1) token_logprobs_join_kernel<F32, TOP><<<dim3((unsigned)p.T), 64, 0, st>>>(p);
     };
     auto by_top = [&](auto f) { k ? go(f, std::true_type()) : go(f, std::false_type()); };
-    f32 ? by_top(std::true_type()) : by_top(std::false_type());
-    return check_launch("osc_token_logprobs");
+    constexpr int64_t MOST = 1 << 23;  // rows of a launch, which has less than 2^32 threads along an axis; calls of as many are not split
+    for (int64_t r = 0; r < T; r += MOST) {
+        p.X = static_cast<const uint8_t*>(X) + r * ldl * (f32 ? 4 : 2), p.T = T - r < MOST ? T - r : MOST;
+        p.tokens = tokens + (tokens ? r * n_tok : 0), p.lp = lp + (lp ? r * n_tok : 0), p.ids = ids + (ids ? r * k : 0), p.top = top + (top ? r * k : 0);
+        p.lse = lse + (lse ? r : 0), p.entropy = entropy + (entropy ? r : 0);
+        f32 ? by_top(std::true_type()) : by_top(std::false_type());
+        const int rc = check_launch("osc_token_logprobs");
+        if (rc) return rc;
+    }
+    return OSC_OK;
 }
 
 }  // namespace osc

@@ -195,3 +195,55 @@ def test_logprobs_outputs_apart(change):
 @pytest.mark.parametrize("change", [dict(N=2 ** 26, T=2 ** 26, Hkv=1, offs=None), dict(N=2 ** 23, T=2 ** 23, Hkv=8, offs=None)])
 def test_move_of_too_many_groups(change):
     assert rc(MOVE, **change) == UNSUPPORTED
+
+
+LAUNCHES = r"""
+/* the runtime's calls around a launch: what was to be launched is written down, nothing runs */
+#include <stddef.h>
+typedef struct { unsigned x, y, z; } dim;
+int launches = 0;
+unsigned grids[64][3], blocks[64];
+static dim grid, block;
+int __hipPushCallConfiguration(dim g, dim b, size_t lds, void *stream) { grid = g, block = b; return 0; }
+int __hipPopCallConfiguration(dim *g, dim *b, size_t *lds, void **stream) { *g = grid, *b = block, *lds = 0, *stream = NULL; return 0; }
+int hipLaunchKernel(const void *f, dim g, dim b, void **args, size_t lds, void *stream) {
+    if (launches < 64) grids[launches][0] = g.x, grids[launches][1] = g.y, grids[launches][2] = g.z, blocks[launches] = b.x;
+    ++launches;
+    return 0;
+}
+int hipGetLastError(void) { return 0; }
+"""
+LAUNCHES_CHILD = r"""
+import ctypes as C, sys
+stub = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+lib = C.CDLL(sys.argv[2])
+lib.osc_token_logprobs_workspace_bytes.restype = C.c_size_t
+vp, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+P = 1 << 62
+for T, V, k in ((1 << 23, 131072, 5), ((1 << 23) + 1, 131072, 5), ((1 << 23) + 60, 40000, 3), ((2 << 23) + 128, 200000, 0)):
+    need = lib.osc_token_logprobs_workspace_bytes(i64(T), i64(V), i32(k))
+    at = C.c_int.in_dll(stub, "launches")
+    at.value = 0
+    rc = lib.osc_token_logprobs(vp(1 << 20), 1, i64(T), i64(V), i64(V), C.c_float(1.0), None, i32(0), i32(k), None, vp(P), vp(P + (1 << 58)), vp(P + (2 << 58)), None,
+                                None, C.c_size_t(0), None)
+    grids = (C.c_uint * 3 * 64).in_dll(stub, "grids")
+    blocks = (C.c_uint * 64).in_dll(stub, "blocks")
+    print(T, need, rc, [(grids[i][0], grids[i][1], blocks[i]) for i in range(at.value)])
+"""
+
+
+def test_rows_of_several_launches_need_no_workspace(tmp_path):
+    """a call's rows past 2^23 are launched as the others are: whole rows, no second kernel, nothing of a workspace that the call does not ask for"""
+    import ast
+    import subprocess
+    import sys
+    src, so = tmp_path / "launches.c", tmp_path / "launches.so"
+    src.write_text(LAUNCHES)
+    subprocess.run(["gcc", "-shared", "-fPIC", "-O1", str(src), "-o", str(so)], check=True)
+    p = subprocess.run([sys.executable, "-c", LAUNCHES_CHILD, str(so), osc.lib_path()], capture_output=True, text=True, timeout=120)
+    assert p.returncode == 0, p.stderr[-2000:]
+    lines = [l.split(maxsplit=3) for l in p.stdout.splitlines()]
+    assert len(lines) == 4
+    for T, need, code, launched in lines:
+        rows = [min(2 ** 23, int(T) - r) for r in range(0, int(T), 2 ** 23)]
+        assert need == "0" and code == "0" and ast.literal_eval(launched) == [(n, 1, 256) for n in rows], (T, launched)
