@@ -539,7 +539,7 @@ int osc_tree_accept(const int32_t *parents, const int32_t *tokens, const int32_t
  *              D 64 or 128
  *   src_slots, dst_slots  int32 [T]; a pair with a slot outside the cache (-1), or with the same slot twice, moves nothing
  *   offsets    int32 [N + 1]: pairs offsets[g] .. offsets[g+1] - 1 are a group (one that leaves [0, T] is left out); NULL: N groups of T / N pairs.
- *              N * Hkv < 2^26
+ *              N * Hkv <= 2^26 - 4
  * Groups are moved at the same time, pairs of a group in order: a slot may be written after it was read in the same group (tokens moved
  * towards a sequence's start), but not read or written again after it was written, nor be in two groups if one of them writes it.
  * Errors: OSC_ERR_NULL, OSC_ERR_SHAPE, OSC_ERR_UNSUPPORTED, OSC_ERR_HIP.

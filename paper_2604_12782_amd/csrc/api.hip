@@ -924,8 +924,8 @@ int osc_cache_move(void* Kc, void* Vc, int32_t n_layers, int64_t layer_stride, i
     REQUIRE(n_layers >= 0 && N >= 0 && T >= 0 && (n_layers <= 1 || layer_stride >= (n_pages * Hkv << lg) * D), OSC_ERR_SHAPE,
             "%s: n_layers=%d layer_stride=%lld N=%d T=%lld", who, n_layers, (long long)layer_stride, N, (long long)T);
     REQUIRE(layer_stride % 8 == 0 || n_layers <= 1, OSC_ERR_UNSUPPORTED, "%s: layers must be 16-byte aligned", who);
-    REQUIRE(n_layers <= 32767 && T <= 0x7fffffff && (int64_t)N * Hkv < 1 << 26, OSC_ERR_UNSUPPORTED,  // a launch has less than 2^32 threads along an axis
-            "%s: n_layers=%d N=%d T=%lld (at most 32767 layers, 2^31-1 pairs; heads of groups below 2^26)", who, n_layers, N, (long long)T);
+    REQUIRE(n_layers <= 32767 && T <= 0x7fffffff && (int64_t)N * Hkv <= (1 << 26) - 4, OSC_ERR_UNSUPPORTED,  // four in 256 threads, and a launch has less than 2^32 along an axis
+            "%s: n_layers=%d N=%d T=%lld (at most 32767 layers, 2^31-1 pairs, 2^26-4 heads of groups)", who, n_layers, N, (long long)T);
     REQUIRE(offsets || N == 0 || T % N == 0, OSC_ERR_SHAPE, "%s: %lld pairs are not %d groups of the same size, and there are no offsets", who, (long long)T, N);
     if (N == 0 || T == 0 || n_layers == 0 || n_pages == 0) return OSC_OK;
     REQUIRE(Kc && Vc && src_slots && dst_slots, OSC_ERR_NULL, "%s: null pointer", who);

@@ -247,3 +247,13 @@ def test_rows_of_several_launches_need_no_workspace(tmp_path):
     for T, need, code, launched in lines:
         rows = [min(2 ** 23, int(T) - r) for r in range(0, int(T), 2 ** 23)]
         assert need == "0" and code == "0" and ast.literal_eval(launched) == [(n, 1, 256) for n in rows], (T, launched)
+
+
+@pytest.mark.parametrize("Hkv,N", [(1, 2 ** 26 - 3), (1, 2 ** 26 - 2), (1, 2 ** 26 - 1), (3, (2 ** 26 - 1) // 3), (2, 2 ** 25 - 1)])
+def test_move_of_the_first_groups_that_are_too_many(Hkv, N):
+    """four heads of groups a workgroup of 256, rounded up: from 2^26 - 3 on a launch would have 2^32 threads"""
+    assert N * Hkv > 2 ** 26 - 4 and rc(MOVE, N=N, T=N, Hkv=Hkv, offs=None) == UNSUPPORTED
+
+
+def test_move_of_as_many_groups_as_there_may_be():
+    assert rc(MOVE, N=2 ** 26 - 4, T=0, Hkv=1, offs=None) == 0
