@@ -501,8 +501,10 @@ int osc_tree_mask(const int32_t *parents, const int32_t *q_offsets, const int32_
  * osc_prefix_attention, whose arguments and notes these are, for trees: row i of a request sees the prefix, the request's tokens
  * 0 .. L - n - 1, and those new tokens j <= i whose bit its words hold.  A row need not see itself; one that sees nothing gives zeros and
  * -infinity.  Bits of later rows are ignored, so any mask under the diagonal will do, not only a tree's.  A new token of which keys or
- * values are NaN or infinite touches no row but those that see it: their O becomes NaN in the token's key/value head (of a prompt's piece perhaps
- * in the values' own channels alone, infinite where they are), by keys their lse too.  All other tokens must be finite.
+ * values are NaN or infinite makes no row NaN or infinite but those that see it.  By NaN or infinite values their O becomes NaN in the token's key/value
+ * head (of a prompt's piece perhaps in the values' own channels alone, infinite where they are).  Keys act through the row's score: NaN or
+ * infinity makes O and lse of the head NaN, -infinity is a weight of 0, and a row with no other score is as one that sees nothing.  All other tokens
+ * must be finite.
  *   mask       uint64 [T, ldm], 8-byte aligned;  words  1 to 8, ldm >= words
  *   workspace  osc_tree_attention_workspace_bytes(...) bytes: osc_prefix_attention's, and 68 MB (D = 64: 52) more behind a prefix where the step has
  *              33 to 255 rows (tokens times Hq / Hkv)

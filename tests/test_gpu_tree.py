@@ -387,3 +387,47 @@ def test_attention_of_drafts_that_are_not_finite_in_long_requests(osc):
         got, was = o.view(-1, 6, 64), before.view(-1, 6, 64)
         assert torch.equal(torch.isnan(got).all(-1), sees) and torch.equal(torch.isnan(got).any(-1), sees)
         assert torch.equal(got[~sees], was[~sees]) and torch.equal(lse, lse0)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("P", [0, 300])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf")])
+def test_attention_of_drafts_with_an_infinite_key(osc, bad, P, D):
+    """an infinite key acts through its scores: a row whose score is infinity is NaN, one whose score is -infinity is as if it did not see the token, and
+    a row that sees nothing else is as one that sees nothing; requests of few rows, of more, of two tiles, a piece of a prompt"""
+    counts, kv = [9, 40, 60, 20, 100, 16], [30, 300, 461, 21, 130, 16]
+    s = make(23 + P, 6, P, kv, counts, 4, 2, D, 16)
+    mask = tree_of(0, s, counts, 1)
+    bits, offs = words_of(mask)[:, 0], np.concatenate([[0], np.cumsum(counts)])
+    q = f64(s["Q"]).reshape(-1, 4, D)
+    plain = [f64(s["V"]), s["prefix"].cpu().numpy(), P, s["table"].cpu().numpy(), s["kv"].cpu().numpy(), s["offs"].cpu().numpy(), words_of(mask), s["scale"]]
+    big = ref.tree_attention(q, f64(s["K"]), *plain)[3]
+    kinds = set()
+    for b, draft, h in ((0, 3, 1), (1, 17, 0), (2, 40, 1), (3, 19, 0), (4, 70, 1), (5, 0, 0), (2, 59, 0)):
+        j, c = kv[b] - counts[b] + draft, 7 + b
+        K = s["K"].clone()
+        K[int(s["table"][b, j // 16]), h, j % 16, c] = bad
+        o, lse = call(osc, dict(s, K=K), mask)
+        sees = np.zeros((sum(counts), 4), bool)
+        for i in range(counts[b]):
+            r = offs[b] + i
+            sees[r, 2 * h:2 * h + 2] = i >= draft if counts[b] > 64 else bits[r] >> np.uint64(draft) & np.uint64(1)
+        score = np.where(sees, np.where(q[:, :, c] == 0, np.nan, np.sign(q[:, :, c]) * bad), 0.0)
+        got, z = f64(o).reshape(-1, 4, D), f64(lse)
+        out = sees & (np.isposinf(score) | np.isnan(score))
+        assert np.array_equal(np.isnan(got).all(-1), out) and np.array_equal(np.isnan(got).any(-1), out) and np.array_equal(np.isnan(z), out)
+        with np.errstate(invalid="ignore"):
+            wo, wl, av, _ = ref.tree_attention(q, f64(K), *plain)
+        alone = sees & np.isneginf(score) & np.isnan(wl)  # of its only token a row has a score of -infinity
+        assert (got[alone] == 0).all() and np.isneginf(z[alone]).all()
+        # check()'s tolerances, with the scores of finite keys.  Rows that do not see the token are held to them too, not to equal bits: a wavefront's rows
+        # move the base of their sums together, and an infinite score moves it
+        keep = ~out & ~alone
+        err = (s["scale"] * (D + 4) * 2.0 ** -24 * big)[keep]
+        assert (np.abs(got - wo)[keep] <= 2.0 ** -8 * np.abs(wo[keep]) + (2.0 ** -8 + 2 * err[:, None] + 2.0 ** -18) * av[keep]).all()
+        empty = np.isneginf(wl[keep])
+        assert np.array_equal(np.isneginf(z[keep]), empty)
+        tol = err + 2.0 ** -21 * (np.abs(np.where(empty, 0, wl[keep])) + s["scale"] * big[keep]) + (P + max(kv) + 8) * 2.0 ** -24
+        assert (np.abs(np.where(empty, 0, z[keep]) - np.where(empty, 0, wl[keep])) <= tol).all()
+        kinds |= {n for n, m in (("out", out), ("left", sees & keep)) if m.any()}
+    assert kinds == {"out", "left"}
