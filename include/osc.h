@@ -557,7 +557,8 @@ int osc_cache_move(void *Kc, void *Vc, int32_t n_layers, int64_t layer_stride, i
  * order of the forks from the end of the free list as in osc_page_slots, and its tokens are to be moved there by osc_cache_move.
  *   refused    a fork whose src or dst is no request, whose dst is also a src or an earlier fork's dst, whose tokens do not fit a row of the
  *              table (these ask for no page), or whose page, counted over all forks up to and with it, exceeds n_free while it needs one.
- *              Its row and length stay as they are
+ *              Its row and length stay as they are: the length of a row that holds no pages must be 0, so after osc_page_free pass its new_lens
+ *              here, not the lengths from before, or a refused fork's request has tokens in pages that are on the free list
  *   src, dst   int32 [N];  kv_lens int32 [B], block_table int32 [B, ldt], refs int32 [n_pages]: in and out (pages outside [0, n_pages) are entered
  *              but not counted, and nothing of them is moved)
  *   free_pages int32 [n_pool], n_free int32 [1], info[0] the next n_free, as in osc_page_slots
@@ -575,6 +576,10 @@ int osc_page_fork(const int32_t *src, const int32_t *dst, int32_t N, int32_t B, 
  * lets go of the pages of its row from ceil(new / page_size) up to ceil(kv / page_size) - 1.  A page with refs[page] > 0 loses one
  * holder; a page that was let go by its last one is appended to the free list.  Pages freed by one call are appended in the
  * order of their numbers, each once, however often the rows name it.  The table is not written.
+ * A length that ends inside a page keeps the page, and osc_page_slots deals the rest of it.  So new_lens[b] must not end inside a page that has other
+ * holders (refs > 0), or the next tokens are written over theirs.  Tokens that were added after a fork never lie in such a page.  To shorten a request
+ * further than that, fork it: give its row the shorter length, fork it into an empty row, which gets a page of its own for the last part, move
+ * the tokens, and free the first row from its true length.
  *   refs       int32 [n_pages] or NULL (every page has one holder), in and out
  *   free_pages int32 [n_pool], in and out: the first n_free entries stay;  n_free int32 [1] (limited to n_pool); info[0] is the next one
  *   info       int32 [4]: pages free afterwards, pages appended, entries whose page has other holders, entries ignored (no page of [0, n_pages),

@@ -246,3 +246,82 @@ def test_most_requests_and_many_pages(osc):
     check_free(osc, gen.integers(0, 145, B), gen.integers(0, 60, B), 16, table, n_pages, 90000, 40, refs=refs)
     rows = gen.permutation(B)
     check_fork(osc, gen.choice(rows[4096:], 4096), rows[:4096], gen.integers(0, 65, B), 16, 4, 5000, 4100)
+
+
+def test_shorter_than_the_fork(osc):
+    """a request that goes back behind the token where it was forked: a fork of its own, and the other holder's tokens stay what they were"""
+    ps, width, n_pages = 16, 4, 20
+    K, V = caches(3, 2, n_pages, 2, ps, 64)
+    table, free, refs = i32(np.full((3, width), -1)), i32(np.arange(n_pages)[::-1].copy()), i32(np.zeros(n_pages))
+    kv, _, _, slots, info = osc.osc_page_slots(i32([0, 0, 0]), i32([40, 0, 0]), free, i32([n_pages]), table, ps, 40)
+    tokens = lambda C, row, n: C[:, table[row].long()[torch.arange(n, device=DEV) // ps], :, torch.arange(n, device=DEV) % ps].clone()
+    first = [tokens(C, 0, 40) for C in (K, V)]
+    a, b, info = osc.osc_page_fork(i32([0]), i32([1]), kv, table, refs, free, info[:1].clone(), ps)
+    osc.osc_cache_move(K, V, a, b)
+    assert kv.tolist() == [40, 40, 0] and refs[table[1, 1].long()].item() == 1
+    # row 1 back to 20 tokens, inside a page that row 0 holds too: into row 2
+    kv[1] = 20
+    a, b, info = osc.osc_page_fork(i32([1]), i32([2]), kv, table, refs, free, info[:1].clone(), ps)
+    osc.osc_cache_move(K, V, a, b)
+    kv[1] = 40
+    new = kv.clone()
+    new[1] = 0
+    info = osc.osc_page_free(kv, new, table, free, info[:1].clone(), ps, refs)
+    assert info[1:].tolist() == [1, 2, 0] and new.tolist() == [40, 0, 20]
+    kv, _, _, slots, info = osc.osc_page_slots(new, i32([0, 0, 20]), free, info[:1].clone(), table, ps, 20)
+    assert (slots >= 0).all()
+    for C in (K, V):
+        C[:, slots.long() // ps, :, slots.long() % ps] = 9.0
+    for C, was in zip((K, V), first):
+        assert torch.equal(tokens(C, 0, 40), was)
+        now = tokens(C, 2, 40)  # [tokens, layers, heads, D]
+        assert torch.equal(now[:20], was[:20]) and (now[20:] == 9).all()
+    held = {p for r, n in ((0, 3), (2, 3)) for p in table[r, :n].tolist()}
+    listed = free[:info[0].item()].tolist()
+    assert len(set(listed)) == len(listed) and not held & set(listed) and len(held) + len(listed) == n_pages
+
+
+def test_refused_forks_after_pages_were_given_back(osc):
+    """rows are dropped, the list has pages for some of the forks alone: the others are empty requests, and every page is in one place"""
+    ps, width, B, n_pages = 16, 3, 8, 26
+    table, free, refs = i32(np.full((B, width), -1)), i32(np.arange(n_pages)), i32(np.zeros(n_pages))
+    kv, _, _, _, info = osc.osc_page_slots(i32([0] * B), i32([40] * B), free, i32([n_pages]), table, ps, 40 * B)
+    assert info[0].item() == 2
+    n_free, new = info[:1].clone(), kv.clone()
+    new[4:] = 0
+    info = osc.osc_page_free(kv, new, table, free, n_free, ps, refs)
+    few = info[:1].clone() - 12  # as if others had taken twelve since
+    _, _, forked = osc.osc_page_fork(i32([0, 0, 1, 3]), i32([4, 5, 6, 7]), new, table, refs, free, few, ps)
+    assert few.item() == 2 and forked.tolist() == [0, 2, 2, 4] and new.tolist() == [40, 40, 40, 40, 40, 40, 0, 0]
+    holders = np.zeros(n_pages, int)
+    for b, n in enumerate(new.tolist()):
+        for j in range(-(-n // ps)):
+            holders[table[b, j].item()] += 1
+    assert np.array_equal(np.maximum(holders - 1, 0), refs.cpu().numpy())
+    gone = osc.osc_page_free(new, None, table, free, i32([0]), ps, refs)
+    assert gone.tolist() == [14, 14, 4, 0] and (refs == 0).all() and sorted(free[:14].tolist()) == sorted(np.flatnonzero(holders))
+
+
+@pytest.mark.parametrize("B", [400, 1024, 1025, 3000])
+@pytest.mark.parametrize("n_pages", [2 ** 19 + 1, 3 * 2 ** 19 + 40])
+def test_free_few_pages_a_request_of_many_ranges(osc, n_pages, B):
+    """no request lets more than eight pages go: pages of all ranges of bits, ends of ranges, the same page several times, pages that no cache has; one request
+    a thread and several"""
+    gen = np.random.default_rng(B)
+    edge = [p for r in range(4) for p in (r * 2 ** 19 - 1, r * 2 ** 19, r * 2 ** 19 + 1, r * 2 ** 19 + 31, r * 2 ** 19 + 32) if 0 <= p < n_pages] + [n_pages - 1, n_pages - 32]
+    table = gen.integers(0, n_pages, (B, 9))
+    flat = table.reshape(-1)
+    flat[gen.permutation(flat.size)[:8 * len(edge)]] = np.tile(edge, 8)
+    flat[gen.permutation(flat.size)[:90]] = np.tile([-1, n_pages, n_pages + 5, 2 ** 31 - 1, -2 ** 31, -2 ** 19], 15)
+    kv = gen.integers(0, 145, B)
+    new = np.maximum(kv - gen.integers(0, 129, B), 0)   # up to nine pages held, eight of them let go at most
+    keep = -(-new // 16)
+    assert (-(-kv // 16) - keep).max() == 8
+    refs = np.zeros(n_pages, int)
+    refs[gen.integers(0, n_pages, n_pages // 3)] = 1
+    refs[edge] = gen.integers(0, 9, len(edge))
+    wi = check_free(osc, kv, new, 16, table, n_pages, 30000, 11, refs=refs)
+    assert wi[1] > B and wi[2] > 0 and wi[3] > 0
+    check_free(osc, kv, new, 16, table, n_pages, 30000, 11)
+    check_free(osc, kv, new, 16, table, n_pages, B, 11, refs=refs)   # a list that is too short
+    check_free(osc, np.minimum(kv, 128), None, 16, table, n_pages, 30000, 0, refs=refs)
