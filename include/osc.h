@@ -457,7 +457,8 @@ int osc_qk_norm_rope(const void *QKV, int64_t T, int32_t Hq, int32_t Hkv, int32_
  *              row of the table can hold, and to 2^30 - 1);  q_offsets int32 [B + 1], non-decreasing, within [0, T] (otherwise nothing is
  *              computed); rows outside [q_offsets[0], q_offsets[B]) are not written
  *              A page outside [0, n_pages) is read as page 0: nothing outside the cache is touched.
- *              What pages hold past a request's last token does not matter; cached tokens must be finite.
+ *              What pages hold past a request's last token does not matter; cached tokens must be finite, and scores below 2^24 in size: single
+ *              precision cannot tell larger ones apart, and from about 2^30 on (queries and keys of 10^4 in every channel) weights may overflow
  *   scale      > 0
  *   workspace  osc_prefix_attention_workspace_bytes(...) bytes, 256-byte aligned; contents do not matter and are
  *              not kept; calls that may overlap need one each.  Its size follows from T, B, the heads and prefix_len,

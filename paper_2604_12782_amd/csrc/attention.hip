@@ -28,7 +28,7 @@
 // keys and values that one tile alone walks go past the caches (24 trees of up to 16 tokens with up to 3100 of their own 68.7 -> 61.7 us; tiles that
 // share them would lose: 95.6 -> 97.4, 192 -> 220), and so the workspace.  Those 24 trees (209 MB, 30 us at a reading pass's rate): 4.6 us until the
 // plan is there, 5 to an item's first request, 30 to 35 walking at 6 TB/s, 9 for the second kernel.  6 trees of up to 97 tokens, 3 heads of
-// 64 a key/value head, with up to 24000 of their own: 94 us, vector ALU 57 %, matrix cores 24 to 30 % busy (43 GFLOP; the cache is read
+// 64 a key/value head, with up to 24000 of their own: 88 to 92 us on the same inputs again, 97 on changing ones, vector ALU 57 %, matrix cores 24 to 30 % busy (43 GFLOP; the cache is read
 // twice from beyond L2).  Tried for trees and dropped: blocks of 32 tokens three ahead (62 -> 68 us), a block's tokens split between
 // wavefronts without rows (62 -> 63), rows on other wavefronts in the workgroups of a CU, priorities for three workgroups a CU, tiles of a request
 // cut at the same tokens (8 trees of 64 with up to 12000 141 -> 155, 6 of 97 95.6 -> 93.9).

@@ -19,10 +19,13 @@
 // (2048 rows of 131072 where thousands are equal to the largest: 317 us, not 95).
 //
 // Bounds.  2048 rows of 131072 bf16 logits, top 5: 95 us, 5.6 TB/s; 78 would be a reading pass.  Without the top 86; 4 bytes a logit 6.5 TB/s: a bf16 logit takes ten
-// operations, one of them a power.  Reads past the caches are a fifth faster (103 with plain ones): nothing here is read twice but the marked
+// operations, one of them a power.  Reads past the caches are 8 % faster (103 with plain ones): nothing here is read twice but the marked
 // chunks.  511 rows of 32000 10.1 us: 33 MB in about 4, the start and the end of a workgroup.  100 rows of 50001, four bytes each, top 20, 15.2: one
-// workgroup a CU on 100 of them, 25 GB/s each; the top's three steps (largest logits, bound, marked chunks) are 4 of it.  One row of 131072: 8.3 and 3.0 us for the
+// workgroup a CU on 100 of them, 25 GB/s each; the top's three steps (largest logits, bound, marked chunks) are 4 of it.  One row of 131072: 8.5 and 3.1 us for the
 // two kernels.  Ranking candidates on the way instead of marking them: 100 rows 30 us, 2048 126.
+// Masked logits.  Finite fills cost nothing (half or nine tenths of the 2048 rows' logits -1e4, -1e10 or -1e30: 90 to 101 us).  A chunk with -infinity leaves
+// the usual path and makes its powers twice, since 0 times -infinity is NaN: with half of the logits -infinity here and there 145 us, nine tenths 142, all behind the
+// first half 114, behind the first tenth 134.
 #include <type_traits>
 
 #include "osc_internal.h"
@@ -478,7 +481,7 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(const LogpArgs 
 // row (or the row is very long) and no more than the CUs.  us, bf16, top 5: parts of 1, 2, 4, 8, 16 of one row of 131072 logits 19.3, 16.2, 13.4, 10.9, 10.7, of
 // 64 rows 20.7, 18.5, 15.0, 14.4, 20.3, of 64 rows of 50001 13.9, 14.2, 11.5, 14.0, 20.5, of 32000 11.0, 12.0, 11.5, 14.3, 22.0.  Wavefronts a row 4, 8, 16, rows of 131072, no
 // top: 256 rows 30.9, 20.7, 17.1, 600 38.3, 33.2, 35.5, 1000 45.8, 46.2, 48.9, 2048 86.6, 85.3, 91.4, 4096 165, 160, 176; of 32000, top 5: 512 rows 18.3, 16.5, 15.8, 1000
-// 23.7, 24.5, 26.8, 4096 58.9, 69.7, 86.8.
+// 23.7, 24.5, 26.8, 4096 58.9, 69.7, 86.8.  Rows of floats, of twice the bytes, go by the same rule, which was not measured for them.
 struct LogpShape {
     int waves, splits;
 };

@@ -215,7 +215,8 @@ int launch_page_fork(const int32_t* src, const int32_t* dst, int32_t N, int32_t 
 // is a bit in LDS, and the bits' order is the list's, so the list is the same in every run and a page enters it once.  Caches of
 // more pages than bits are done range by range.  Bound by latency: lengths, sum, table, holders, bits, list.
 // Where no request lets more than FEW_PAGES go, a thread has its requests' pages itself, all of one on their way at once, and nothing is summed or
-// searched: 150 of 512 requests of up to 5 pages 6.6 us, summed and searched 7.5 (a launch alone is 2 to 3); 16 requests of up to 19 pages 4.6.
+// searched: 150 of 512 requests of up to 5 pages 6.6 us, summed and searched 7.5 (a launch alone is 2 to 3); 16 requests of up to 19 pages 4.6.  Many
+// pages are many turns of one workgroup: 150 requests of 250, 500 and 1500 pages 124, 259 and 755 us.
 constexpr int FREE_NT = 1024, FREE_WORDS = 16384;  // 2^19 pages a range, 64 KB
 constexpr int FEW_PAGES = 8;
 __global__ __launch_bounds__(FREE_NT, 1) void page_free_kernel(const int32_t* __restrict__ kv_lens, const int32_t* __restrict__ new_lens, int B, int lg, const int32_t* __restrict__ table,
